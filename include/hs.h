@@ -471,6 +471,115 @@ hs_status hs_run_feeds(const hs_feed* feeds, int n_feeds, double fps, int n_fram
 hs_status hs_partition_copy(hs_app* app, void* d_dst, const void* d_src, size_t bytes,
                             int repeats, double* seconds_per_copy);
 
+/* ---- operators of a track decoder -------------------------------------------------- */
+
+/* What a decoder with one token per tool and frame is made of, next to the network: a track's
+ * tokens carry a state from frame to frame (hs_retention, the counterpart of the ConvLSTM's state
+ * per stream) and look at the cells of the frame's feature map (hs_cross_attention); queries and
+ * keys of both are normalised and rotated by the frame's number (hs_norm_rotate).
+ *
+ * Every call enqueues its kernels on the caller's HIP stream (hip_stream: a hipStream_t of the
+ * context's device, NULL: the default stream) and returns; nothing is allocated, copied to the
+ * host or waited for, so the calls may be captured into a HIP graph.  Everything that a call reads
+ * or writes on the device must stay in place until the stream has passed it; the description and
+ * the HOST arrays it names are read during the call only.  The calls are thread-safe; two calls
+ * that may run at the same time need workspaces of their own.  All checks come before the first
+ * launch: a refused call has changed nothing.  The caller's current device is left as it was.
+ *
+ * Tensors are [batch][tokens][heads][dim], the dim values of a head side by side, the other strides
+ * the caller's (a view of a larger projection will do).  q_heads must be a multiple of the keys'
+ * heads: query head h uses key and value head h / (q_heads / kv_heads).  dims are multiples of 8,
+ * 8..128; pointers 16-byte aligned and strides multiples of 8 elements, both where more than
+ * nothing is read.  Strides of inputs may be 0 (one tensor for all) or negative; an output's rows
+ * must not overlap.  Offsets are 64-bit.  Sums, norms, softmax statistics and states are fp32; every
+ * output is rounded once. */
+typedef enum { HS_F16 = 1, HS_BF16 = 2 } hs_dtype;
+typedef struct {
+  void* d;                      /* first value of batch 0, token 0, head 0 (inputs are only read)  */
+  int64_t batch, token, head;   /* strides in elements                                             */
+} hs_heads;
+
+/* Root-mean-square norm of every head of q and k and rotation by position, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight                                      (norm != 0)
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * d_frequencies[i],
+ * for pair i of the first rotary_dim values of the head: values (2i, 2i+1) where interleaved != 0,
+ * else (i, i + rotary_dim/2); the values behind rotary_dim are only normalised.  Angles are formed
+ * in 64 bits.  q_heads or k_heads may be 0 (that side is left alone).  Outputs may be the inputs
+ * themselves (same pointer and strides); otherwise they must not overlap them. */
+typedef struct {
+  int dtype;                    /* hs_dtype of q, k and the outputs                                */
+  int batch, tokens;
+  int q_heads, k_heads;         /* here k_heads need not divide q_heads                            */
+  int head_dim;
+  hs_heads q, k, q_out, k_out;
+  int norm;                     /* 0: rotation only                                                */
+  float eps;                    /* >= 0                                                            */
+  const float* d_q_weight;      /* DEVICE fp32 [head_dim], NULL: ones                              */
+  const float* d_k_weight;
+  int rotary_dim;               /* multiple of 16, 0 (norm only) .. head_dim                       */
+  int interleaved;
+  const double* d_frequencies;  /* DEVICE [rotary_dim/2], radians per position: any base or scaling */
+  const int64_t* d_positions;   /* DEVICE, token t of batch b: d_positions[b*position_batch_stride  */
+  int64_t position_batch_stride;/* + t]; NULL: first_position + t                                  */
+  int64_t first_position;
+} hs_norm_rotate_desc;
+hs_status hs_norm_rotate(hs_ctx* ctx, const hs_norm_rotate_desc* desc, void* hip_stream);
+
+/* Linear attention with a decay for each head (a recurrent state per sequence and query head):
+ *   S_t = decay[h] * S_(t-1) + k_t v_t^T        S_0 = state_in, [key_dim][value_dim] fp32
+ *   out_t = scale * S_t^T q_t
+ * for the first lengths[b] tokens of sequence b (all of them without lengths; values outside
+ * 0..tokens are taken as the nearer end).  state_out is the state behind the sequence's last token;
+ * out is zero for the tokens behind it, whose q, k and v are not used whatever they hold.
+ * One call serves a whole clip (tokens = its frames) or one frame of every live stream
+ * (tokens = 1); a clip cut into calls gives the same results up to the order of fp32 sums.
+ * state_in may be NULL (zeros) or be state_out itself; tokens = 0 copies the state. */
+typedef struct {
+  int dtype;                    /* hs_dtype of q, k, v, out                                        */
+  int batch, tokens;
+  int q_heads, kv_heads;        /* q_heads <= HS_MAX_HEADS                                         */
+  int key_dim, value_dim;
+  float scale;
+  const double* decay;          /* HOST [q_heads], each in [0, 1]                                  */
+  hs_heads q, k, v, out;
+  const int32_t* d_lengths;     /* DEVICE [batch] or NULL                                          */
+  const float* d_state_in;      /* DEVICE [batch][q_heads][key_dim][value_dim] or NULL             */
+  float* d_state_out;           /* DEVICE, same shape                                              */
+  void* d_workspace;            /* DEVICE, 256-byte aligned, hs_query_retention_workspace() bytes  */
+  size_t workspace_bytes;
+} hs_retention_desc;
+#define HS_MAX_HEADS 64
+/* Device bytes that the call needs for this description (possibly 0; pointers are not looked at). Pure
+ * host computation.  They need no initialisation and hold nothing between calls. */
+hs_status hs_query_retention_workspace(const hs_retention_desc* desc, size_t* bytes);
+hs_status hs_retention(hs_ctx* ctx, const hs_retention_desc* desc, void* hip_stream);
+
+/* Attention of tokens to an encoder's states of another length (the cells of a feature map, or of
+ * the last frames' maps):
+ *   out = softmax(scale * q K^T over the visible keys) V
+ * A key j of batch b is visible if j < lengths[b] (all without lengths; values outside 0..k_tokens
+ * are taken as the nearer end) and, with a mask, mask[b][j] != 0.  Hidden keys and values are not used
+ * whatever they hold (infinities and NaN included).  A token that sees no key gets zeros and a log-sum-exp
+ * of minus infinity. */
+typedef struct {
+  int dtype;                    /* hs_dtype of q, k, v, out                                        */
+  int batch, q_tokens, k_tokens;
+  int q_heads, kv_heads;
+  int head_dim;                 /* of q, k, v and out                                              */
+  float scale;
+  hs_heads q, k, v, out;
+  const int32_t* d_lengths;     /* DEVICE [batch] or NULL                                          */
+  const uint8_t* d_mask;        /* DEVICE, key j of batch b: d_mask[b*mask_batch_stride + j], or NULL */
+  int64_t mask_batch_stride;    /* 0: one mask for all                                             */
+  float* d_lse;                 /* DEVICE [batch][q_heads][q_tokens]: log of the softmax's sum (of  */
+                                /* exp(scale * q k)), or NULL                                      */
+  void* d_workspace;            /* DEVICE, 256-byte aligned                                        */
+  size_t workspace_bytes;
+} hs_cross_attention_desc;
+/* As hs_query_retention_workspace. */
+hs_status hs_query_cross_attention_workspace(const hs_cross_attention_desc* desc, size_t* bytes);
+hs_status hs_cross_attention(hs_ctx* ctx, const hs_cross_attention_desc* desc, void* hip_stream);
+
 /* Thread-local, never NULL; valid until the next failing call on this thread. */
 const char* hs_last_error(void);
 /* Library version string. */

@@ -26,6 +26,9 @@ __all__ = [
     "HS_MAX_GROUP", "hs_feed", "hs_run_feeds", "hs_create_mux", "hs_destroy_mux", "hs_mux_submit",
     "hs_mux_poll", "hs_mux_wait", "hs_latency_metrics_compute", "hs_mann_whitney_u", "hs_set_cpu_affinity", "hs_set_kernel_timing", "hs_set_launch_mode", "HS_LAUNCH_GRAPH", "HS_LAUNCH_EAGER",
     "hs_get_kernel_times", "hs_device_copy", "hs_partition_copy", "hs_last_error", "hs_version", "make_desc", "cu_mask_words",
+    "HS_F16", "HS_BF16", "HS_MAX_HEADS", "hs_heads", "hs_norm_rotate_desc", "hs_retention_desc", "hs_cross_attention_desc",
+    "hs_norm_rotate", "hs_query_retention_workspace", "hs_retention", "hs_query_cross_attention_workspace",
+    "hs_cross_attention", "make_norm_rotate_desc", "make_retention_desc", "make_cross_attention_desc",
 ]
 
 HS_OK, HS_E_INVAL, HS_E_NOMEM, HS_E_OVERSUBSCRIBED = 0, -1, -2, -3
@@ -34,6 +37,8 @@ HS_NET_TINY4, HS_NET_RESNET18_CONVLSTM = 1, 2
 HS_NUM_TOOLS, HS_MAX_CU_WORDS = 8, 8
 HS_LAUNCH_GRAPH, HS_LAUNCH_EAGER = 0, 1
 HS_MAX_GROUP = 4
+HS_F16, HS_BF16 = 1, 2
+HS_MAX_HEADS = 64
 
 _STATUS_NAME = {0: "HS_OK", -1: "HS_E_INVAL", -2: "HS_E_NOMEM", -3: "HS_E_OVERSUBSCRIBED",
                 -4: "HS_E_QUEUE_FULL", -5: "HS_E_NOT_READY", -6: "HS_E_DEVICE", -7: "HS_E_STATE"}
@@ -85,6 +90,41 @@ class hs_mwu(C.Structure):
 class hs_kernel_time(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_uint64), ("total_ms", C.c_double),
                 ("flops", C.c_double), ("bytes", C.c_double)]
+
+
+class hs_heads(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class hs_norm_rotate_desc(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("batch", C.c_int), ("tokens", C.c_int), ("q_heads", C.c_int),
+        ("k_heads", C.c_int), ("head_dim", C.c_int), ("q", hs_heads), ("k", hs_heads),
+        ("q_out", hs_heads), ("k_out", hs_heads), ("norm", C.c_int), ("eps", C.c_float),
+        ("d_q_weight", C.c_void_p), ("d_k_weight", C.c_void_p), ("rotary_dim", C.c_int),
+        ("interleaved", C.c_int), ("d_frequencies", C.c_void_p), ("d_positions", C.c_void_p),
+        ("position_batch_stride", C.c_int64), ("first_position", C.c_int64),
+    ]
+
+
+class hs_retention_desc(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("batch", C.c_int), ("tokens", C.c_int), ("q_heads", C.c_int),
+        ("kv_heads", C.c_int), ("key_dim", C.c_int), ("value_dim", C.c_int), ("scale", C.c_float),
+        ("decay", C.c_void_p), ("q", hs_heads), ("k", hs_heads), ("v", hs_heads), ("out", hs_heads),
+        ("d_lengths", C.c_void_p), ("d_state_in", C.c_void_p), ("d_state_out", C.c_void_p),
+        ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class hs_cross_attention_desc(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("batch", C.c_int), ("q_tokens", C.c_int), ("k_tokens", C.c_int),
+        ("q_heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("scale", C.c_float),
+        ("q", hs_heads), ("k", hs_heads), ("v", hs_heads), ("out", hs_heads),
+        ("d_lengths", C.c_void_p), ("d_mask", C.c_void_p), ("mask_batch_stride", C.c_int64),
+        ("d_lse", C.c_void_p), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
 
 
 _lib = None
@@ -163,6 +203,12 @@ def load() -> C.CDLL:
         "hs_device_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t]),
         "hs_partition_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int,
                                         P(C.c_double)]),
+        "hs_norm_rotate": (C.c_int, [C.c_void_p, P(hs_norm_rotate_desc), C.c_void_p]),
+        "hs_query_retention_workspace": (C.c_int, [P(hs_retention_desc), P(C.c_size_t)]),
+        "hs_retention": (C.c_int, [C.c_void_p, P(hs_retention_desc), C.c_void_p]),
+        "hs_query_cross_attention_workspace": (C.c_int, [P(hs_cross_attention_desc),
+                                                         P(C.c_size_t)]),
+        "hs_cross_attention": (C.c_int, [C.c_void_p, P(hs_cross_attention_desc), C.c_void_p]),
         "hs_last_error": (C.c_char_p, []),
         "hs_version": (C.c_char_p, []),
     }
@@ -513,3 +559,71 @@ def hs_get_kernel_times(app: int) -> list:
     return [{"name": buf[i].name.decode(), "launches": buf[i].launches,
              "total_ms": buf[i].total_ms, "flops": buf[i].flops, "bytes": buf[i].bytes}
             for i in range(min(n.value, 16))]
+
+
+# ---- operators of a track decoder -----------------------------------------------------------
+def make_norm_rotate_desc(*, dtype, batch, tokens, q_heads, k_heads, head_dim, q=None, k=None,
+                          q_out=None, k_out=None, norm=True, eps=1e-6, d_q_weight=0, d_k_weight=0,
+                          rotary_dim=0, interleaved=False, d_frequencies=0, d_positions=0,
+                          position_batch_stride=0, first_position=0) -> hs_norm_rotate_desc:
+    """q, k, q_out, k_out: hs_heads (device pointer and strides); d_*: device pointers as integers."""
+    none = hs_heads()
+    return hs_norm_rotate_desc(
+        int(dtype), int(batch), int(tokens), int(q_heads), int(k_heads), int(head_dim), q or none,
+        k or none, q_out or none, k_out or none, int(bool(norm)), float(eps), d_q_weight or None,
+        d_k_weight or None, int(rotary_dim), int(bool(interleaved)), d_frequencies or None,
+        d_positions or None, int(position_batch_stride), int(first_position))
+
+
+def make_retention_desc(*, dtype, batch, tokens, q_heads, kv_heads, key_dim, value_dim, scale, decay,
+                        q=None, k=None, v=None, out=None, d_lengths=0, d_state_in=0, d_state_out=0,
+                        d_workspace=0, workspace_bytes=0) -> hs_retention_desc:
+    """decay: q_heads values (kept alive, as float64, by the returned object)."""
+    none = hs_heads()
+    g = np.ascontiguousarray(decay, dtype=np.float64)
+    if g.size != q_heads:
+        raise ValueError("decay needs one value per query head")
+    d = hs_retention_desc(
+        int(dtype), int(batch), int(tokens), int(q_heads), int(kv_heads), int(key_dim),
+        int(value_dim), float(scale), g.ctypes.data, q or none, k or none, v or none, out or none,
+        d_lengths or None, d_state_in or None, d_state_out or None, d_workspace or None,
+        int(workspace_bytes))
+    d._keepalive = g
+    return d
+
+
+def make_cross_attention_desc(*, dtype, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, scale,
+                              q=None, k=None, v=None, out=None, d_lengths=0, d_mask=0,
+                              mask_batch_stride=0, d_lse=0, d_workspace=0,
+                              workspace_bytes=0) -> hs_cross_attention_desc:
+    none = hs_heads()
+    return hs_cross_attention_desc(
+        int(dtype), int(batch), int(q_tokens), int(k_tokens), int(q_heads), int(kv_heads),
+        int(head_dim), float(scale), q or none, k or none, v or none, out or none, d_lengths or None,
+        d_mask or None, int(mask_batch_stride), d_lse or None, d_workspace or None,
+        int(workspace_bytes))
+
+
+def hs_norm_rotate(ctx: int, desc: hs_norm_rotate_desc, hip_stream: int = 0) -> None:
+    """hip_stream: a stream's handle as an integer (``torch.cuda.Stream.cuda_stream``)."""
+    _check(load().hs_norm_rotate(ctx, C.byref(desc), hip_stream))
+
+
+def hs_query_retention_workspace(desc: hs_retention_desc) -> int:
+    n = C.c_size_t()
+    _check(load().hs_query_retention_workspace(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def hs_retention(ctx: int, desc: hs_retention_desc, hip_stream: int = 0) -> None:
+    _check(load().hs_retention(ctx, C.byref(desc), hip_stream))
+
+
+def hs_query_cross_attention_workspace(desc: hs_cross_attention_desc) -> int:
+    n = C.c_size_t()
+    _check(load().hs_query_cross_attention_workspace(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def hs_cross_attention(ctx: int, desc: hs_cross_attention_desc, hip_stream: int = 0) -> None:
+    _check(load().hs_cross_attention(ctx, C.byref(desc), hip_stream))

@@ -14,7 +14,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libhs.so")
 
-SOURCES = ["hs_host.cpp", "hs_lib.cpp", "hs_driver.cpp", "hs_kernels.hip"]
+SOURCES = ["hs_host.cpp", "hs_lib.cpp", "hs_driver.cpp", "hs_track.cpp", "hs_kernels.hip",
+           "hs_norm_rotate.hip", "hs_retention.hip", "hs_cross_attention.hip"]
 
 
 def hipcc() -> str:

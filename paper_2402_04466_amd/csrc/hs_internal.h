@@ -68,6 +68,8 @@ hs_status guarded(const char* fn, F&& body) {
 // What the per-stream front (hs_mux) must know of the application it drives.
 int hs_internal_app_batch(const hs_app* app);      // streams per submit
 int hs_internal_app_grouped(const hs_app* app);    // 1 while a member of a group
+// What the track decoder's operators must know of the context they run in.
+int hs_internal_ctx_device(const hs_ctx* ctx);
 // The calling thread's current device (-1: unknown), which every call here may change.
 int hs_internal_current_device();
 void hs_internal_use_device(int device);

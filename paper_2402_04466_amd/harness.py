@@ -18,6 +18,13 @@ import torch
 from . import api
 
 
+def heads_of(t: torch.Tensor) -> api.hs_heads:
+    """A tensor [batch, tokens, heads, dim] as the track decoder's operators take it."""
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError("need [batch, tokens, heads, dim] with contiguous dim")
+    return api.hs_heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
 class AppStream:
     def __init__(self, ctx: int, *, net: int, frame_w: int, frame_h: int, net_w: int, net_h: int,
                  blob: np.ndarray, palette: np.ndarray, queue_depth: int = 2,
