@@ -3,75 +3,350 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 namespace hs {
 
-// One wave per token and head: 64 keys at a time, one per lane; running maximum and sum; then the values, two
-// dimensions per lane.
-template <class T>
-__global__ __launch_bounds__(64) void k_cross_wave(CrossParams p) {
+// out = softmax(scale * Q K^T) V by tiles of keys with a running maximum and sum.
+//
+// A wave has 32 rows (a row is a token and one of the query heads that share a key head) and forms, per tile of BN keys,
+//   S^T = K Q^T          keys x rows: a lane's 16 values per 32 keys belong to ONE row, so maximum, sum and
+//                        rescaling are per lane, with one exchange between the wave's halves;
+//   O^T += V^T P^T       whose B operand is the lane's own P, rounded to 16 bits in place: the keys that a lane holds
+//                        of S^T are taken as the product's k positions, and V^T is read from LDS (transposed) in that order.
+// The weights P are rounded once to the inputs' type, as the matrix pipe takes them; their sum is formed
+// before that, in fp32, as everything else.  Q stays in registers; K and V tiles go through registers into LDS
+// while the tile before them is computed.
+//
+// QW waves side by side have other rows and share the tiles; KW groups of them take the keys in turn and are
+// joined in LDS at the end.  Where that leaves the device idle the keys are cut further, over `splits`
+// workgroups, whose partial results k_cross_join puts together.
+constexpr float kLog2e = 1.44269504088896340736f;
+// A row's maximum is only raised, and what it has summed only rescaled, when the scores have grown by
+// more than this many powers of two: weights then stay below 2^8, as exact as weights below 1.
+constexpr float kSlack = 8.0f;
+
+struct CrossGrid {
+  int row_tiles, splits;
+};
+
+template <int CH>   // 16-byte chunks per row of a tile: 8 or 16
+__device__ __forceinline__ int swizzle(int row) {
+  // Chunk c of a row lies at c ^ swizzle(row): 16 rows' same chunk (K's reads) and 4 rows' 64 bytes (V's transposed
+  // reads) then cover all banks once.
+  return CH == 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+}
+
+template <class T, int DP, int QW, int KW, int BN>
+__global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid grid) {
   typedef typename Vec<T>::x8 x8;
-  __shared__ float s_q[128];
-  __shared__ float s_p[64];
-  const int lane = threadIdx.x;
-  const int64_t id = blockIdx.x;
-  const int t = (int)(id % p.q_tokens);
-  const int64_t bh = id / p.q_tokens;
-  const int h = (int)(bh % p.q_heads), hk = h / p.group;
-  const int64_t b = bh / p.q_heads;
-  for (int i = lane; i < p.dim; i += 64) s_q[i] = (float)at<T>(p.q, b, t, h)[i] * p.scale;
-  __syncthreads();
+  typedef typename Vec<T>::x4 x4;
+  constexpr int CH = DP / 8, KS = DP / 16, DT = DP / 32, NB = BN / 32;
+  constexpr int NT = 64 * QW;                       // threads that fill a tile together
+  constexpr int NL = BN * CH / NT;                  // 16-byte loads per thread for K, and for V
+  constexpr int kTile = BN * DP * 2;                // bytes
+  constexpr int kBuffers = QW > 1 ? 2 : 1;          // a wave alone needs no second buffer: its accesses are in order
+  constexpr int PT = DP + 4;                        // floats per row of a group's part: reads and writes spread over the banks
+  constexpr int kTiles = KW * kBuffers * 2 * kTile, kParts = KW > 1 ? KW * QW * 32 * (PT + 2) * 4 : 0;
+  constexpr int kLds = kTiles > kParts ? kTiles : kParts;
+  __shared__ __align__(16) char lds[kLds];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, qw = wave % QW, kw = wave / QW;
+  const int row_in_wave = lane & 31, half = lane >> 5;
+  char* const tiles = lds + kw * kBuffers * 2 * kTile;
+
+  // workgroups of one batch and key head next to each other on the same XCD (workgroup i runs on XCD i % 8)
+  const int total = gridDim.x, x = blockIdx.x % 8, rest = total % 8;
+  int id = x * (total / 8) + min(x, rest) + blockIdx.x / 8;
+  const int row_tile = id % grid.row_tiles;
+  id /= grid.row_tiles;
+  const int split = id % grid.splits;
+  const int bh = id / grid.splits, kv_heads = p.q_heads / p.group, hk = bh % kv_heads, b = bh / kv_heads;
+  const int64_t rows = (int64_t)p.q_tokens * p.group;
+  const int64_t row = ((int64_t)row_tile * QW + qw) * 32 + row_in_wave;
+  const bool live = row < rows;
+  const int64_t token = live ? row / p.group : 0;
+  const int head = hk * p.group + (live ? (int)(row % p.group) : 0);
+
+  // the keys of this workgroup: tiles first .. last - 1, of which group kw takes every KW-th
   const int n = length_of(p.lengths, b, p.k_tokens);
-  float top = -INFINITY, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int j0 = 0; j0 < n; j0 += 64) {
-    const int j = j0 + lane;
-    const bool seen = j < n && (!p.mask || p.mask[b * p.mask_batch + j]);
-    float s = -INFINITY;
-    if (seen) {
-      const T* const k = at<T>(p.k, b, j, hk);
-      s = 0.0f;
-      for (int i = 0; i < p.dim; i += 8) {
-        const x8 x = *(const x8*)(k + i);
+  const int all_tiles = (int)(((int64_t)n + BN - 1) / BN);
+  const int first = (int)((int64_t)all_tiles * split / grid.splits), last = (int)((int64_t)all_tiles * (split + 1) / grid.splits);
+
+  // a negative scale is taken out of Q's signs, a zero one made positive: maxima of scores are maxima of exponents
+  const float scale = p.scale == 0.0f ? 1e-30f : fabsf(p.scale), c = scale * kLog2e;
+  x8 q[KS];
+  {
+    const T* const src = at<T>(p.q, b, token, head);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(s_q[i + e], (float)x[e], s);
+    for (int k = 0; k < KS; ++k) {
+      q[k] = x8{};
+      const int d0 = 16 * k + 8 * half;
+      if (live && d0 < p.dim) q[k] = *(const x8*)(src + d0);
+      if (p.scale < 0.0f) q[k] = -q[k];
+    }
+  }
+  f32x16 o[DT] = {};
+  float m = -INFINITY, l = 0.0f;
+
+  // staging: this thread's chunk of rows r0, r0 + NT / CH, ...
+  const int tg = threadIdx.x % NT, r0 = tg / CH, ch = tg % CH;
+  const bool in_dim = 8 * ch < p.dim;
+  const T* const ksrc = at<T>(p.k, b, 0, hk) + 8 * ch;
+  const T* const vsrc = at<T>(p.v, b, 0, hk) + 8 * ch;
+  const uint8_t* const mask = p.mask ? p.mask + b * p.mask_batch : nullptr;
+  s16x8 kreg[NL], vreg[NL];
+  bool seen = false;
+  auto fetch = [&](int tile) {
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      const int j = tile * BN + r0 + e * (NT / CH);
+      kreg[e] = vreg[e] = s16x8{};
+      if (j < n && in_dim) {
+        kreg[e] = *(const s16x8*)(ksrc + j * p.k.token);
+        vreg[e] = *(const s16x8*)(vsrc + j * p.v.token);
       }
     }
-    uint64_t left = __ballot(seen);
-    if (!left) continue;
-    float m = s;
+    const int j = tile * BN + lane;
+    seen = lane < BN && j < n && (!mask || mask[j]);
+  };
+  // the tile's keys as a bit set, and its values in LDS: hidden values as zeros, whatever they hold
+  auto store = [&](char* at_tile) -> uint64_t {
+    const uint64_t visible = __ballot(seen);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    m = fmaxf(m, top);
-    const float e = seen ? expf(s - m) : 0.0f, keep = expf(top - m);
-    top = m;
-    float part = e;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) part += __shfl_xor(part, d);
-    sum = fmaf(sum, keep, part);
-    s_p[lane] = e;
-    __syncthreads();
-    o0 *= keep;
-    o1 *= keep;
-    while (left) {
-      const int i = __ffsll((unsigned long long)left) - 1;
-      left &= left - 1;
-      const T* const v = at<T>(p.v, b, j0 + i, hk);
-      if (lane < p.dim) o0 = fmaf(s_p[i], (float)v[lane], o0);
-      if (lane + 64 < p.dim) o1 = fmaf(s_p[i], (float)v[lane + 64], o1);
+    for (int e = 0; e < NL; ++e) {
+      const int r = r0 + e * (NT / CH), slot = (r * CH + (ch ^ swizzle<CH>(r))) * 16;
+      *(s16x8*)(at_tile + slot) = kreg[e];
+      *(s16x8*)(at_tile + kTile + slot) = visible >> r & 1 ? vreg[e] : s16x8{};
     }
-    __syncthreads();
+    return visible;
+  };
+  int koff[KS], voff[DT][2];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) koff[k] = (row_in_wave * CH + ((2 * k + half) ^ swizzle<CH>(row_in_wave))) * 16;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int r = 8 * s + 4 * half + (lane >> 2 & 3), cc = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+      voff[d][s] = kTile + (r * CH + (cc ^ swizzle<CH>(r))) * 16 + (lane & 1) * 8;
+    }
+
+  constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
+  const int rounds = (last - first + KW - 1) / KW;
+  if (rounds > 0) fetch(first + kw);
+  for (int i = 0; i < rounds; ++i) {
+    const int tile = first + kw + i * KW;
+    char* const here = tiles + (kBuffers == 2 ? (i & 1) * 2 * kTile : 0);
+    const uint64_t visible = store(here);
+    if (QW > 1) __syncthreads();
+    if (i + 1 < rounds) fetch(tile + KW < last ? tile + KW : INT32_MAX / BN);   // (a tile behind the last key holds nothing)
+    if (tile >= last || !visible) continue;
+
+    f32x16 s[NB];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      s[kb] = f32x16{};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) s[kb] = mfma32(*(const x8*)(here + koff[k] + kb * 32 * CH * 16), q[k], s[kb]);
+    }
+    if (visible != kAll) {
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        const uint32_t bits = (uint32_t)(visible >> (32 * kb)) >> (4 * half);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(bits >> (8 * (e / 4) + e % 4) & 1)) s[kb][e] = -INFINITY;
+      }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+    float lo, hi;
+    both_halves(top, lo, hi);
+    top = fmaxf(lo, hi);
+    if (__any((top - m) * c > kSlack)) {
+      const float raised = fmaxf(m, top), keep = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - raised) * c);
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= keep;
+      m = raised;
+    }
+    const float mc = m == -INFINITY ? 0.0f : m * c;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c, -mc));
+      float part[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[e] = (s[kb][e] + s[kb][4 + e]) + (s[kb][8 + e] + s[kb][12 + e]);
+      l += (part[0] + part[1]) + (part[2] + part[3]);
+    }
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (T)s[kb][8 * j + e];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const char* const at_v = here + (32 * kb + 16 * j) * CH * 16;
+          o[d] = mfma32(join8<T>(read_transposed(at_v + voff[d][0]), read_transposed(at_v + voff[d][1])), w, o[d]);
+        }
+      }
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  T* const out = at_out<T>(p.out, b, t, h);
-  if (lane < p.dim) out[lane] = (T)(o0 * inv);
-  if (lane + 64 < p.dim) out[lane + 64] = (T)(o1 * inv);
-  if (p.lse && lane == 0) p.lse[bh * p.q_tokens + t] = top + logf(sum);
+  float lower, upper;
+  both_halves(l, lower, upper);
+  l = lower + upper;
+
+  if (KW > 1) {   // the groups' parts of the same rows
+    float* const part_o = (float*)lds;
+    float* const part_ml = part_o + KW * QW * 32 * PT;
+    __syncthreads();
+    if (half == 0) {
+      part_ml[2 * (wave * 32 + row_in_wave)] = m;
+      part_ml[2 * (wave * 32 + row_in_wave) + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *(f32x4*)(part_o + (wave * 32 + row_in_wave) * PT + 32 * d + 2 * e + 4 * half) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+    __syncthreads();
+    // thread t: row t / 8 (of QW * 32), values 4 * (t % 8 + 8 * i)
+    for (int r = threadIdx.x / 8; r < QW * 32; r += 8 * QW * KW) {
+      const int64_t at_row = (int64_t)row_tile * QW * 32 + r;
+      if (at_row >= rows) break;
+      float mm = -INFINITY, ll = 0.0f, f[KW];
+#pragma unroll
+      for (int g = 0; g < KW; ++g) mm = fmaxf(mm, part_ml[2 * (g * QW * 32 + r)]);
+#pragma unroll
+      for (int g = 0; g < KW; ++g) {
+        const float mg = part_ml[2 * (g * QW * 32 + r)];
+        f[g] = mg == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mg - mm) * c);
+        ll = fmaf(part_ml[2 * (g * QW * 32 + r) + 1], f[g], ll);
+      }
+      const bool whole = grid.splits == 1;
+      const float inv = whole ? ll > 0.0f ? 1.0f / ll : ll == 0.0f ? 0.0f : ll : 1.0f;
+      const int64_t tok = at_row / p.group;
+      const int hh = hk * p.group + (int)(at_row % p.group);
+      const int64_t part_row = (int64_t)(split * (int64_t)(p.batch * kv_heads) + bh) * rows + at_row;
+      for (int d0 = 4 * (threadIdx.x % 8); d0 < p.dim; d0 += 32) {
+        f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int g = 0; g < KW; ++g) sum += f[g] * *(const f32x4*)(part_o + (g * QW * 32 + r) * PT + d0);
+        if (whole) {
+          x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
+          *(x4*)(at_out<T>(p.out, b, tok, hh) + d0) = y;
+        } else {
+          *(f32x4*)(p.parts + part_row * (p.dim + 4) + 4 + d0) = sum;
+        }
+      }
+      if (threadIdx.x % 8 == 0) {
+        if (!whole) {
+          p.parts[part_row * (p.dim + 4)] = mm;
+          p.parts[part_row * (p.dim + 4) + 1] = ll;
+        } else if (p.lse) {
+          p.lse[((int64_t)b * p.q_heads + hh) * p.q_tokens + tok] = ll == 0.0f ? -INFINITY : fmaf(mm, scale, logf(ll));
+        }
+      }
+    }
+    return;
+  }
+  if (!live) return;
+  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  T* const dst = at_out<T>(p.out, b, token, head);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const int d0 = 32 * d + 2 * e + 4 * half;
+      x4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = (T)(o[d][e + i] * inv);
+      if (d0 < p.dim) *(x4*)(dst + d0) = y;
+    }
+  if (p.lse && half == 0) p.lse[((int64_t)b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l));
+}
+
+// The splits' parts of a row, each a maximum, a sum and a weighted sum of values: 32 lanes per row.
+template <class T>
+__global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
+  typedef typename Vec<T>::x4 x4;
+  const int kv_heads = p.q_heads / p.group;
+  const int64_t rows = (int64_t)p.q_tokens * p.group, all = (int64_t)p.batch * kv_heads * rows;
+  const int64_t id = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  if (id >= all) return;
+  const float scale = p.scale == 0.0f ? 1e-30f : fabsf(p.scale), c = scale * kLog2e;
+  const int64_t row = id % rows, bh = id / rows, b = bh / kv_heads, token = row / p.group;
+  const int head = (int)(bh % kv_heads) * p.group + (int)(row % p.group);
+  const int d0 = 4 * (threadIdx.x % 32), pitch = p.dim + 4;
+  float m = -INFINITY, l = 0.0f;
+  f32x4 sum = {0, 0, 0, 0};
+  for (int s = 0; s < splits; ++s) m = fmaxf(m, p.parts[(s * all + id) * pitch]);
+  for (int s = 0; s < splits; ++s) {
+    const float* const part = p.parts + (s * all + id) * pitch;
+    if (part[0] == -INFINITY) continue;
+    const float f = __builtin_amdgcn_exp2f((part[0] - m) * c);
+    l = fmaf(part[1], f, l);
+    if (d0 < p.dim) sum += f * *(const f32x4*)(part + 4 + d0);
+  }
+  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  if (d0 < p.dim) {
+    x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
+    *(x4*)(at_out<T>(p.out, b, token, head) + d0) = y;
+  }
+  if (p.lse && threadIdx.x % 32 == 0) p.lse[(b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l));
+}
+
+namespace {
+struct CrossPlan {
+  bool wide;                    // four waves with 32 rows each, else one set of 32 rows with the keys dealt to four waves
+  CrossGrid grid;
+  int64_t workgroups;
+};
+CrossPlan plan_of(const CrossParams& p) {
+  const int64_t bh = (int64_t)p.batch * (p.q_heads / p.group), rows = (int64_t)p.q_tokens * p.group;
+  CrossPlan plan;
+  plan.wide = bh * ((rows + 127) / 128) >= 256;
+  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? (rows + 127) / 128 : (rows + 31) / 32, INT32_MAX);
+  plan.grid.splits = 1;
+  if (!plan.wide) {
+    // two rounds of workgroups where the keys are enough for two tiles per wave
+    const int64_t tiles = (p.k_tokens + 31) / 32, base = bh * plan.grid.row_tiles;
+    plan.grid.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(base, 1), tiles / 8));
+  }
+  plan.workgroups = bh * plan.grid.row_tiles * plan.grid.splits;
+  return plan;
+}
+}  // namespace
+
+size_t cross_workspace(const CrossParams& p) {
+  const CrossPlan plan = plan_of(p);
+  return plan.grid.splits == 1 ? 0 : (size_t)plan.grid.splits * p.batch * p.q_heads * p.q_tokens * (p.dim + 4) * sizeof(float);
 }
 
 hipError_t launch(const CrossParams& p, hipStream_t stream) {
   CrossParams params = p;
-  void* args[] = {&params};
-  return launch_kernel(p.dtype == HS_F16 ? (const void*)k_cross_wave<f16> : (const void*)k_cross_wave<bf16>,
-                       (int64_t)p.batch * p.q_heads * p.q_tokens, 64, args, stream);
+  CrossPlan plan = plan_of(p);
+  void* args[] = {&params, &plan.grid};
+  const bool narrow = p.dim <= 64, half = p.dtype == HS_F16;
+  const void* kernel;
+  if (plan.wide) kernel = half ? narrow ? (const void*)k_cross<f16, 64, 4, 1, 64> : (const void*)k_cross<f16, 128, 4, 1, 64>
+                               : narrow ? (const void*)k_cross<bf16, 64, 4, 1, 64> : (const void*)k_cross<bf16, 128, 4, 1, 64>;
+  else kernel = half ? narrow ? (const void*)k_cross<f16, 64, 1, 4, 32> : (const void*)k_cross<f16, 128, 1, 4, 32>
+                     : narrow ? (const void*)k_cross<bf16, 64, 1, 4, 32> : (const void*)k_cross<bf16, 128, 1, 4, 32>;
+  hipError_t e = launch_kernel(kernel, plan.workgroups, 256, args, stream);
+  if (e != hipSuccess || plan.grid.splits == 1) return e;
+  void* join_args[] = {&params, &plan.grid.splits};
+  return launch_kernel(half ? (const void*)k_cross_join<f16> : (const void*)k_cross_join<bf16>,
+                       ((int64_t)p.batch * p.q_heads * p.q_tokens + 7) / 8, 256, join_args, stream);
 }
 
 }  // namespace hs

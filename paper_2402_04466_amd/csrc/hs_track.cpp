@@ -225,6 +225,7 @@ CrossParams params_of(const hs_cross_attention_desc* d) {
   p.q_heads = d->q_heads; p.group = d->q_heads / d->kv_heads;
   p.dim = d->head_dim;
   p.scale = d->scale;
+  p.parts = (float*)d->d_workspace;
   return p;
 }
 
@@ -294,7 +295,7 @@ hs_status hs_query_cross_attention_workspace(const hs_cross_attention_desc* desc
   return guarded(fn, [&]() -> hs_status {
   if (!bytes) { set_error("%s: NULL bytes", fn); return HS_E_INVAL; }
   HS_TRY(check(fn, desc));
-  *bytes = 0;
+  *bytes = cross_workspace(params_of(desc));
   return HS_OK;
   });
 }
@@ -314,7 +315,7 @@ hs_status hs_cross_attention(hs_ctx* ctx, const hs_cross_attention_desc* desc, v
     HS_TRY(check_pointer(fn, "d_lengths", desc->d_lengths, 4));
     HS_TRY(check_pointer(fn, "d_lse", desc->d_lse, 4));
   }
-  HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, 0));
+  HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, cross_workspace(params_of(desc))));
   HS_TRY(check_context(fn, ctx));
   if (!any) return HS_OK;
   return run(fn, ctx, params_of(desc), hip_stream);

@@ -48,7 +48,9 @@ struct CrossParams {
   float* lse;                    // NULL: not wanted
   int dtype, batch, q_tokens, k_tokens, q_heads, group, dim;
   float scale;
+  float* parts;                  // workspace: cross_workspace() bytes
 };
+size_t cross_workspace(const CrossParams& p);
 hipError_t launch(const CrossParams& p, hipStream_t stream);
 
 }  // namespace hs

@@ -17,6 +17,33 @@ template <> struct Vec<bf16> {
   typedef bf16 x8 __attribute__((ext_vector_type(8)));
 };
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// D[32][32] += A[32][16] B[16][32].  Lane l has A[l % 32][8 * (l / 32) + i], B[8 * (l / 32) + i][l % 32], i < 8, and
+// D[8 * (i / 4) + 4 * (l / 32) + i % 4][l % 32], i < 16.
+__device__ __forceinline__ f32x16 mfma32(Vec<f16>::x8 a, Vec<f16>::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma32(Vec<bf16>::x8 a, Vec<bf16>::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// Transposed read from LDS: of each 16 lanes, lane l gives the address of 4 values of row l / 4, columns 4 * (l % 4) .. + 3,
+// and receives column l of the four rows.
+__device__ __forceinline__ s16x4 read_transposed(const char* lds) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds);
+}
+template <class T>
+__device__ __forceinline__ typename Vec<T>::x8 join8(s16x4 a, s16x4 b) {
+  return __builtin_bit_cast(typename Vec<T>::x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// The value of lane l ^ 32 is among the two; both halves get both.
+__device__ __forceinline__ void both_halves(float x, float& lower, float& upper) {
+  const unsigned bits = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+  const unsigned r0 = r[0], r1 = r[1];   // (a bit cast of an element itself gives element 0)
+  lower = __builtin_bit_cast(float, r0);
+  upper = __builtin_bit_cast(float, r1);
+}
 
 template <class T>
 __device__ __forceinline__ const T* at(const Heads& h, int64_t batch, int64_t token, int64_t head) {
