@@ -25,17 +25,14 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // A row's maximum is only raised, and what it has summed only rescaled, when the scores have grown by
 // more than this many powers of two: weights then stay below 2^8, as exact as weights below 1.
 constexpr float kSlack = 8.0f;
+// fp16 weights are formed 2^7 times as large, below 2^15 then: those of up to 2^-21 of the largest keep all their bits, and
+// what is lost of the others stays below 2^-32 of it.
+template <class T> constexpr float kRaise = __is_same(T, f16) ? 7.0f : 0.0f;
+constexpr float kLn2 = 0.69314718055994530942f;
 
 struct CrossGrid {
   int row_tiles, splits;
 };
-
-template <int CH>   // 16-byte chunks per row of a tile: 8 or 16
-__device__ __forceinline__ int swizzle(int row) {
-  // Chunk c of a row lies at c ^ swizzle(row): 16 rows' same chunk (K's reads) and 4 rows' 64 bytes (V's transposed
-  // reads) then cover all banks once.
-  return CH == 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
-}
 
 template <class T, int DP, int QW, int KW, int BN>
 __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid grid) {
@@ -54,9 +51,8 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
   const int row_in_wave = lane & 31, half = lane >> 5;
   char* const tiles = lds + kw * kBuffers * 2 * kTile;
 
-  // workgroups of one batch and key head next to each other on the same XCD (workgroup i runs on XCD i % 8)
-  const int total = gridDim.x, x = blockIdx.x % 8, rest = total % 8;
-  int id = x * (total / 8) + min(x, rest) + blockIdx.x / 8;
+  // the workgroups of one batch and key head read the same keys: on the same XCD
+  int id = xcd_number();
   const int row_tile = id % grid.row_tiles;
   id /= grid.row_tiles;
   const int split = id % grid.splits;
@@ -114,21 +110,21 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
     const uint64_t visible = __ballot(seen);
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
-      const int r = r0 + e * (NT / CH), slot = (r * CH + (ch ^ swizzle<CH>(r))) * 16;
-      *(s16x8*)(at_tile + slot) = kreg[e];
-      *(s16x8*)(at_tile + kTile + slot) = visible >> r & 1 ? vreg[e] : s16x8{};
+      const int r = r0 + e * (NT / CH), to = slot<CH>(r, ch);
+      *(s16x8*)(at_tile + to) = kreg[e];
+      *(s16x8*)(at_tile + kTile + to) = visible >> r & 1 ? vreg[e] : s16x8{};
     }
     return visible;
   };
   int koff[KS], voff[DT][2];
 #pragma unroll
-  for (int k = 0; k < KS; ++k) koff[k] = (row_in_wave * CH + ((2 * k + half) ^ swizzle<CH>(row_in_wave))) * 16;
+  for (int k = 0; k < KS; ++k) koff[k] = slot<CH>(row_in_wave, 2 * k + half);
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int r = 8 * s + 4 * half + (lane >> 2 & 3), cc = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-      voff[d][s] = kTile + (r * CH + (cc ^ swizzle<CH>(r))) * 16 + (lane & 1) * 8;
+      voff[d][s] = kTile + slot<CH>(r, cc) + (lane & 1) * 8;
     }
 
   constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
@@ -173,7 +169,7 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
       for (int d = 0; d < DT; ++d) o[d] *= keep;
       m = raised;
     }
-    const float mc = m == -INFINITY ? 0.0f : m * c;
+    const float mc = m == -INFINITY ? 0.0f : fmaf(m, c, -kRaise<T>);
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
@@ -251,7 +247,7 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
           p.parts[part_row * (p.dim + 4)] = mm;
           p.parts[part_row * (p.dim + 4) + 1] = ll;
         } else if (p.lse) {
-          p.lse[((int64_t)b * p.q_heads + hh) * p.q_tokens + tok] = ll == 0.0f ? -INFINITY : fmaf(mm, scale, logf(ll));
+          p.lse[((int64_t)b * p.q_heads + hh) * p.q_tokens + tok] = ll == 0.0f ? -INFINITY : fmaf(mm, scale, logf(ll) - kRaise<T> * kLn2);
         }
       }
     }
@@ -270,7 +266,7 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
       for (int i = 0; i < 4; ++i) y[i] = (T)(o[d][e + i] * inv);
       if (d0 < p.dim) *(x4*)(dst + d0) = y;
     }
-  if (p.lse && half == 0) p.lse[((int64_t)b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l));
+  if (p.lse && half == 0) p.lse[((int64_t)b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l) - kRaise<T> * kLn2);
 }
 
 // The splits' parts of a row, each a maximum, a sum and a weighted sum of values: 32 lanes per row.
@@ -302,7 +298,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
     for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
     *(x4*)(at_out<T>(p.out, b, token, head) + d0) = y;
   }
-  if (p.lse && threadIdx.x % 32 == 0) p.lse[(b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l));
+  if (p.lse && threadIdx.x % 32 == 0) p.lse[(b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l) - kRaise<T> * kLn2);
 }
 
 namespace {

@@ -200,6 +200,7 @@ RetentionParams params_of(const hs_retention_desc* d) {
   for (int h = 0; h < d->q_heads; ++h) {
     p.decay[h] = (float)d->decay[h];
     p.decay_rest[h] = (float)(d->decay[h] - (double)p.decay[h]);
+    p.log2_decay[h] = std::max(std::log2(d->decay[h]), -1e4);   // (a decay of 0: 2^0 = 1 after no step, 0 after one)
   }
   return p;
 }

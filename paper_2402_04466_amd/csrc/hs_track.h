@@ -37,6 +37,7 @@ struct RetentionParams {
   int dtype, batch, tokens, q_heads, group, key_dim, value_dim;   // group: query heads per key head
   float scale;
   float decay[HS_MAX_HEADS], decay_rest[HS_MAX_HEADS];   // the decay in two parts, 48 bits of it together
+  double log2_decay[HS_MAX_HEADS];
 };
 hipError_t launch(const RetentionParams& p, hipStream_t stream);
 

@@ -26,6 +26,29 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ f32x16 mfma32(Vec<f16>::x8 a, Vec<f16>::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma32(Vec<bf16>::x8 a, Vec<bf16>::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
+// D[16][16] += A[16][32] B[32][16].  Lane l has A[l % 16][8 * (l / 16) + i], B[8 * (l / 16) + i][l % 16], i < 8, and
+// D[4 * (l / 16) + i][l % 16], i < 4.
+__device__ __forceinline__ f32x4 mfma16(Vec<f16>::x8 a, Vec<f16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma16(Vec<bf16>::x8 a, Vec<bf16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// A tile of 16-bit values in LDS, CH 16-byte chunks per row (8 or 16): chunk c of a row lies at c ^ swizzle(row).  16 rows' same
+// chunk (an operand read along the rows) and 4 or 8 rows' neighbouring ones (a transposed read) then cover all
+// banks once.
+template <int CH>
+__device__ __forceinline__ int swizzle(int row) {
+  return CH == 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+}
+template <int CH>   // byte offset of chunk c of a row
+__device__ __forceinline__ int slot(int row, int c) {
+  return (row * CH + (c ^ swizzle<CH>(row))) * 16;
+}
+
+// Workgroup i runs on XCD i % 8; this numbers the workgroups so that consecutive numbers share an XCD and its L2.
+__device__ __forceinline__ int xcd_number() {
+  const int total = gridDim.x, x = blockIdx.x % 8;
+  return x * (total / 8) + min(x, total % 8) + blockIdx.x / 8;
+}
+
 // Transposed read from LDS: of each 16 lanes, lane l gives the address of 4 values of row l / 4, columns 4 * (l % 4) .. + 3,
 // and receives column l of the four rows.
 __device__ __forceinline__ s16x4 read_transposed(const char* lds) {
