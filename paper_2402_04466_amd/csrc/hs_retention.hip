@@ -79,10 +79,13 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 // i, j = 0 .. c - 1:
 //   A_ij = scale * decay^(i - j) q_i k_j (j <= i)          out_i = sum_j A_ij v_j + scale * decay^(i + 1) S^T q_i
 //   S   <- decay^c S + sum_j k_j (decay^(c - 1 - j) v_j)^T
-// A workgroup has one sequence and head and 64 of the values' dimensions, 16 per wave.  The four waves share
-// the lower triangle of A (through LDS); all else of a chunk is a wave's own: its slice of the state stays in the
-// accumulators, whose layout is at once that of the operand S^T of the next chunk's S^T Q^T, if that product takes the
-// key dimensions in the accumulators' order (Q is read in it).
+// A workgroup has one sequence and head and 64 of the values' dimensions, and waves of two kinds, one of each per SIMD:
+//   waves 0 .. 3 carry the state, 16 of the dimensions each, in their accumulators, and leave a 16-bit copy of it in LDS
+//   for the next chunk;
+//   waves 4 .. 7 form out, 16 of the chunk's rows each: A by K Q^T, so that a lane holds four keys of one row per tile
+//   and A is the operand of the next product where it lies, if that one takes V's rows in the same order.
+// While a chunk is worked on the next one goes from registers into the other half of LDS and the one behind it is on
+// its way from memory; one barrier a chunk.
 //
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
 // is then half a step off, as out itself); of the fp16 copy a power of two is taken out, so that it stays in
@@ -91,216 +94,237 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 constexpr int kChunk = 64;
 
 template <class T, int KP>
-__global__ __launch_bounds__(256) void k_retain_chunks(RetentionParams p) {
+__global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
-  constexpr int CH = KP / 8, KT = KP / 16, KS = KP / 32;
-  constexpr int RP = 256 / CH, NL = kChunk / RP;    // rows per pass of the workgroup over Q or K, passes
+  constexpr int CH = KP / 8, KT = KP / 16, KS = KP / 32;   // KT: 16-wide tiles of key dimensions, KS: steps of 32
+  constexpr int RP = 512 / CH, NL = kChunk / RP;    // rows per pass of the workgroup over Q or K, passes
   constexpr bool kHalf = __is_same(T, f16);
-  constexpr int kQ = 0, kK = kChunk * KP * 2, kV = 2 * kK, kA = kV + kChunk * 64 * 2;
-  __shared__ __align__(16) char lds[kA + kChunk * kChunk * 2];
+  constexpr int kK = kChunk * KP * 2, kV = 2 * kK, kSlot = kV + kChunk * 64 * 2;   // Q, K and V of a chunk
+  constexpr int kS = 2 * kSlot, kCopy = 64 * KP * 2;
+  __shared__ __align__(16) char lds[kS + 2 * kCopy];
+  __shared__ int exponents[2][4];
   __shared__ double power[kChunk + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w4 = wave & 3, l16 = lane & 15, g = lane >> 4;
   const int blocks = (p.value_dim + 63) / 64;
   const int id = xcd_number(), block = id % blocks, bh = id / blocks, h = bh % p.q_heads, hk = h / p.group, b = bh / p.q_heads;
   const int n = length_of(p.lengths, b, p.tokens), chunks = (int)(((int64_t)n + kChunk - 1) / kChunk);
-  const int dv0 = 64 * block + 16 * wave;           // the wave's 16 dimensions
 
-  if (threadIdx.x <= kChunk) power[threadIdx.x] = exp2(p.log2_decay[h] * threadIdx.x);
-
-  // staging: this thread's 16-byte chunk of rows r0, r0 + RP, ... of Q and K, and of V (8 chunks per row)
-  const int r0 = threadIdx.x / CH, ch = threadIdx.x % CH, vr0 = threadIdx.x / 8, vch = threadIdx.x % 8;
+  // staging: this thread's 16-byte piece of rows r0, r0 + RP, ... of Q and K, and of a row of V (8 pieces)
+  const int r0 = threadIdx.x / CH, ch = threadIdx.x % CH, vr = threadIdx.x / 8, vch = threadIdx.x % 8;
   const bool in_k = 8 * ch < p.key_dim, in_v = 64 * block + 8 * vch < p.value_dim;
   const T* const qsrc = at<T>(p.q, b, 0, h) + 8 * ch;
   const T* const ksrc = at<T>(p.k, b, 0, hk) + 8 * ch;
   const T* const vsrc = at<T>(p.v, b, 0, hk) + 64 * block + 8 * vch;
-  s16x8 qreg[NL], kreg[NL], vreg[2];
-  auto fetch = [&](int t0) {
+  s16x8 qreg[NL], kreg[NL], vreg;
+  auto fetch = [&](int c) {
+    const int64_t t0 = (int64_t)c * kChunk;
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
-      const int t = t0 + r0 + e * RP;
+      const int64_t t = t0 + r0 + e * RP;
       qreg[e] = kreg[e] = s16x8{};
       if (t < n && in_k) {
         qreg[e] = *(const s16x8*)(qsrc + t * p.q.token);
         kreg[e] = *(const s16x8*)(ksrc + t * p.k.token);
       }
     }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int t = t0 + vr0 + e * 32;
-      vreg[e] = s16x8{};
-      if (t < n && in_v) vreg[e] = *(const s16x8*)(vsrc + t * p.v.token);
-    }
+    vreg = s16x8{};
+    if (t0 + vr < n && in_v) vreg = *(const s16x8*)(vsrc + (t0 + vr) * p.v.token);
   };
-  if (chunks) fetch(0);
-
-  // the state's slice: lane has dimension dv0 + l16, key dimensions 16 t + 4 g + i
-  f32x4 S[KT];
-  const int64_t state0 = (int64_t)bh * p.key_dim * p.value_dim + dv0 + l16;
-  const bool in_state = dv0 + l16 < p.value_dim;
-#pragma unroll
-  for (int t = 0; t < KT; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int dk = 16 * t + 4 * g + i;
-      S[t][i] = p.state_in && in_state && dk < p.key_dim ? p.state_in[state0 + (int64_t)dk * p.value_dim] : 0.0f;
-    }
-
-  __syncthreads();
-  float diagonal[4][4], after[4], weight[2][8];     // decays of A's tiles by distance, of S in out_i, of v_j in S
-#pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    after[d] = p.scale * (float)power[16 * d + l16 + 1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int apart = 16 * d + l16 - 4 * g - i;
-      diagonal[d][i] = apart < 0 ? 0.0f : p.scale * (float)power[apart];
-    }
-  }
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[kChunk - 1 - (32 * s + 8 * g + i)];
-  float keep = (float)power[kChunk], keep_rest = (float)(power[kChunk] - (double)keep);
-
-  for (int c = 0; c < chunks; ++c) {
-    const int t0 = c * kChunk, left = min(n - t0, kChunk);
-    if (c) __syncthreads();                         // the chunk before this one has been read
+  auto store = [&](char* to) {
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
-      *(s16x8*)(lds + kQ + slot<CH>(r0 + e * RP, ch)) = qreg[e];
-      *(s16x8*)(lds + kK + slot<CH>(r0 + e * RP, ch)) = kreg[e];
+      *(s16x8*)(to + slot<CH>(r0 + e * RP, ch)) = qreg[e];
+      *(s16x8*)(to + kK + slot<CH>(r0 + e * RP, ch)) = kreg[e];
     }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) *(s16x8*)(lds + kV + slot<8>(vr0 + e * 32, vch)) = vreg[e];
-    __syncthreads();
-    if (c + 1 < chunks) fetch(t0 + kChunk);
+    *(s16x8*)(to + kV + slot<8>(vr, vch)) = vreg;
+  };
+  if (chunks) fetch(0);
+  if (threadIdx.x <= kChunk) power[threadIdx.x] = exp2(p.log2_decay[h] * threadIdx.x);
 
-    // A's ten tiles on and below the diagonal, dealt to the waves: tile (row block, column block)
+  if (wave < 4) {
+    // ---- the state: lane has dimension dv, key dimensions 16 t + 4 g + i
+    const int dv = 64 * block + 16 * w4 + l16;
+    const int64_t state0 = (int64_t)bh * p.key_dim * p.value_dim + dv;
+    f32x4 S[KT];
 #pragma unroll
-    for (int e = 0; e < 3; ++e) {
-      const int tile = wave + 4 * e;
-      if (tile >= 10) break;
-      const int rb = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, cb = tile - rb * (rb + 1) / 2;
-      f32x4 a = {0, 0, 0, 0};
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-        a = mfma16(*(const x8*)(lds + kK + slot<CH>(16 * cb + l16, 4 * s + g)), *(const x8*)(lds + kQ + slot<CH>(16 * rb + l16, 4 * s + g)), a);
-      x4 r;
+    for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float d = diagonal[0][i];
-        d = rb - cb == 1 ? diagonal[1][i] : d;
-        d = rb - cb == 2 ? diagonal[2][i] : d;
-        d = rb - cb == 3 ? diagonal[3][i] : d;
-        r[i] = (T)(a[i] * d);
+        const int dk = 16 * t + 4 * g + i;
+        S[t][i] = p.state_in && dv < p.value_dim && dk < p.key_dim ? p.state_in[state0 + (int64_t)dk * p.value_dim] : 0.0f;
       }
-      *(x4*)(lds + kA + slot<8>(16 * rb + l16, 2 * cb + (g >> 1)) + (g & 1) * 8) = r;
+    if (chunks) {
+      store(lds);
+      fetch(1);
     }
-    // (tile (0, 1) and (2, 3), right of the diagonal but within a step of 32 keys, are zeros from the start)
-    if (c == 0 && wave < 2) *(x4*)(lds + kA + slot<8>(32 * wave + l16, 4 * wave + 2 + (g >> 1)) + (g & 1) * 8) = x4{};
+    // the state's 16-bit copy, [dimension][key dimension]
+    auto leave_copy = [&](int to) {
+      int exponent = 0;
+      if (kHalf) {
+        float most = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(S[t][i]));
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        exponent = max(min(__builtin_amdgcn_frexp_expf(most) - 12, 100), -100);
+        if (lane == 0) exponents[to][w4] = exponent;
+      }
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (T)(kHalf ? ldexpf(S[t][i], -exponent) : S[t][i]);
+        *(x4*)(lds + kS + to * kCopy + slot<CH>(16 * w4 + l16, 2 * t + (g >> 1)) + (g & 1) * 8) = w;
+      }
+    };
+    leave_copy(0);
     __syncthreads();
-
-    // V^T, the operand of both products: dimension 16 * wave + l16, tokens 32 s + 8 g + i
-    x8 v[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int r = 32 * s + 8 * g + (lane >> 2 & 3), cc = 2 * wave + (lane >> 1 & 1);
-      v[s] = join8<T>(read_transposed(lds + kV + slot<8>(r, cc) + (lane & 1) * 8), read_transposed(lds + kV + slot<8>(r + 4, cc) + (lane & 1) * 8));
-    }
-    int exponent = 0;                               // of what is taken out of the copy
-    if (kHalf) {
-      float most = 0.0f;
-#pragma unroll
-      for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(S[t][i]));
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-      exponent = max(min(__builtin_amdgcn_frexp_expf(most) - 12, 100), -100);
-    }
-    x8 s16[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s16[s][i] = (T)(kHalf ? ldexpf(S[2 * s + i / 4][i % 4], -exponent) : S[2 * s + i / 4][i % 4]);
-    f32x4 out[4];
-#pragma unroll
-    for (int rb = 0; rb < 4; ++rb) {
-      f32x4 o = {0, 0, 0, 0};
-      const int r = 16 * rb + l16;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const x4 q0 = *(const x4*)(lds + kQ + slot<CH>(r, 4 * s + (g >> 1)) + (g & 1) * 8);
-        const x4 q1 = *(const x4*)(lds + kQ + slot<CH>(r, 4 * s + 2 + (g >> 1)) + (g & 1) * 8);
-        o = mfma16(s16[s], __builtin_shufflevector(q0, q1, 0, 1, 2, 3, 4, 5, 6, 7), o);
-      }
-      o *= kHalf ? ldexpf(after[rb], exponent) : after[rb];
-#pragma unroll
-      for (int s = 0; s <= rb / 2; ++s) o = mfma16(v[s], *(const x8*)(lds + kA + slot<8>(r, 4 * s + g)), o);
-      out[rb] = o;
-    }
-
-    // the state
-    if (left < kChunk) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[max(left - 1 - (32 * s + 8 * g + i), 0)];   // (later values are zeros)
-      keep = (float)power[left];
-      keep_rest = (float)(power[left] - (double)keep);
-    }
-    x8 part[2][3];
+    float weight[2][8];                             // decays of v_j in S
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float x = (float)v[s][i] * weight[s][i];
-        asm("" : "+v"(x));   // the rounded product: rounded to 16 bits from the exact one in one place and from this in another, a part
-                             // and what is left of it would not belong together
-        part[s][0][i] = (T)x;
-        x -= (float)part[s][0][i];
-        if (kHalf) x *= 4096.0f;
-        part[s][1][i] = (T)x;
-        if (!kHalf) part[s][2][i] = (T)(x - (float)part[s][1][i]);
+      for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[kChunk - 1 - (32 * s + 8 * g + i)];
+    float keep = (float)power[kChunk], keep_rest = (float)(power[kChunk] - (double)keep);
+
+    for (int c = 0; c < chunks; ++c) {
+      char* const here = lds + (c & 1) * kSlot;
+      if (c + 1 < chunks) {
+        store(lds + (~c & 1) * kSlot);
+        fetch(c + 2);
       }
+      const int left = n - c * kChunk;
+      if (left < kChunk) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) S[t][i] = fmaf(S[t][i], keep, S[t][i] * keep_rest);
-      f32x4 low = {0, 0, 0, 0};
+          for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[max(left - 1 - (32 * s + 8 * g + i), 0)];   // (later values are zeros)
+        keep = (float)power[left];
+        keep_rest = (float)(power[left] - (double)keep);
+      }
+      x8 part[2][3];                                // decayed values: dimension 16 w4 + l16, tokens 32 s + 8 g + i
+      const int r = 8 * g + (lane >> 2 & 3), low8 = (lane & 1) * 8;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int r = 32 * s + 8 * g + (lane >> 2 & 3), cc = 2 * t + (lane >> 1 & 1);
-        const x8 k = join8<T>(read_transposed(lds + kK + slot<CH>(r, cc) + (lane & 1) * 8), read_transposed(lds + kK + slot<CH>(r + 4, cc) + (lane & 1) * 8));
-        S[t] = mfma16(k, part[s][0], S[t]);
-        if (kHalf) {
-          low = mfma16(k, part[s][1], low);
-        } else {
-          S[t] = mfma16(k, part[s][1], S[t]);
-          S[t] = mfma16(k, part[s][2], S[t]);
+        const char* const from = here + kV + 32 * s * 128 + low8;
+        const int cc = 2 * w4 + (lane >> 1 & 1);
+        const x8 v = join8<T>(read_transposed(from + slot<8>(r, cc)), read_transposed(from + slot<8>(r + 4, cc)));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float x = (float)v[i] * weight[s][i];
+          asm("" : "+v"(x));   // the rounded product: rounded to 16 bits from the exact one in one place and from this in another, a
+                               // part and what is left of it would not belong together
+          part[s][0][i] = (T)x;
+          x -= (float)part[s][0][i];
+          if (kHalf) x *= 4096.0f;
+          part[s][1][i] = (T)x;
+          if (!kHalf) part[s][2][i] = (T)(x - (float)part[s][1][i]);
         }
       }
-      if (kHalf) S[t] += low * (1.0f / 4096.0f);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[t][i] = fmaf(S[t][i], keep, S[t][i] * keep_rest);
+        f32x4 low = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const char* const from = here + kK + 32 * s * CH * 16 + low8;
+          const int cc = 2 * t + (lane >> 1 & 1);
+          const x8 k = join8<T>(read_transposed(from + slot<CH>(r, cc)), read_transposed(from + slot<CH>(r + 4, cc)));
+          S[t] = mfma16(k, part[s][0], S[t]);
+          if (kHalf) {
+            low = mfma16(k, part[s][1], low);
+          } else {
+            S[t] = mfma16(k, part[s][1], S[t]);
+            S[t] = mfma16(k, part[s][2], S[t]);
+          }
+        }
+        if (kHalf) S[t] += low * (1.0f / 4096.0f);
+      }
+      if (c + 1 < chunks) leave_copy(~c & 1);
+      __syncthreads();
     }
 #pragma unroll
-    for (int rb = 0; rb < 4; ++rb) {
-      x4 y;
+    for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = (T)out[rb][i];
-      const int r = 16 * rb + l16;
-      if (r < left && dv0 + 4 * g < p.value_dim) *(x4*)(at_out<T>(p.out, b, t0 + r, h) + dv0 + 4 * g) = y;
+      for (int i = 0; i < 4; ++i) {
+        const int dk = 16 * t + 4 * g + i;
+        if (dv < p.value_dim && dk < p.key_dim) p.state_out[state0 + (int64_t)dk * p.value_dim] = S[t][i];
+      }
+  } else {
+    // ---- out: rows 16 w4 .. + 15 of the chunk, lane has row 16 w4 + l16
+    if (chunks) {
+      store(lds);
+      fetch(1);
     }
+    __syncthreads();
+    float decay[4][4];                              // of A's tiles: keys 16 cb + 4 g + i
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int apart = 16 * (w4 - cb) + l16 - 4 * g - i;
+        decay[cb][i] = apart < 0 ? 0.0f : p.scale * (float)power[max(apart, 0)];
+      }
+    const float after = p.scale * (float)power[16 * w4 + l16 + 1];
+    const int vrow = 4 * g + (lane >> 2 & 3), low8 = (lane & 1) * 8;
+    for (int c = 0; c < chunks; ++c) {
+      const char* const here = lds + (c & 1) * kSlot;
+      const char* const copy = lds + kS + (c & 1) * kCopy;
+      if (c + 1 < chunks) {
+        store(lds + (~c & 1) * kSlot);
+        fetch(c + 2);
+      }
+      x8 q[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) q[s] = *(const x8*)(here + 16 * w4 * CH * 16 + slot<CH>(l16, 4 * s + g));
+      f32x4 o[4];
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        o[d] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) o[d] = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], o[d]);
+        o[d] *= kHalf ? ldexpf(after, exponents[c & 1][d]) : after;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {                 // 32 keys
+        if (2 * j > w4) break;
+        x8 a = {};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int cb = 2 * j + e;
+          if (cb > w4) break;
+          f32x4 t = {0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(here + kK + 16 * cb * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a[4 * e + i] = (T)(t[i] * decay[cb][i]);
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const char* const from = here + kV + 32 * j * 128 + low8;
+          const int cc = 2 * d + (lane >> 1 & 1);
+          o[d] = mfma16(join8<T>(read_transposed(from + slot<8>(vrow, cc)), read_transposed(from + 16 * 128 + slot<8>(vrow, cc))), a, o[d]);
+        }
+      }
+      const int64_t t = (int64_t)c * kChunk + 16 * w4 + l16;
+      if (t < n) {
+        T* const to = at_out<T>(p.out, b, t, h) + 64 * block + 4 * g;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          x4 y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = (T)o[d][i];
+          if (64 * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = y;
+        }
+      }
+      __syncthreads();
+    }
+    if (in_v)
+      for (int64_t t = (int64_t)n + vr - 32; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + 64 * block + 8 * vch) = s16x8{};
   }
-  if (in_v)
-    for (int t = n + vr0; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + 64 * block + 8 * vch) = s16x8{};
-#pragma unroll
-  for (int t = 0; t < KT; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int dk = 16 * t + 4 * g + i;
-      if (in_state && dk < p.key_dim) p.state_out[state0 + (int64_t)dk * p.value_dim] = S[t][i];
-    }
 }
 
 hipError_t launch(const RetentionParams& p, hipStream_t stream) {
@@ -313,7 +337,7 @@ hipError_t launch(const RetentionParams& p, hipStream_t stream) {
                            : wide ? (const void*)k_retain_steps<bf16, 8> : (const void*)k_retain_steps<bf16, 4>;
   else kernel = half ? wide ? (const void*)k_retain_chunks<f16, 128> : (const void*)k_retain_chunks<f16, 64>
                      : wide ? (const void*)k_retain_chunks<bf16, 128> : (const void*)k_retain_chunks<bf16, 64>;
-  return launch_kernel(kernel, workgroups, 256, args, stream);
+  return launch_kernel(kernel, workgroups, steps ? 256 : 512, args, stream);
 }
 
 }  // namespace hs

@@ -32,11 +32,11 @@ __device__ __forceinline__ f32x4 mfma16(Vec<f16>::x8 a, Vec<f16>::x8 b, f32x4 c)
 __device__ __forceinline__ f32x4 mfma16(Vec<bf16>::x8 a, Vec<bf16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 // A tile of 16-bit values in LDS, CH 16-byte chunks per row (8 or 16): chunk c of a row lies at c ^ swizzle(row).  16 rows' same
-// chunk (an operand read along the rows) and 4 or 8 rows' neighbouring ones (a transposed read) then cover all
-// banks once.
+// chunk (an operand read along the rows), and two neighbouring chunks of rows 0 .. 3 and of 4 .. 7 or 8 .. 11
+// behind them (transposed reads), then cover all banks once.
 template <int CH>
 __device__ __forceinline__ int swizzle(int row) {
-  return CH == 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+  return (CH == 16 ? (row & 3) << 2 : (row >> 1 & 1) << 2) | ((row >> 2 ^ row >> 3) & 1) << 1 | (row >> 3 & 1);
 }
 template <int CH>   // byte offset of chunk c of a row
 __device__ __forceinline__ int slot(int row, int c) {
