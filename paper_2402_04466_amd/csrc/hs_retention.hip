@@ -1,6 +1,8 @@
 // hs_retention: linear attention with a decay for each head.
 #include "hs_track_device.h"
 
+#include <algorithm>
+
 namespace hs {
 
 // Recurrent form: S = decay * S + k v^T, out = scale * q S, token by token.  A workgroup holds key_dim x 64 values of
@@ -93,8 +95,11 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 // three bf16 or two fp16 parts (the second scaled by 2^12, out of fp16's subnormal numbers).
 constexpr int kChunk = 64;
 
-template <class T, int KP>
-__global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
+// Few sequences and heads: their chunks are cut into segments, a workgroup for each.  A first launch (kStates) finds what
+// every segment but the last adds to a state of zeros, a second one (k_retain_starts) puts together by the decays of whole
+// segments what each starts from, and the third goes on from there as above.
+template <class T, int KP, bool kStates>
+__global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int segments) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
   constexpr int CH = KP / 8, KT = KP / 16, KS = KP / 32;   // KT: 16-wide tiles of key dimensions, KS: steps of 32
@@ -107,8 +112,16 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
   __shared__ double power[kChunk + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w4 = wave & 3, l16 = lane & 15, g = lane >> 4;
   const int blocks = (p.value_dim + 63) / 64;
-  const int id = xcd_number(), block = id % blocks, bh = id / blocks, h = bh % p.q_heads, hk = h / p.group, b = bh / p.q_heads;
-  const int n = length_of(p.lengths, b, p.tokens), chunks = (int)(((int64_t)n + kChunk - 1) / kChunk);
+  int id = xcd_number();
+  const int block = id % blocks;
+  id /= blocks;
+  const int parts = kStates ? segments - 1 : segments, segment = id % parts, bh = id / parts;
+  const int h = bh % p.q_heads, hk = h / p.group, b = bh / p.q_heads;
+  const int n = length_of(p.lengths, b, p.tokens), all_chunks = (int)(((int64_t)n + kChunk - 1) / kChunk);
+  const int per_segment = (all_chunks + segments - 1) / segments;
+  const int first = min(segment * per_segment, all_chunks), chunks = min(per_segment, all_chunks - first);
+  const bool last = segment == (all_chunks ? (all_chunks - 1) / per_segment : 0);   // the one with the end
+  if (kStates ? !chunks || last : !chunks && !last) return;
 
   // staging: this thread's 16-byte piece of rows r0, r0 + RP, ... of Q and K, and of a row of V (8 pieces)
   const int r0 = threadIdx.x / CH, ch = threadIdx.x % CH, vr = threadIdx.x / 8, vch = threadIdx.x % 8;
@@ -118,13 +131,13 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
   const T* const vsrc = at<T>(p.v, b, 0, hk) + 64 * block + 8 * vch;
   s16x8 qreg[NL], kreg[NL], vreg;
   auto fetch = [&](int c) {
-    const int64_t t0 = (int64_t)c * kChunk;
+    const int64_t t0 = (int64_t)(first + c) * kChunk;
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
       const int64_t t = t0 + r0 + e * RP;
       qreg[e] = kreg[e] = s16x8{};
       if (t < n && in_k) {
-        qreg[e] = *(const s16x8*)(qsrc + t * p.q.token);
+        if (!kStates) qreg[e] = *(const s16x8*)(qsrc + t * p.q.token);
         kreg[e] = *(const s16x8*)(ksrc + t * p.k.token);
       }
     }
@@ -134,25 +147,27 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
   auto store = [&](char* to) {
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
-      *(s16x8*)(to + slot<CH>(r0 + e * RP, ch)) = qreg[e];
+      if (!kStates) *(s16x8*)(to + slot<CH>(r0 + e * RP, ch)) = qreg[e];
       *(s16x8*)(to + kK + slot<CH>(r0 + e * RP, ch)) = kreg[e];
     }
     *(s16x8*)(to + kV + slot<8>(vr, vch)) = vreg;
   };
   if (chunks) fetch(0);
-  if (threadIdx.x <= kChunk) power[threadIdx.x] = exp2(p.log2_decay[h] * threadIdx.x);
+  if (threadIdx.x >= 384 && threadIdx.x <= 384 + kChunk) power[threadIdx.x - 384] = exp2(p.log2_decay[h] * (threadIdx.x - 384));
 
   if (wave < 4) {
     // ---- the state: lane has dimension dv, key dimensions 16 t + 4 g + i
     const int dv = 64 * block + 16 * w4 + l16;
     const int64_t state0 = (int64_t)bh * p.key_dim * p.value_dim + dv;
+    const int64_t states = (int64_t)p.batch * p.q_heads * p.key_dim * p.value_dim;
+    const float* const from = kStates ? nullptr : segment ? p.parts + (segment - 1) * states : p.state_in;
     f32x4 S[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int dk = 16 * t + 4 * g + i;
-        S[t][i] = p.state_in && dv < p.value_dim && dk < p.key_dim ? p.state_in[state0 + (int64_t)dk * p.value_dim] : 0.0f;
+        S[t][i] = from && dv < p.value_dim && dk < p.key_dim ? from[state0 + (int64_t)dk * p.value_dim] : 0.0f;
       }
     if (chunks) {
       store(lds);
@@ -180,7 +195,7 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
         *(x4*)(lds + kS + to * kCopy + slot<CH>(16 * w4 + l16, 2 * t + (g >> 1)) + (g & 1) * 8) = w;
       }
     };
-    leave_copy(0);
+    if (!kStates) leave_copy(0);
     __syncthreads();
     float weight[2][8];                             // decays of v_j in S
 #pragma unroll
@@ -195,12 +210,12 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
         store(lds + (~c & 1) * kSlot);
         fetch(c + 2);
       }
-      const int left = n - c * kChunk;
+      const int64_t left = n - (int64_t)(first + c) * kChunk;
       if (left < kChunk) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[max(left - 1 - (32 * s + 8 * g + i), 0)];   // (later values are zeros)
+          for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[max((int)left - 1 - (32 * s + 8 * g + i), 0)];   // (later values are zeros)
         keep = (float)power[left];
         keep_rest = (float)(power[left] - (double)keep);
       }
@@ -243,15 +258,18 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
         }
         if (kHalf) S[t] += low * (1.0f / 4096.0f);
       }
-      if (c + 1 < chunks) leave_copy(~c & 1);
+      if (!kStates && c + 1 < chunks) leave_copy(~c & 1);
       __syncthreads();
     }
+    float* to = p.state_out + state0;
+    if (kStates) to = p.parts + segment * states + state0;
+    else if (!last) return;
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int dk = 16 * t + 4 * g + i;
-        if (dv < p.value_dim && dk < p.key_dim) p.state_out[state0 + (int64_t)dk * p.value_dim] = S[t][i];
+        if (dv < p.value_dim && dk < p.key_dim) to[(int64_t)dk * p.value_dim] = S[t][i];
       }
   } else {
     // ---- out: rows 16 w4 .. + 15 of the chunk, lane has row 16 w4 + l16
@@ -276,6 +294,10 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
       if (c + 1 < chunks) {
         store(lds + (~c & 1) * kSlot);
         fetch(c + 2);
+      }
+      if (kStates) {
+        __syncthreads();
+        continue;
       }
       x8 q[KS];
 #pragma unroll
@@ -309,7 +331,7 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
           o[d] = mfma16(join8<T>(read_transposed(from + slot<8>(vrow, cc)), read_transposed(from + 16 * 128 + slot<8>(vrow, cc))), a, o[d]);
         }
       }
-      const int64_t t = (int64_t)c * kChunk + 16 * w4 + l16;
+      const int64_t t = (int64_t)(first + c) * kChunk + 16 * w4 + l16;
       if (t < n) {
         T* const to = at_out<T>(p.out, b, t, h) + 64 * block + 4 * g;
 #pragma unroll
@@ -322,22 +344,80 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p) {
       }
       __syncthreads();
     }
-    if (in_v)
+    if (last && in_v)
       for (int64_t t = (int64_t)n + vr - 32; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + 64 * block + 8 * vch) = s16x8{};
   }
 }
 
+// parts[s], s < segments - 1: what segment s adds, replaced by the state behind it.  Four values per thread.
+__global__ __launch_bounds__(256) void k_retain_starts(RetentionParams p, int segments) {
+  const int64_t size = (int64_t)p.key_dim * p.value_dim, states = (int64_t)p.batch * p.q_heads * size;
+  const int64_t at_value = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (at_value >= states) return;
+  const int64_t bh = at_value / size, b = bh / p.q_heads;
+  const int n = length_of(p.lengths, b, p.tokens), chunks = (int)(((int64_t)n + kChunk - 1) / kChunk), per_segment = (chunks + segments - 1) / segments;
+  const int used = per_segment ? (chunks - 1) / per_segment : 0;   // segments before the sequence's last one
+  const double far = exp2(p.log2_decay[bh % p.q_heads] * ((double)per_segment * kChunk));
+  const float keep = (float)far, keep_rest = (float)(far - (double)keep);
+  f32x4 S = {0, 0, 0, 0};
+  if (p.state_in) S = *(const f32x4*)(p.state_in + at_value);
+  float* part = p.parts + at_value;
+#pragma unroll 4
+  for (int s = 0; s < used; ++s, part += states) {
+    const f32x4 add = *(const f32x4*)part;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) S[i] = fmaf(S[i], keep, fmaf(S[i], keep_rest, add[i]));
+    *(f32x4*)part = S;
+  }
+}
+
+namespace {
+struct RetentionPlan {
+  bool steps;
+  int segments;
+  int64_t workgroups;            // of one segment
+};
+RetentionPlan plan_of(const RetentionParams& p) {
+  RetentionPlan plan;
+  plan.workgroups = (int64_t)p.batch * p.q_heads * ((p.value_dim + 63) / 64);
+  plan.steps = p.tokens <= 8;
+  plan.segments = 1;
+  if (!plan.steps) {
+    const int64_t chunks = ((int64_t)p.tokens + kChunk - 1) / kChunk;
+    if (chunks >= 16) plan.segments = (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(plan.workgroups, 1), chunks / 3, 32}));
+  }
+  return plan;
+}
+
+template <class T>
+const void* chunks_kernel(bool wide, bool states) {
+  return wide ? states ? (const void*)k_retain_chunks<T, 128, true> : (const void*)k_retain_chunks<T, 128, false>
+              : states ? (const void*)k_retain_chunks<T, 64, true> : (const void*)k_retain_chunks<T, 64, false>;
+}
+}  // namespace
+
+size_t retention_workspace(const RetentionParams& p) {
+  const RetentionPlan plan = plan_of(p);
+  return (size_t)(plan.segments - 1) * p.batch * p.q_heads * p.key_dim * p.value_dim * sizeof(float);
+}
+
 hipError_t launch(const RetentionParams& p, hipStream_t stream) {
   RetentionParams params = p;
-  void* args[] = {&params};
-  const int64_t workgroups = (int64_t)p.batch * p.q_heads * ((p.value_dim + 63) / 64);
-  const bool wide = p.key_dim > 64, half = p.dtype == HS_F16, steps = p.tokens <= 8;
-  const void* kernel;
-  if (steps) kernel = half ? wide ? (const void*)k_retain_steps<f16, 8> : (const void*)k_retain_steps<f16, 4>
-                           : wide ? (const void*)k_retain_steps<bf16, 8> : (const void*)k_retain_steps<bf16, 4>;
-  else kernel = half ? wide ? (const void*)k_retain_chunks<f16, 128> : (const void*)k_retain_chunks<f16, 64>
-                     : wide ? (const void*)k_retain_chunks<bf16, 128> : (const void*)k_retain_chunks<bf16, 64>;
-  return launch_kernel(kernel, workgroups, steps ? 256 : 512, args, stream);
+  RetentionPlan plan = plan_of(p);
+  const bool wide = p.key_dim > 64, half = p.dtype == HS_F16;
+  void* args[] = {&params, &plan.segments};
+  if (plan.steps) {
+    const void* const kernel = half ? wide ? (const void*)k_retain_steps<f16, 8> : (const void*)k_retain_steps<f16, 4>
+                                    : wide ? (const void*)k_retain_steps<bf16, 8> : (const void*)k_retain_steps<bf16, 4>;
+    return launch_kernel(kernel, plan.workgroups, 256, args, stream);
+  }
+  if (plan.segments > 1) {
+    const hipError_t e = launch_kernel(half ? chunks_kernel<f16>(wide, true) : chunks_kernel<bf16>(wide, true), plan.workgroups * (plan.segments - 1), 512, args, stream);
+    if (e != hipSuccess) return e;
+    const hipError_t joined = launch_kernel((const void*)k_retain_starts, ((int64_t)p.batch * p.q_heads * p.key_dim * p.value_dim / 4 + 255) / 256, 256, args, stream);
+    if (joined != hipSuccess) return joined;
+  }
+  return launch_kernel(half ? chunks_kernel<f16>(wide, false) : chunks_kernel<bf16>(wide, false), plan.workgroups * plan.segments, 512, args, stream);
 }
 
 }  // namespace hs

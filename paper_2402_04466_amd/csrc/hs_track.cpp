@@ -197,6 +197,7 @@ RetentionParams params_of(const hs_retention_desc* d) {
   p.q_heads = d->q_heads; p.group = d->q_heads / d->kv_heads;
   p.key_dim = d->key_dim; p.value_dim = d->value_dim;
   p.scale = d->scale;
+  p.parts = (float*)d->d_workspace;
   for (int h = 0; h < d->q_heads; ++h) {
     p.decay[h] = (float)d->decay[h];
     p.decay_rest[h] = (float)(d->decay[h] - (double)p.decay[h]);
@@ -263,7 +264,7 @@ hs_status hs_query_retention_workspace(const hs_retention_desc* desc, size_t* by
   return guarded(fn, [&]() -> hs_status {
   if (!bytes) { set_error("%s: NULL bytes", fn); return HS_E_INVAL; }
   HS_TRY(check(fn, desc));
-  *bytes = 0;
+  *bytes = retention_workspace(params_of(desc));
   return HS_OK;
   });
 }
@@ -284,7 +285,7 @@ hs_status hs_retention(hs_ctx* ctx, const hs_retention_desc* desc, void* hip_str
     HS_TRY(check_pointer(fn, "d_state_out", desc->d_state_out, 16));
     HS_TRY(check_pointer(fn, "d_lengths", desc->d_lengths, 4));
   }
-  HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, 0));
+  HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, retention_workspace(params_of(desc))));
   HS_TRY(check_context(fn, ctx));
   if (desc->batch == 0) return HS_OK;
   return run(fn, ctx, params_of(desc), hip_stream);

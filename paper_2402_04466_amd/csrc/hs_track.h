@@ -38,7 +38,9 @@ struct RetentionParams {
   float scale;
   float decay[HS_MAX_HEADS], decay_rest[HS_MAX_HEADS];   // the decay in two parts, 48 bits of it together
   double log2_decay[HS_MAX_HEADS];
+  float* parts;                  // workspace: retention_workspace() bytes
 };
+size_t retention_workspace(const RetentionParams& p);
 hipError_t launch(const RetentionParams& p, hipStream_t stream);
 
 struct CrossParams {

@@ -244,6 +244,24 @@ def test_retention_matches_the_recurrence(hs, ctx, gen, dtype, b, n, hq, hk, dk,
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("b, n, hq, hk, dk, dv", [(7, 1000, 2, 1, 64, 48), (4, 1345, 2, 2, 104, 72), (1, 4100, 1, 1, 64, 64)])
+def test_few_long_sequences_of_every_length(hs, ctx, gen, dtype, b, n, hq, hk, dk, dv):
+    """Cut over the device: sequences that end in the first, a middle or the last part, or never begin."""
+    t = TYPES[dtype]
+    q, k, v, state, decay = retention_inputs(gen, b, n, hq, hk, dk, dv, t)
+    lengths = torch.tensor([n, 0, 1, 64, 65, 3 * n // 4, n - 1][:b], dtype=torch.int32, device=DEV)
+    ref = retention_reference(q, k, v, state, decay, dk ** -0.5, lengths)
+    out, end = torch.full((b, n, hq, dv), 7.0, dtype=t, device=DEV), torch.full_like(state, 7.0)
+    keep = retention_call(hs, ctx, q, k, v, out, state, end, decay, dk ** -0.5, lengths)
+    retention_check(out, end, ref, t, n, "long")
+    if n > 4000:
+        assert keep.numel() > 0, "meant to be cut"
+    again = torch.empty_like(out)
+    retention_call(hs, ctx, q, k, v, again, state, state, decay, dk ** -0.5, lengths)
+    assert torch.equal(again, out) and torch.equal(state, end)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
 def test_a_clip_cut_into_calls_is_the_clip(hs, ctx, gen, dtype):
     """A recording in one call, in pieces, and frame by frame: each against the recurrence."""
     t = TYPES[dtype]
