@@ -35,7 +35,7 @@ struct CrossGrid {
 };
 
 template <class T, int DP, int QW, int KW, int BN>
-__global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid grid) {
+__global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossGrid grid) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
   constexpr int CH = DP / 8, KS = DP / 16, DT = DP / 32, NB = BN / 32;
@@ -84,35 +84,59 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
   f32x16 o[DT] = {};
   float m = -INFINITY, l = 0.0f;
 
-  // staging: this thread's chunk of rows r0, r0 + NT / CH, ...
+  // staging: this thread's chunk of rows r0, r0 + NT / CH, ...  Rows behind the last key are read as that one, so that every
+  // tile's loads are the same instructions: loads of two branches would be waited for where the branches meet.
   const int tg = threadIdx.x % NT, r0 = tg / CH, ch = tg % CH;
   const bool in_dim = 8 * ch < p.dim;
   const T* const ksrc = at<T>(p.k, b, 0, hk) + 8 * ch;
   const T* const vsrc = at<T>(p.v, b, 0, hk) + 8 * ch;
+  const T* const klane = ksrc + r0 * p.k.token;
+  const T* const vlane = vsrc + r0 * p.v.token;
   const uint8_t* const mask = p.mask ? p.mask + b * p.mask_batch : nullptr;
-  s16x8 kreg[NL], vreg[NL];
-  bool seen = false;
+  s16x8 kreg[NL] = {}, vreg[NL] = {};
+  uint8_t seen = 0;
   auto fetch = [&](int tile) {
+    const int64_t j0 = (int64_t)tile * BN;
+    const T *ka[NL], *va[NL];
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
-      const int j = tile * BN + r0 + e * (NT / CH);
-      kreg[e] = vreg[e] = s16x8{};
-      if (j < n && in_dim) {
-        kreg[e] = *(const s16x8*)(ksrc + j * p.k.token);
-        vreg[e] = *(const s16x8*)(vsrc + j * p.v.token);
+      ka[e] = klane + (j0 + e * (NT / CH)) * p.k.token;
+      va[e] = vlane + (j0 + e * (NT / CH)) * p.v.token;
+    }
+    if (j0 + BN > n) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        const int64_t j = j0 + r0 + e * (NT / CH) < n ? j0 + r0 + e * (NT / CH) : (int64_t)n - 1;
+        ka[e] = ksrc + j * p.k.token;
+        va[e] = vsrc + j * p.v.token;
       }
     }
-    const int j = tile * BN + lane;
-    seen = lane < BN && j < n && (!mask || mask[j]);
+    if (in_dim) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        kreg[e] = *(const s16x8*)ka[e];
+        vreg[e] = *(const s16x8*)va[e];
+      }
+    }
+    if (mask) seen = mask[j0 + (lane & (BN - 1)) < n ? j0 + (lane & (BN - 1)) : (int64_t)n - 1];
   };
   // the tile's keys as a bit set, and its values in LDS: hidden values as zeros, whatever they hold
-  auto store = [&](char* at_tile) -> uint64_t {
-    const uint64_t visible = __ballot(seen);
+  constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
+  auto store = [&](int tile, char* at_tile) -> uint64_t {
+    uint64_t visible = kAll;
+    const int64_t left = n - (int64_t)tile * BN;
+    if (left < BN) visible = (1ull << left) - 1;
+    if (mask) visible &= __ballot(seen != 0);
+    if (visible != kAll) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e)
+        if (!(visible >> (r0 + e * (NT / CH)) & 1)) vreg[e] = s16x8{};
+    }
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
-      const int r = r0 + e * (NT / CH), to = slot<CH>(r, ch);
+      const int to = slot<CH>(r0 + e * (NT / CH), ch);
       *(s16x8*)(at_tile + to) = kreg[e];
-      *(s16x8*)(at_tile + kTile + to) = visible >> r & 1 ? vreg[e] : s16x8{};
+      *(s16x8*)(at_tile + kTile + to) = vreg[e];
     }
     return visible;
   };
@@ -127,16 +151,16 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
       voff[d][s] = kTile + slot<CH>(r, cc) + (lane & 1) * 8;
     }
 
-  constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
   const int rounds = (last - first + KW - 1) / KW;
-  if (rounds > 0) fetch(first + kw);
+  if (first + kw < last) fetch(first + kw);
   for (int i = 0; i < rounds; ++i) {
     const int tile = first + kw + i * KW;
     char* const here = tiles + (kBuffers == 2 ? (i & 1) * 2 * kTile : 0);
-    const uint64_t visible = store(here);
+    uint64_t visible = 0;
+    if (tile < last) visible = store(tile, here);
     if (QW > 1) __syncthreads();
-    if (i + 1 < rounds) fetch(tile + KW < last ? tile + KW : INT32_MAX / BN);   // (a tile behind the last key holds nothing)
-    if (tile >= last || !visible) continue;
+    if (tile + KW < last) fetch(tile + KW);
+    if (!visible) continue;
 
     f32x16 s[NB];
 #pragma unroll
@@ -183,9 +207,10 @@ __global__ __launch_bounds__(64 * QW * KW) void k_cross(CrossParams p, CrossGrid
     for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        x8 w;
+        float w8[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = (T)s[kb][8 * j + e];
+        for (int e = 0; e < 8; ++e) w8[e] = s[kb][8 * j + e];
+        const x8 w = round8<T>(w8);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const char* const at_v = here + (32 * kb + 16 * j) * CH * 16;
@@ -303,15 +328,18 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
 
 namespace {
 struct CrossPlan {
-  bool wide;                    // four waves with 32 rows each, else one set of 32 rows with the keys dealt to four waves
+  int wide;                     // so many waves with 32 rows each; 0: one set of 32 rows, the keys dealt to four waves
   CrossGrid grid;
   int64_t workgroups;
 };
 CrossPlan plan_of(const CrossParams& p) {
   const int64_t bh = (int64_t)p.batch * (p.q_heads / p.group), rows = (int64_t)p.q_tokens * p.group;
   CrossPlan plan;
-  plan.wide = bh * ((rows + 127) / 128) >= 256;
-  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? (rows + 127) / 128 : (rows + 31) / 32, INT32_MAX);
+  // Eight waves share a tile of wide heads, four one of narrow ones: 2040 tokens of 16 heads on 8160 keys, 8 times, take
+  // 1095 and 1180 us of 128 dimensions, 757 and 721 of 64.
+  const int waves = p.dim > 64 ? 8 : 4, tile = 32 * waves;
+  plan.wide = bh * ((rows + tile - 1) / tile) >= 256 ? waves : 0;
+  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? (rows + tile - 1) / tile : (rows + 31) / 32, INT32_MAX);
   plan.grid.splits = 1;
   if (!plan.wide) {
     // two rounds of workgroups where the keys are enough for two tiles per wave
@@ -334,11 +362,11 @@ hipError_t launch(const CrossParams& p, hipStream_t stream) {
   void* args[] = {&params, &plan.grid};
   const bool narrow = p.dim <= 64, half = p.dtype == HS_F16;
   const void* kernel;
-  if (plan.wide) kernel = half ? narrow ? (const void*)k_cross<f16, 64, 4, 1, 64> : (const void*)k_cross<f16, 128, 4, 1, 64>
-                               : narrow ? (const void*)k_cross<bf16, 64, 4, 1, 64> : (const void*)k_cross<bf16, 128, 4, 1, 64>;
+  if (plan.wide) kernel = half ? narrow ? (const void*)k_cross<f16, 64, 4, 1, 64> : (const void*)k_cross<f16, 128, 8, 1, 64>
+                               : narrow ? (const void*)k_cross<bf16, 64, 4, 1, 64> : (const void*)k_cross<bf16, 128, 8, 1, 64>;
   else kernel = half ? narrow ? (const void*)k_cross<f16, 64, 1, 4, 32> : (const void*)k_cross<f16, 128, 1, 4, 32>
                      : narrow ? (const void*)k_cross<bf16, 64, 1, 4, 32> : (const void*)k_cross<bf16, 128, 1, 4, 32>;
-  hipError_t e = launch_kernel(kernel, plan.workgroups, 256, args, stream);
+  hipError_t e = launch_kernel(kernel, plan.workgroups, plan.wide ? 64 * plan.wide : 256, args, stream);
   if (e != hipSuccess || plan.grid.splits == 1) return e;
   void* join_args[] = {&params, &plan.grid.splits};
   return launch_kernel(half ? (const void*)k_cross_join<f16> : (const void*)k_cross_join<bf16>,

@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256) void k_retain_starts(RetentionParams p, int se
   const int64_t at_value = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
   if (at_value >= states) return;
   const int64_t bh = at_value / size, b = bh / p.q_heads;
-  const int n = length_of(p.lengths, b, p.tokens), chunks = (int)(((int64_t)n + kChunk - 1) / kChunk), per_segment = (chunks + segments - 1) / segments;
+  const int n = p.lengths ? min(max(p.lengths[b], 0), p.tokens) : p.tokens, chunks = (int)(((int64_t)n + kChunk - 1) / kChunk), per_segment = (chunks + segments - 1) / segments;
   const int used = per_segment ? (chunks - 1) / per_segment : 0;   // segments before the sequence's last one
   const double far = exp2(p.log2_decay[bh % p.q_heads] * ((double)per_segment * kChunk));
   const float keep = (float)far, keep_rest = (float)(far - (double)keep);

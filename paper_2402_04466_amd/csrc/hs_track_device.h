@@ -59,6 +59,16 @@ __device__ __forceinline__ typename Vec<T>::x8 join8(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(typename Vec<T>::x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Eight sums, each rounded once.  (The conversion of a whole vector, not of its elements: that takes pairs.)
+template <class T>
+__device__ __forceinline__ typename Vec<T>::x8 round8(const float* x) {
+  typedef float f32x8 __attribute__((ext_vector_type(8)));
+  const f32x8 v = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+  return __builtin_convertvector(v, typename Vec<T>::x8);
+}
+template <class T>
+__device__ __forceinline__ typename Vec<T>::x4 round4(f32x4 v) { return __builtin_convertvector(v, typename Vec<T>::x4); }
+
 // The value of lane l ^ 32 is among the two; both halves get both.
 __device__ __forceinline__ void both_halves(float x, float& lower, float& upper) {
   const unsigned bits = __builtin_bit_cast(unsigned, x);
@@ -77,9 +87,10 @@ __device__ __forceinline__ T* at_out(const Heads& h, int64_t batch, int64_t toke
   return (T*)h.p + batch * h.batch + token * h.token + head * h.head;
 }
 
-// A sequence's length as the caller gives it, taken into its range.
+// A sequence's length as the caller gives it, taken into its range.  `batch` is the same for the whole wave, and so, said
+// aloud, is the length: loops over it are the scalar unit's then.
 __device__ __forceinline__ int length_of(const int32_t* lengths, int batch, int longest) {
-  return lengths ? min(max(lengths[batch], 0), longest) : longest;
+  return __builtin_amdgcn_readfirstlane(lengths ? min(max(lengths[batch], 0), longest) : longest);
 }
 
 inline hipError_t launch_kernel(const void* func, int64_t workgroups, unsigned threads, void** args, hipStream_t stream) {
