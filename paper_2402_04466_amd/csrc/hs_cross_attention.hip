@@ -3,6 +3,7 @@
 
 #include <math.h>
 
+
 #include <algorithm>
 
 namespace hs {
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
   constexpr int kTiles = KW * kBuffers * 2 * kTile, kParts = KW > 1 ? KW * QW * 32 * (PT + 2) * 4 : 0;
   constexpr int kLds = kTiles > kParts ? kTiles : kParts;
   __shared__ __align__(16) char lds[kLds];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, qw = wave % QW, kw = wave / QW;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qw = wave % QW, kw = wave / QW;
   const int row_in_wave = lane & 31, half = lane >> 5;
   char* const tiles = lds + kw * kBuffers * 2 * kTile;
 
@@ -57,11 +58,11 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
   id /= grid.row_tiles;
   const int split = id % grid.splits;
   const int bh = id / grid.splits, kv_heads = p.q_heads / p.group, hk = bh % kv_heads, b = bh / kv_heads;
-  const int64_t rows = (int64_t)p.q_tokens * p.group;
-  const int64_t row = ((int64_t)row_tile * QW + qw) * 32 + row_in_wave;
+  const uint32_t rows = (uint32_t)p.q_tokens * p.group, group = p.group;   // below 2^31
+  const uint32_t row = (row_tile * QW + qw) * 32 + row_in_wave;
   const bool live = row < rows;
-  const int64_t token = live ? row / p.group : 0;
-  const int head = hk * p.group + (live ? (int)(row % p.group) : 0);
+  const uint32_t token = live ? row / group : 0;
+  const int head = hk * p.group + (live ? (int)(row - token * group) : 0);
 
   // the keys of this workgroup: tiles first .. last - 1, of which group kw takes every KW-th
   const int n = length_of(p.lengths, b, p.k_tokens);
@@ -226,10 +227,11 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
     float* const part_o = (float*)lds;
     float* const part_ml = part_o + KW * QW * 32 * PT;
     __syncthreads();
-    if (half == 0) {
+    if (half == 0 && live) {
       part_ml[2 * (wave * 32 + row_in_wave)] = m;
       part_ml[2 * (wave * 32 + row_in_wave) + 1] = l;
     }
+    if (live)
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -238,7 +240,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
     __syncthreads();
     // thread t: row t / 8 (of QW * 32), values 4 * (t % 8 + 8 * i)
     for (int r = threadIdx.x / 8; r < QW * 32; r += 8 * QW * KW) {
-      const int64_t at_row = (int64_t)row_tile * QW * 32 + r;
+      const uint32_t at_row = row_tile * QW * 32 + r;
       if (at_row >= rows) break;
       float mm = -INFINITY, ll = 0.0f, f[KW];
 #pragma unroll
@@ -251,8 +253,8 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
       }
       const bool whole = grid.splits == 1;
       const float inv = whole ? ll > 0.0f ? 1.0f / ll : ll == 0.0f ? 0.0f : ll : 1.0f;
-      const int64_t tok = at_row / p.group;
-      const int hh = hk * p.group + (int)(at_row % p.group);
+      const uint32_t tok = at_row / group;
+      const int hh = hk * p.group + (int)(at_row - tok * group);
       const int64_t part_row = (int64_t)(split * (int64_t)(p.batch * kv_heads) + bh) * rows + at_row;
       for (int d0 = 4 * (threadIdx.x % 8); d0 < p.dim; d0 += 32) {
         f32x4 sum = {0, 0, 0, 0};
@@ -294,41 +296,50 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
   if (p.lse && half == 0) p.lse[((int64_t)b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l) - kRaise<T> * kLn2);
 }
 
-// The splits' parts of a row, each a maximum, a sum and a weighted sum of values: 32 lanes per row.
+// The splits' parts of a row, each a maximum, a sum and a weighted sum of values: a wave per row.  Lane s has what weighs
+// part s; then the wave's halves take even and odd parts, four values per lane.
+constexpr int kMostSplits = 64;
 template <class T>
 __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
   typedef typename Vec<T>::x4 x4;
-  const int kv_heads = p.q_heads / p.group;
+  const int kv_heads = p.q_heads / p.group, lane = threadIdx.x & 63, half = lane >> 5;
   const int64_t rows = (int64_t)p.q_tokens * p.group, all = (int64_t)p.batch * kv_heads * rows;
-  const int64_t id = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
   if (id >= all) return;
   const float scale = p.scale == 0.0f ? 1e-30f : fabsf(p.scale), c = scale * kLog2e;
   const int64_t row = id % rows, bh = id / rows, b = bh / kv_heads, token = row / p.group;
   const int head = (int)(bh % kv_heads) * p.group + (int)(row % p.group);
-  const int d0 = 4 * (threadIdx.x % 32), pitch = p.dim + 4;
+  const int d0 = 4 * (lane & 31), pitch = p.dim + 4;
+  const float* const parts = p.parts + id * pitch;
   float m = -INFINITY, l = 0.0f;
-  f32x4 sum = {0, 0, 0, 0};
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, p.parts[(s * all + id) * pitch]);
-  for (int s = 0; s < splits; ++s) {
-    const float* const part = p.parts + (s * all + id) * pitch;
-    if (part[0] == -INFINITY) continue;
-    const float f = __builtin_amdgcn_exp2f((part[0] - m) * c);
-    l = fmaf(part[1], f, l);
-    if (d0 < p.dim) sum += f * *(const f32x4*)(part + 4 + d0);
+  if (lane < splits) {
+    m = parts[lane * all * pitch];
+    l = parts[lane * all * pitch + 1];
   }
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-  if (d0 < p.dim) {
-    x4 y;
+  float top = m;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
-    *(x4*)(at_out<T>(p.out, b, token, head) + d0) = y;
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c);
+  l = m == -INFINITY ? 0.0f : l * f;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+  f32x4 sum = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int s = 0; s < splits; s += 2) {
+    const float w = __shfl(f, s + half);            // (of a part that is not there, or saw no key: 0)
+    if (d0 < p.dim && w != 0.0f) sum += w * *(const f32x4*)(parts + (s + half) * all * pitch + 4 + d0);
   }
-  if (p.lse && threadIdx.x % 32 == 0) p.lse[(b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l) - kRaise<T> * kLn2);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], 32);
+  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  if (half == 0 && d0 < p.dim) *(x4*)(at_out<T>(p.out, b, token, head) + d0) = round4<T>(sum * inv);
+  if (p.lse && lane == 0) p.lse[(b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(top, scale, logf(l) - kRaise<T> * kLn2);
 }
 
 namespace {
 struct CrossPlan {
-  int wide;                     // so many waves with 32 rows each; 0: one set of 32 rows, the keys dealt to four waves
+  int wide;                     // so many waves with 32 rows each, or
+  int groups;                   // one set of 32 rows whose keys are dealt to so many waves
   CrossGrid grid;
   int64_t workgroups;
 };
@@ -338,13 +349,17 @@ CrossPlan plan_of(const CrossParams& p) {
   // Eight waves share a tile of wide heads, four one of narrow ones: 2040 tokens of 16 heads on 8160 keys, 8 times, take
   // 1095 and 1180 us of 128 dimensions, 757 and 721 of 64.
   const int waves = p.dim > 64 ? 8 : 4, tile = 32 * waves;
+  plan.groups = 0;
   plan.wide = bh * ((rows + tile - 1) / tile) >= 256 ? waves : 0;
   plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? (rows + tile - 1) / tile : (rows + 31) / 32, INT32_MAX);
   plan.grid.splits = 1;
   if (!plan.wide) {
-    // two rounds of workgroups where the keys are enough for two tiles per wave
-    const int64_t tiles = (p.k_tokens + 31) / 32, base = bh * plan.grid.row_tiles;
-    plan.grid.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(base, 1), tiles / 8));
+    // Keys over several workgroups where there are fewer than the device holds at once (two per CU of up to 64 dimensions,
+    // one of more) and at least four tiles per wave; a second launch then joins them.  One workgroup per row tile takes eight
+    // waves instead: 77 tokens on up to 1001 keys of 80 dimensions, 20 times (160 row tiles) 15.1 us, 17.6 in three parts.
+    const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, base = bh * plan.grid.row_tiles;
+    plan.grid.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(p.dim > 64 ? 256 : 512) / std::max<int64_t>(base, 1), tiles / 16, kMostSplits}));
+    plan.groups = plan.grid.splits == 1 ? 8 : 4;
   }
   plan.workgroups = bh * plan.grid.row_tiles * plan.grid.splits;
   return plan;
@@ -364,13 +379,15 @@ hipError_t launch(const CrossParams& p, hipStream_t stream) {
   const void* kernel;
   if (plan.wide) kernel = half ? narrow ? (const void*)k_cross<f16, 64, 4, 1, 64> : (const void*)k_cross<f16, 128, 8, 1, 64>
                                : narrow ? (const void*)k_cross<bf16, 64, 4, 1, 64> : (const void*)k_cross<bf16, 128, 8, 1, 64>;
+  else if (plan.groups == 8) kernel = half ? narrow ? (const void*)k_cross<f16, 64, 1, 8, 32> : (const void*)k_cross<f16, 128, 1, 8, 32>
+                                           : narrow ? (const void*)k_cross<bf16, 64, 1, 8, 32> : (const void*)k_cross<bf16, 128, 1, 8, 32>;
   else kernel = half ? narrow ? (const void*)k_cross<f16, 64, 1, 4, 32> : (const void*)k_cross<f16, 128, 1, 4, 32>
                      : narrow ? (const void*)k_cross<bf16, 64, 1, 4, 32> : (const void*)k_cross<bf16, 128, 1, 4, 32>;
-  hipError_t e = launch_kernel(kernel, plan.workgroups, plan.wide ? 64 * plan.wide : 256, args, stream);
+  hipError_t e = launch_kernel(kernel, plan.workgroups, 64 * (plan.wide + plan.groups), args, stream);
   if (e != hipSuccess || plan.grid.splits == 1) return e;
   void* join_args[] = {&params, &plan.grid.splits};
   return launch_kernel(half ? (const void*)k_cross_join<f16> : (const void*)k_cross_join<bf16>,
-                       ((int64_t)p.batch * p.q_heads * p.q_tokens + 7) / 8, 256, join_args, stream);
+                       ((int64_t)p.batch * p.q_heads * p.q_tokens + 3) / 4, 256, join_args, stream);
 }
 
 }  // namespace hs

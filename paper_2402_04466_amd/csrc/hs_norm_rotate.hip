@@ -2,90 +2,158 @@
 #include "hs_track_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace hs {
 
 // y = x * rsqrt(mean(x^2) + eps) * w; pairs (a, b) of the first `rotary` values turned by t = position * frequency.
 //
 // Bound by reading and writing every value once.  A head is held by LANES = 2, 4, 8 or 16 lanes with 8 values (16
-// bytes) each; a group of LANES lanes takes one token and up to HEADS of its heads one after the other, so that the
-// token's sines and cosines, folded into the weights (own value times A plus partner's times B), are formed once
-// and stay in registers.  The partner's values come from the lane that has them (half layout) or are the lane's
-// own (interleaved).
+// bytes) each; a group of LANES lanes takes one token and some of its heads, four at a time, so that the token's
+// sines and cosines, folded into the weights (own value times A plus partner's times B), are formed once and stay in
+// registers, behind the loads of the first four heads.  The partner's values come from the lane that has them (half layout)
+// or are the lane's own (interleaved).
+
+// Sum over the LANES lanes of a group, in each of them: neighbours, pairs, then mirrored halves, whose lanes agree by then.
+template <int LANES>
+__device__ __forceinline__ float group_sum(float x) {
+  auto moved = [](float v, auto control) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+  };
+  x += moved(x, std::integral_constant<int, 0xb1>{});                     // lane ^ 1
+  if (LANES > 2) x += moved(x, std::integral_constant<int, 0x4e>{});      // lane ^ 2
+  if (LANES > 4) x += moved(x, std::integral_constant<int, 0x141>{});     // 7 - lane
+  if (LANES > 8) x += moved(x, std::integral_constant<int, 0x140>{});     // 15 - lane
+  return x;
+}
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));     // as the caller's pointers are aligned
+typedef double f64x2_any __attribute__((ext_vector_type(2), aligned(8)));
+__device__ __forceinline__ void load8(const float* from, float* to) {
+  const f32x4_any a = *(const f32x4_any*)from, b = *(const f32x4_any*)(from + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    to[i] = a[i];
+    to[4 + i] = b[i];
+  }
+}
+// Eight pairs' frequencies, or the four of a lane that holds both values of its pairs.
+__device__ __forceinline__ void load_frequencies(const double* from, bool four, double* to) {
+  const f64x2_any a = *(const f64x2_any*)from, b = *(const f64x2_any*)(from + 2);
+  to[0] = a[0], to[1] = a[1], to[2] = b[0], to[3] = b[1];
+  if (four) return;
+  const f64x2_any c = *(const f64x2_any*)(from + 4), d = *(const f64x2_any*)(from + 6);
+  to[4] = c[0], to[5] = c[1], to[6] = d[0], to[7] = d[1];
+}
+
 template <class T, int LANES>
 __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateParams p, int heads_per_group, int q_blocks, int k_blocks) {
   typedef typename Vec<T>::x8 x8;
+  constexpr int kAhead = 4;
   const int lane = threadIdx.x % LANES, lane0 = (threadIdx.x & 63) - lane;
-  const int64_t group = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  const int blocks = q_blocks + k_blocks;
-  const int64_t row = group / blocks;
-  if (row >= (int64_t)p.batch * p.tokens) return;
-  const int block = (int)(group % blocks);
-  const int64_t b = row / p.tokens, t = row % p.tokens;
-  const bool is_q = block < q_blocks;
-  const Heads& in = is_q ? p.q : p.k;
-  const Heads& out = is_q ? p.q_out : p.k_out;
-  const float* const w = is_q ? p.wq : p.wk;
+  const uint32_t group = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, blocks = q_blocks + k_blocks;
+  const uint32_t row = group / blocks, block = group % blocks;
+  if (row >= (uint32_t)p.batch * (uint32_t)p.tokens) return;
+  const uint32_t b = row / (uint32_t)p.tokens, t = row % (uint32_t)p.tokens;
+  const bool is_q = block < (uint32_t)q_blocks;
   const int h0 = (is_q ? block : block - q_blocks) * heads_per_group;
   const int h1 = min(h0 + heads_per_group, is_q ? p.q_heads : p.k_heads);
   const int c0 = 8 * lane;                       // the lane's first value of the head
   const bool there = c0 < p.dim, turned = c0 < p.rotary;
+  const int64_t in_head = is_q ? p.q.head : p.k.head, out_head = is_q ? p.q_out.head : p.k_out.head;
+  const T* from = (is_q ? at<T>(p.q, b, t, h0) : at<T>(p.k, b, t, h0)) + c0;
+  T* to = (is_q ? at_out<T>(p.q_out, b, t, h0) : at_out<T>(p.k_out, b, t, h0)) + c0;
+  x8 x[kAhead];
+#pragma unroll
+  for (int e = 0; e < kAhead; ++e) {
+    x[e] = x8{};
+    if (there && h0 + e < h1) x[e] = *(const x8*)(from + e * in_head);
+  }
+
+  const float* const w = is_q ? p.wq : p.wk;
   const int half = p.rotary / 2;
   // the lane that holds the other values of this lane's pairs (half layout)
   const int partner = lane0 + (p.interleaved || !turned ? lane : c0 < half ? lane + half / 8 : lane - half / 8);
   const int p0 = 8 * (partner - lane0);
-
-  float A[8], B[8];
+  // weights and frequencies: whole vectors, behind one branch each
+  float weight[8], other[8], A[8], B[8];          // the lane's, and its pairs' other values'
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    A[i] = w && there ? w[c0 + i] : 1.0f;
-    B[i] = 0.0f;
+  for (int i = 0; i < 8; ++i) weight[i] = other[i] = 1.0f;
+  if (w && there) {
+    load8(w + c0, weight);
+    load8(w + p0, other);
   }
+  double freq[8] = {};
+  int64_t place = p.first + t;
   if (turned) {
-    const double pos = (double)(p.pos ? p.pos[b * p.pos_batch + t] : p.first + t);
+    load_frequencies(p.freq + (p.interleaved ? c0 / 2 : c0 < half ? c0 : c0 - half), p.interleaved, freq);
+    if (p.pos) place = p.pos[b * p.pos_batch + t];
+  }
+  const double pos = (double)place * 0.15915494309189533577;
+  // Whole turns are taken off in 64 bits, which leaves 2^-53 of the position's turns; the sine and cosine instructions take
+  // turns, and are within 1.25e-7 of the value over all of -1/2 .. 1/2.
+  auto angle = [&](double f, float& sine, float& cosine) {
+    const double turns = pos * f;
+    const float part = (float)(turns - rint(turns));
+    sine = __builtin_amdgcn_sinf(part);
+    cosine = __builtin_amdgcn_cosf(part);
+  };
+  if (p.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float sine, cosine;
+      angle(freq[i / 2], sine, cosine);
+      A[i] = cosine * weight[i];
+      A[i + 1] = cosine * weight[i + 1];
+      B[i] = -sine * weight[i + 1];
+      B[i + 1] = sine * weight[i];
+    }
+  } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      // whole turns are taken off in 64 bits: what is left is exact to 2^-53 of the position's turns
-      const int f = p.interleaved ? (c0 + i) / 2 : (c0 + i) % half;
-      const double turns = pos * p.freq[f] * 0.15915494309189533577;
       float sine, cosine;
-      sincospif(2.0f * (float)(turns - rint(turns)), &sine, &cosine);
-      const bool first = p.interleaved ? i % 2 == 0 : c0 < half;
-      const int other = p.interleaved ? c0 + (i ^ 1) : p0 + i;
-      B[i] = (first ? -sine : sine) * (w ? w[other] : 1.0f);
-      A[i] *= cosine;
+      angle(freq[i], sine, cosine);
+      A[i] = cosine * weight[i];
+      B[i] = (c0 < half ? -sine : sine) * other[i];
     }
   }
-  for (int h = h0; h < h1; ++h) {
-    x8 x = {};
-    if (there) x = *(const x8*)(at<T>(in, b, t, h) + c0);
-    float inv = 1.0f;
-    if (p.norm) {
-      float sum = 0.0f;
+  if (!turned) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf((float)x[i], (float)x[i], sum);
+    for (int i = 0; i < 8; ++i) A[i] = weight[i];
+  }
+  const float mean = 1.0f / (float)p.dim;
+  for (int h = h0; h < h1; h += kAhead) {
 #pragma unroll
-      for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
-      inv = 1.0f / sqrtf(sum / (float)p.dim + p.eps);
+    for (int e = 0; e < kAhead; ++e) {
+      if (h + e >= h1) break;
+      float inv = 1.0f;
+      if (p.norm) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fmaf((float)x[e][i], (float)x[e][i], sum);
+        inv = rsqrtf(fmaf(group_sum<LANES>(sum), mean, p.eps));
+      }
+      x8 o;
+      if (p.interleaved) {
+        o = __builtin_shufflevector(x[e], x[e], 1, 0, 3, 2, 5, 4, 7, 6);
+      } else {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        u32x4 words = __builtin_bit_cast(u32x4, x[e]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) words[i] = __shfl(words[i], partner);
+        o = __builtin_bit_cast(x8, words);
+      }
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float a = (float)x[e][i] * A[i];
+        y[i] = inv * (turned ? fmaf((float)o[i], B[i], a) : a);
+      }
+      if (there) *(x8*)(to + (h - h0 + e) * out_head) = round8<T>(y);
     }
-    x8 o = x;
-    if (p.interleaved) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = x[i ^ 1];
-    } else {
-      uint32_t words[4];
-      __builtin_memcpy(words, &x, 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) words[i] = __shfl(words[i], partner);
-      __builtin_memcpy(&o, words, 16);
-    }
-    x8 y;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float a = (float)x[i] * inv * A[i];
-      y[i] = (T)(turned ? fmaf((float)o[i] * inv, B[i], a) : a);
-    }
-    if (there) *(x8*)(at_out<T>(out, b, t, h) + c0) = y;
+    for (int e = 0; e < kAhead; ++e)
+      if (there && h + kAhead + e < h1) x[e] = *(const x8*)(from + (h - h0 + kAhead + e) * in_head);
   }
 }
 

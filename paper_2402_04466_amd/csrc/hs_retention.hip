@@ -7,52 +7,54 @@ namespace hs {
 
 // Recurrent form: S = decay * S + k v^T, out = scale * q S, token by token.  A workgroup holds key_dim x 64 values of
 // one sequence's and head's state in registers: 16 lanes side by side have 4 values of 16 bytes each, so a row of
-// the state is read in 256-byte pieces, and thread group g of 16 has the rows g, g + 16, ...
+// the state is read in 256-byte pieces, and thread group g of 16 has ROWS rows from ROWS * g on.  Bound by reading and
+// writing the state (5.2 TB/s at 128 tracks of 16 heads of 128 x 128); for few tracks by the chain of loads, so the first token's
+// are issued beside the state's and the length's, and each further token's beside the sums of the one before.
 template <class T, int ROWS>
 __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
   typedef typename Vec<T>::x4 x4;
+  typedef T xr __attribute__((ext_vector_type(ROWS)));
   __shared__ f32x4 partial[2][4][16];
   const int blocks = (p.value_dim + 63) / 64;
   const int block = blockIdx.x % blocks;
-  const int64_t bh = blockIdx.x / blocks;
-  const int h = (int)(bh % p.q_heads), hk = h / p.group;
-  const int64_t b = bh / p.q_heads;
+  const int bh = blockIdx.x / blocks, h = bh % p.q_heads, hk = h / p.group, b = bh / p.q_heads;
   const int c = threadIdx.x & 15, g = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-  const int dv0 = 64 * block + 4 * c;
-  const bool there = dv0 < p.value_dim;
-  const int64_t state0 = bh * p.key_dim * p.value_dim + dv0;
+  const int dv0 = 64 * block + 4 * c, dk0 = ROWS * g;
+  const bool in_v = dv0 < p.value_dim, in_k = dk0 < p.key_dim, there = in_v && in_k;
+  const int64_t state0 = ((int64_t)bh * p.key_dim + dk0) * p.value_dim + dv0;
+  const T* const q = at<T>(p.q, b, 0, h) + dk0;
+  const T* const k = at<T>(p.k, b, 0, hk) + dk0;
+  const T* const v = at<T>(p.v, b, 0, hk) + dv0;
 
   f32x4 S[ROWS];
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
-    const int dk = g + 16 * r;
     S[r] = f32x4{0, 0, 0, 0};
-    if (p.state_in && there && dk < p.key_dim) S[r] = *(const f32x4*)(p.state_in + state0 + (int64_t)dk * p.value_dim);
+    if (p.state_in && there) S[r] = *(const f32x4*)(p.state_in + state0 + (int64_t)r * p.value_dim);
   }
+  xr qq = {}, kk = {};
+  x4 vv = {};
+  auto fetch = [&](int64_t t) {                     // (also of a token behind the sequence's end: then not used)
+    if (in_k) {
+      qq = *(const xr*)(q + t * p.q.token);
+      kk = *(const xr*)(k + t * p.k.token);
+    }
+    if (in_v) vv = *(const x4*)(v + t * p.v.token);
+  };
+  if (p.tokens > 0) fetch(0);
   const int n = length_of(p.lengths, b, p.tokens);
   // (an fp32 decay near one is 2^-25 off, which 7200 steps raise to 2e-4 of the state)
   const float decay = p.decay[h], rest = p.decay_rest[h];
   for (int t = 0; t < n; ++t) {
-    const T* const q = at<T>(p.q, b, t, h);
-    const T* const k = at<T>(p.k, b, t, hk);
-    f32x4 v = {0, 0, 0, 0}, o = {0, 0, 0, 0};
-    if (there) {
-      const x4 raw = *(const x4*)(at<T>(p.v, b, t, hk) + dv0);
+    f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = (float)raw[i];
-    }
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const int dk = g + 16 * r;
-      if (dk < p.key_dim) {
-        const float kk = (float)k[dk], qq = (float)q[dk];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          S[r][i] = fmaf(decay, S[r][i], fmaf(rest, S[r][i], kk * v[i]));
-          o[i] = fmaf(qq, S[r][i], o[i]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        S[r][i] = fmaf(decay, S[r][i], fmaf(rest, S[r][i], (float)kk[r] * (float)vv[i]));
+        o[i] = fmaf((float)qq[r], S[r][i], o[i]);
       }
-    }
+    if (t + 1 < n) fetch(t + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       o[i] += __shfl_xor(o[i], 16);
@@ -60,21 +62,14 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
     }
     if ((threadIdx.x & 63) < 16) partial[t & 1][wave][c] = o;
     __syncthreads();   // the other half of `partial` is written before the next one
-    if (threadIdx.x < 16 && there) {
-      x4 y;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        y[i] = (T)(p.scale * ((partial[t & 1][0][c][i] + partial[t & 1][1][c][i]) + (partial[t & 1][2][c][i] + partial[t & 1][3][c][i])));
-      *(x4*)(at_out<T>(p.out, b, t, h) + dv0) = y;
-    }
+    if (threadIdx.x < 16 && in_v)
+      *(x4*)(at_out<T>(p.out, b, t, h) + dv0) = round4<T>(p.scale * ((partial[t & 1][0][c] + partial[t & 1][1][c]) + (partial[t & 1][2][c] + partial[t & 1][3][c])));
   }
-  if (there)
+  if (in_v)
     for (int t = n + g; t < p.tokens; t += 16) *(x4*)(at_out<T>(p.out, b, t, h) + dv0) = x4{};
+  if (there && !(n == 0 && p.state_out == p.state_in))
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    const int dk = g + 16 * r;
-    if (there && dk < p.key_dim) *(f32x4*)(p.state_out + state0 + (int64_t)dk * p.value_dim) = S[r];
-  }
+    for (int r = 0; r < ROWS; ++r) *(f32x4*)(p.state_out + state0 + (int64_t)r * p.value_dim) = S[r];
 }
 
 // Chunked form: 64 tokens at a time, products on the matrix pipe.  With c tokens in a chunk, S the state before it and

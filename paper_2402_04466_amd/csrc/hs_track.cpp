@@ -214,6 +214,10 @@ hs_status check(const char* fn, const hs_cross_attention_desc* d) {   // all but
   HS_TRY(check_groups(fn, d->q_heads, d->kv_heads));
   HS_TRY(check_dim(fn, "head_dim", d->head_dim));
   if (!std::isfinite(d->scale)) { set_error("%s: scale must be finite", fn); return HS_E_INVAL; }
+  if ((int64_t)d->q_tokens * (d->q_heads / d->kv_heads) > INT32_MAX - 1024) {
+    set_error("%s: too many tokens for one call (%d, of %d heads each)", fn, d->q_tokens, d->q_heads / d->kv_heads);
+    return HS_E_INVAL;
+  }
   return HS_OK;
 }
 
