@@ -3,7 +3,6 @@
 
 #include <math.h>
 
-
 #include <algorithm>
 
 namespace hs {
@@ -30,6 +29,8 @@ constexpr float kSlack = 8.0f;
 // what is lost of the others stays below 2^-32 of it.
 template <class T> constexpr float kRaise = __is_same(T, f16) ? 7.0f : 0.0f;
 constexpr float kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float positive_scale(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale); }
 
 struct CrossGrid {
   int row_tiles, splits;
@@ -69,8 +70,8 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
   const int all_tiles = (int)(((int64_t)n + BN - 1) / BN);
   const int first = (int)((int64_t)all_tiles * split / grid.splits), last = (int)((int64_t)all_tiles * (split + 1) / grid.splits);
 
-  // a negative scale is taken out of Q's signs, a zero one made positive: maxima of scores are maxima of exponents
-  const float scale = p.scale == 0.0f ? 1e-30f : fabsf(p.scale), c = scale * kLog2e;
+  // the scale's sign, and a scale of zero, are taken into Q: maxima of scores are maxima of exponents
+  const float scale = positive_scale(p.scale), c = scale * kLog2e;
   x8 q[KS];
   {
     const T* const src = at<T>(p.q, b, token, head);
@@ -80,6 +81,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
       const int d0 = 16 * k + 8 * half;
       if (live && d0 < p.dim) q[k] = *(const x8*)(src + d0);
       if (p.scale < 0.0f) q[k] = -q[k];
+      if (p.scale == 0.0f) q[k] = x8{};
     }
   }
   f32x16 o[DT] = {};
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
   const int64_t rows = (int64_t)p.q_tokens * p.group, all = (int64_t)p.batch * kv_heads * rows;
   const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
   if (id >= all) return;
-  const float scale = p.scale == 0.0f ? 1e-30f : fabsf(p.scale), c = scale * kLog2e;
+  const float scale = positive_scale(p.scale), c = scale * kLog2e;
   const int64_t row = id % rows, bh = id / rows, b = bh / kv_heads, token = row / p.group;
   const int head = (int)(bh % kv_heads) * p.group + (int)(row % p.group);
   const int d0 = 4 * (lane & 31), pitch = p.dim + 4;
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
   const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c);
-  l = m == -INFINITY ? 0.0f : l * f;
+  l *= f;                                           // (a part that saw no key has 0, one whose scores are NaN keeps that)
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
   f32x4 sum = {0, 0, 0, 0};

@@ -2,7 +2,6 @@
 #include "hs_track_device.h"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace hs {
 
@@ -17,13 +16,10 @@ namespace hs {
 // Sum over the LANES lanes of a group, in each of them: neighbours, pairs, then mirrored halves, whose lanes agree by then.
 template <int LANES>
 __device__ __forceinline__ float group_sum(float x) {
-  auto moved = [](float v, auto control) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
-  };
-  x += moved(x, std::integral_constant<int, 0xb1>{});                     // lane ^ 1
-  if (LANES > 2) x += moved(x, std::integral_constant<int, 0x4e>{});      // lane ^ 2
-  if (LANES > 4) x += moved(x, std::integral_constant<int, 0x141>{});     // 7 - lane
-  if (LANES > 8) x += moved(x, std::integral_constant<int, 0x140>{});     // 15 - lane
+  x += moved<0xb1>(x);                     // lane ^ 1
+  if (LANES > 2) x += moved<0x4e>(x);      // lane ^ 2
+  if (LANES > 4) x += moved<0x141>(x);     // 7 - lane
+  if (LANES > 8) x += moved<0x140>(x);     // 15 - lane
   return x;
 }
 

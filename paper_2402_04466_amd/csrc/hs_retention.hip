@@ -118,28 +118,55 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
   const bool last = segment == (all_chunks ? (all_chunks - 1) / per_segment : 0);   // the one with the end
   if (kStates ? !chunks || last : !chunks && !last) return;
 
-  // staging: this thread's 16-byte piece of rows r0, r0 + RP, ... of Q and K, and of a row of V (8 pieces)
+  // staging: this thread's 16-byte piece of rows r0, r0 + RP, ... of Q and K, and of a row of V (8 pieces).  Rows behind the
+  // last token are read as that one and emptied on their way into LDS.
   const int r0 = threadIdx.x / CH, ch = threadIdx.x % CH, vr = threadIdx.x / 8, vch = threadIdx.x % 8;
   const bool in_k = 8 * ch < p.key_dim, in_v = 64 * block + 8 * vch < p.value_dim;
-  const T* const qsrc = at<T>(p.q, b, 0, h) + 8 * ch;
-  const T* const ksrc = at<T>(p.k, b, 0, hk) + 8 * ch;
-  const T* const vsrc = at<T>(p.v, b, 0, hk) + 64 * block + 8 * vch;
-  s16x8 qreg[NL], kreg[NL], vreg;
-  auto fetch = [&](int c) {
-    const int64_t t0 = (int64_t)(first + c) * kChunk;
+  const T *qsrc[NL], *ksrc[NL], *vsrc;              // of the chunk that is fetched next
 #pragma unroll
-    for (int e = 0; e < NL; ++e) {
-      const int64_t t = t0 + r0 + e * RP;
-      qreg[e] = kreg[e] = s16x8{};
-      if (t < n && in_k) {
-        if (!kStates) qreg[e] = *(const s16x8*)(qsrc + t * p.q.token);
-        kreg[e] = *(const s16x8*)(ksrc + t * p.k.token);
+  for (int e = 0; e < NL; ++e) {
+    const int64_t t = (int64_t)first * kChunk + r0 + e * RP;
+    qsrc[e] = at<T>(p.q, b, t, h) + 8 * ch;
+    ksrc[e] = at<T>(p.k, b, t, hk) + 8 * ch;
+  }
+  vsrc = at<T>(p.v, b, (int64_t)first * kChunk + vr, hk) + 64 * block + 8 * vch;
+  s16x8 qreg[NL] = {}, kreg[NL] = {}, vreg = {};
+  auto left_of = [&](int c) { return (int)min((int64_t)n - (int64_t)(first + c) * kChunk, (int64_t)kChunk); };   // tokens of chunk c
+  auto fetch = [&](int c) {                         // chunk c, after the ones before it
+    if (c >= chunks) return;
+    const int left = left_of(c);
+    if (left < kChunk) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        const int64_t behind = max(r0 + e * RP - (left - 1), 0);
+        qsrc[e] -= behind * p.q.token;
+        ksrc[e] -= behind * p.k.token;
+      }
+      vsrc -= (int64_t)max(vr - (left - 1), 0) * p.v.token;
+    }
+    if (in_k) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        if (!kStates) qreg[e] = *(const s16x8*)qsrc[e];
+        kreg[e] = *(const s16x8*)ksrc[e];
       }
     }
-    vreg = s16x8{};
-    if (t0 + vr < n && in_v) vreg = *(const s16x8*)(vsrc + (t0 + vr) * p.v.token);
+    if (in_v) vreg = *(const s16x8*)vsrc;
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      qsrc[e] += kChunk * p.q.token;
+      ksrc[e] += kChunk * p.k.token;
+    }
+    vsrc += kChunk * p.v.token;
   };
-  auto store = [&](char* to) {
+  auto store = [&](int c, char* to) {
+    const int left = left_of(c);
+    if (left < kChunk) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e)
+        if (r0 + e * RP >= left) qreg[e] = kreg[e] = s16x8{};
+      if (vr >= left) vreg = s16x8{};
+    }
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
       if (!kStates) *(s16x8*)(to + slot<CH>(r0 + e * RP, ch)) = qreg[e];
@@ -165,7 +192,7 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
         S[t][i] = from && dv < p.value_dim && dk < p.key_dim ? from[state0 + (int64_t)dk * p.value_dim] : 0.0f;
       }
     if (chunks) {
-      store(lds);
+      store(0, lds);
       fetch(1);
     }
     // the state's 16-bit copy, [dimension][key dimension]
@@ -177,17 +204,22 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
         for (int t = 0; t < KT; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(S[t][i]));
+        most = wave_max(most);
+        if (most == INFINITY) {                     // (the finite values keep theirs)
+          most = 0.0f;
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(S[t][i]) < INFINITY ? fabsf(S[t][i]) : 0.0f);
+          most = wave_max(most);
+        }
         exponent = max(min(__builtin_amdgcn_frexp_expf(most) - 12, 100), -100);
         if (lane == 0) exponents[to][w4] = exponent;
       }
+      const float small = ldexpf(1.0f, -exponent);
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
-        x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (T)(kHalf ? ldexpf(S[t][i], -exponent) : S[t][i]);
-        *(x4*)(lds + kS + to * kCopy + slot<CH>(16 * w4 + l16, 2 * t + (g >> 1)) + (g & 1) * 8) = w;
+        *(x4*)(lds + kS + to * kCopy + slot<CH>(16 * w4 + l16, 2 * t + (g >> 1)) + (g & 1) * 8) = round4<T>(kHalf ? S[t] * small : S[t]);
       }
     };
     if (!kStates) leave_copy(0);
@@ -197,22 +229,26 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[kChunk - 1 - (32 * s + 8 * g + i)];
-    float keep = (float)power[kChunk], keep_rest = (float)(power[kChunk] - (double)keep);
+    // A chunk's decay in fp32; what that drops is carried to the next one, so that many chunks' decay is as exact.
+    const float keep = (float)power[kChunk], keep_rest = (float)(power[kChunk] - (double)keep);
+    float carried = 0.0f;
 
     for (int c = 0; c < chunks; ++c) {
       char* const here = lds + (c & 1) * kSlot;
       if (c + 1 < chunks) {
-        store(lds + (~c & 1) * kSlot);
+        store(c + 1, lds + (~c & 1) * kSlot);
         fetch(c + 2);
       }
-      const int64_t left = n - (int64_t)(first + c) * kChunk;
+      carried += keep_rest;
+      float now = keep + carried;
+      carried -= now - keep;
+      const int left = left_of(c);
       if (left < kChunk) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[max((int)left - 1 - (32 * s + 8 * g + i), 0)];   // (later values are zeros)
-        keep = (float)power[left];
-        keep_rest = (float)(power[left] - (double)keep);
+          for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[max(left - 1 - (32 * s + 8 * g + i), 0)];   // (later values are zeros)
+        now = (float)power[left];
       }
       x8 part[2][3];                                // decayed values: dimension 16 w4 + l16, tokens 32 s + 8 g + i
       const int r = 8 * g + (lane >> 2 & 3), low8 = (lane & 1) * 8;
@@ -221,22 +257,30 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
         const char* const from = here + kV + 32 * s * 128 + low8;
         const int cc = 2 * w4 + (lane >> 1 & 1);
         const x8 v = join8<T>(read_transposed(from + slot<8>(r, cc)), read_transposed(from + slot<8>(r + 4, cc)));
+        float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          float x = (float)v[i] * weight[s][i];
-          asm("" : "+v"(x));   // the rounded product: rounded to 16 bits from the exact one in one place and from this in another, a
-                               // part and what is left of it would not belong together
-          part[s][0][i] = (T)x;
-          x -= (float)part[s][0][i];
-          if (kHalf) x *= 4096.0f;
-          part[s][1][i] = (T)x;
-          if (!kHalf) part[s][2][i] = (T)(x - (float)part[s][1][i]);
+          x[i] = (float)v[i] * weight[s][i];
+          asm("" : "+v"(x[i]));   // the rounded product: rounded to 16 bits from the exact one in one place and from this in another, a
+                                  // part and what is left of it would not belong together
+        }
+        part[s][0] = round8<T>(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] -= (float)part[s][0][i];
+          if (kHalf) x[i] *= 4096.0f;
+        }
+        part[s][1] = round8<T>(x);
+        if (!kHalf) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] -= (float)part[s][1][i];
+          part[s][2] = round8<T>(x);
         }
       }
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S[t][i] = fmaf(S[t][i], keep, S[t][i] * keep_rest);
+        for (int i = 0; i < 4; ++i) S[t][i] *= now;
         f32x4 low = {0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -269,7 +313,7 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
   } else {
     // ---- out: rows 16 w4 .. + 15 of the chunk, lane has row 16 w4 + l16
     if (chunks) {
-      store(lds);
+      store(0, lds);
       fetch(1);
     }
     __syncthreads();
@@ -287,7 +331,7 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
       const char* const here = lds + (c & 1) * kSlot;
       const char* const copy = lds + kS + (c & 1) * kCopy;
       if (c + 1 < chunks) {
-        store(lds + (~c & 1) * kSlot);
+        store(c + 1, lds + (~c & 1) * kSlot);
         fetch(c + 2);
       }
       if (kStates) {
@@ -298,13 +342,22 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
 #pragma unroll
       for (int s = 0; s < KS; ++s) q[s] = *(const x8*)(here + 16 * w4 * CH * 16 + slot<CH>(l16, 4 * s + g));
       f32x4 o[4];
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
+      auto from_state = [&](int d) {
         o[d] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KS; ++s) o[d] = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], o[d]);
         o[d] *= kHalf ? ldexpf(after, exponents[c & 1][d]) : after;
-      }
+      };
+      auto scores = [&](int cb) {
+        f32x4 t = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(here + kK + 16 * cb * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] *= decay[cb][i];
+        return t;
+      };
+#pragma unroll
+      for (int d = 0; d < 4; ++d) from_state(d);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {                 // 32 keys
         if (2 * j > w4) break;
@@ -313,11 +366,9 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
         for (int e = 0; e < 2; ++e) {
           const int cb = 2 * j + e;
           if (cb > w4) break;
-          f32x4 t = {0, 0, 0, 0};
+          const f32x4 t = scores(cb);
 #pragma unroll
-          for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(here + kK + 16 * cb * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) a[4 * e + i] = (T)(t[i] * decay[cb][i]);
+          for (int i = 0; i < 4; ++i) a[4 * e + i] = (T)t[i];
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
@@ -326,15 +377,42 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
           o[d] = mfma16(join8<T>(read_transposed(from + slot<8>(vrow, cc)), read_transposed(from + 16 * 128 + slot<8>(vrow, cc))), a, o[d]);
         }
       }
+      float finite = 0.0f;                          // zero, or NaN
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) finite = fmaf(o[d][i], 0.0f, finite);
+      if (__any(finite != 0.0f)) {
+        // A product beyond fp16's range, or an input that is not finite, which must not reach earlier tokens through their zeros
+        // in A: term by term, in fp32.
+#pragma unroll
+        for (int d = 0; d < 4; ++d) from_state(d);
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) {
+          if (cb > w4) break;
+          const f32x4 t = scores(cb);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+            for (int from = 0; from < 4; ++from) {
+              const int key = 16 * cb + 4 * from + i;
+              const float a = __shfl(t[i], 16 * from + l16);
+              if (key > 16 * w4 + l16) continue;
+#pragma unroll
+              for (int d = 0; d < 4; ++d) {
+                const x4 v = *(const x4*)(here + kV + slot<8>(key, 2 * d + (g >> 1)) + (g & 1) * 8);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][e] = fmaf(a, (float)v[e], o[d][e]);
+              }
+            }
+        }
+      }
       const int64_t t = (int64_t)(first + c) * kChunk + 16 * w4 + l16;
       if (t < n) {
         T* const to = at_out<T>(p.out, b, t, h) + 64 * block + 4 * g;
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          x4 y;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = (T)o[d][i];
-          if (64 * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = y;
+          if (64 * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = round4<T>(o[d]);
         }
       }
       __syncthreads();

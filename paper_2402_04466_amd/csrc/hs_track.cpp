@@ -134,6 +134,10 @@ hs_status check(const char* fn, const hs_norm_rotate_desc* d) {
     set_error("%s: bad number of heads (%d and %d)", fn, d->q_heads, d->k_heads);
     return HS_E_INVAL;
   }
+  if ((int64_t)d->batch * d->tokens > INT32_MAX) {
+    set_error("%s: too many tokens for one call (%d x %d)", fn, d->batch, d->tokens);
+    return HS_E_INVAL;
+  }
   if (d->rotary_dim < 0 || d->rotary_dim > d->head_dim || d->rotary_dim % 16) {
     set_error("%s: rotary_dim must be a multiple of 16 in 0..head_dim, got %d", fn, d->rotary_dim);
     return HS_E_INVAL;
@@ -214,6 +218,10 @@ hs_status check(const char* fn, const hs_cross_attention_desc* d) {   // all but
   HS_TRY(check_groups(fn, d->q_heads, d->kv_heads));
   HS_TRY(check_dim(fn, "head_dim", d->head_dim));
   if (!std::isfinite(d->scale)) { set_error("%s: scale must be finite", fn); return HS_E_INVAL; }
+  if ((int64_t)d->batch * d->q_heads > INT32_MAX) {
+    set_error("%s: too many heads of sequences for one call (%d x %d)", fn, d->batch, d->q_heads);
+    return HS_E_INVAL;
+  }
   if ((int64_t)d->q_tokens * (d->q_heads / d->kv_heads) > INT32_MAX - 1024) {
     set_error("%s: too many tokens for one call (%d, of %d heads each)", fn, d->q_tokens, d->q_heads / d->kv_heads);
     return HS_E_INVAL;

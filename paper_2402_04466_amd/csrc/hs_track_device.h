@@ -78,6 +78,26 @@ __device__ __forceinline__ void both_halves(float x, float& lower, float& upper)
   upper = __builtin_bit_cast(float, r1);
 }
 
+// The largest of a wave's values (NaN is left out), in all lanes: rows of 16 by neighbours, pairs and mirrored halves, then
+// pairs of rows and the wave's halves.
+template <int CONTROL>
+__device__ __forceinline__ float moved(float x) {   // from another lane of the row of 16
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, moved<0xb1>(x));                     // lane ^ 1
+  x = fmaxf(x, moved<0x4e>(x));                     // lane ^ 2
+  x = fmaxf(x, moved<0x141>(x));                    // 7 - lane
+  x = fmaxf(x, moved<0x140>(x));                    // 15 - lane
+  const unsigned bits = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+  const unsigned r0 = r[0], r1 = r[1];
+  x = fmaxf(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
+  float lower, upper;
+  both_halves(x, lower, upper);
+  return fmaxf(lower, upper);
+}
+
 template <class T>
 __device__ __forceinline__ const T* at(const Heads& h, int64_t batch, int64_t token, int64_t head) {
   return (const T*)h.p + batch * h.batch + token * h.token + head * h.head;

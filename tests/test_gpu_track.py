@@ -499,3 +499,64 @@ def test_refused_calls_change_nothing(hs, ctx, gen):
         retention_call(hs, ctx, x, x, x, out, None, torch.empty(1, 2, 64, 64, device=DEV), [0.5, 2.0], 1.0)
     torch.cuda.synchronize()
     assert bool((out == 7).all())
+
+
+def finite_check(got, want, bound, what):
+    """Finite where the definition is, and there within the bound."""
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), fine), what
+    close(torch.where(fine, got.double(), 0.0), torch.where(fine, want, 0.0), torch.where(fine, bound, 0.0), what)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n, spot", [(5, 3), (70, 1), (70, 40), (200, 63), (200, 64), (200, 171), (2600, 1500)])
+@pytest.mark.parametrize("which", ["q", "k", "v"])
+def test_what_is_not_finite_reaches_no_earlier_token(hs, ctx, gen, dtype, n, spot, which):
+    """An infinity or NaN in one token: tokens before it, and what it has no part in, keep their values."""
+    t = TYPES[dtype]
+    b, h, dk, dv = 2, 2, 64, 72
+    q, k, v, state, _ = retention_inputs(gen, b, n, h, h, dk, dv, t)
+    decay, u, steps = [0.9, 0.99], half_step(t), (64 + 2 * n) * F32
+    {"q": q, "k": k, "v": v}[which][0, spot, 0, 5] = float("nan")
+    {"q": q, "k": k, "v": v}[which][1, spot, 1, 60] = float("inf")
+    out, S, size, A = retention_reference(q, k, v, state, decay, 0.125, None)
+    got, end = torch.full_like(out, 7.0, dtype=t), torch.full_like(state, 7.0)
+    retention_call(hs, ctx, q, k, v, got, state, end, decay, 0.125)
+    finite_check(got, out, u * out.abs() + (u + steps) * (1 + u) * size + 2.0 ** -25, "out")
+    finite_check(end, S, steps * A + 2.0 ** -40, "state")
+
+
+@pytest.mark.parametrize("n", [3, 64, 150])
+def test_products_beyond_the_range_of_fp16(hs, ctx, gen, n):
+    """q k alone is beyond 65504, what it weighs is not."""
+    b, h, d, t = 2, 3, 64, torch.float16
+    q, k, v, state, _ = retention_inputs(gen, b, n, h, h, d, d, t)
+    q, k, v, decay = q * 400, k * 400, v * 0.01, [0.0, 0.5, 0.9]
+    out, S, size, A = retention_reference(q, k, v, state, decay, 0.125, None)
+    assert out.abs().max() < 60000, "meant to be in range"
+    got, end = torch.empty_like(q), torch.empty_like(state)
+    retention_call(hs, ctx, q, k, v, got, state, end, decay, 0.125)
+    retention_check(got, end, (out, S, size, A), t, n, "large")
+
+
+@pytest.mark.parametrize("scale", [0.0, 0.125])
+def test_nan_in_a_visible_key_is_not_lost(hs, ctx, gen, scale):
+    """In one of many parts that the keys are cut into: as the formula, every token that sees it gets NaN."""
+    b, nq, nk, h, d = 2, 3, 4000, 2, 64
+    q, k, v = (normal(gen, b, n, h, d, dtype=torch.bfloat16) for n in (nq, nk, nk))
+    k[0, 100:2200, 1] = float("nan")
+    out, lse = torch.empty_like(q), torch.empty(b, h, nq, device=DEV)
+    cross_call(hs, ctx, q, k, v, out, scale, lse=lse)
+    assert torch.isnan(out[0, :, 1]).all() and torch.isnan(lse[0, 1]).all()
+    keep = torch.ones(b, h, dtype=torch.bool, device=DEV)
+    keep[0, 1] = False
+    assert torch.isfinite(out.transpose(1, 2)[keep]).all() and torch.isfinite(lse[keep]).all()
+
+
+def test_a_scale_of_zero_averages_whatever_the_scores(hs, ctx, gen):
+    b, nq, nk, h, d = 1, 40, 90, 2, 64
+    q, k, v = (normal(gen, b, n, h, d, dtype=torch.bfloat16) for n in (nq, nk, nk))
+    q, k = q * 1e17, k * 1e17
+    out, lse = torch.empty_like(q), torch.empty(b, h, nq, device=DEV)
+    cross_call(hs, ctx, q, k, v, out, 0.0, lse=lse)
+    cross_check(out, lse, torch.zeros_like(q), k, v, 0.0, torch.ones(b, nk, dtype=torch.bool, device=DEV), "zero")
