@@ -2,6 +2,7 @@
 #include "hs_track_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace hs {
 
@@ -76,13 +77,16 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 // i, j = 0 .. c - 1:
 //   A_ij = scale * decay^(i - j) q_i k_j (j <= i)          out_i = sum_j A_ij v_j + scale * decay^(i + 1) S^T q_i
 //   S   <- decay^c S + sum_j k_j (decay^(c - 1 - j) v_j)^T
-// A workgroup has one sequence and head and 64 of the values' dimensions, and waves of two kinds, one of each per SIMD:
+// A workgroup has one sequence and head and 64 of the values' dimensions, and waves of three kinds, one of each per SIMD:
 //   waves 0 .. 3 carry the state, 16 of the dimensions each, in their accumulators, and leave a 16-bit copy of it in LDS
 //   for the next chunk;
-//   waves 4 .. 7 form out, 16 of the chunk's rows each: A by K Q^T, so that a lane holds four keys of one row per tile
+//   waves 4 .. 7 load: a chunk that is two ahead is on its way from memory into their registers while the next one goes
+//   from there into the other half of LDS, with the values' decayed parts;
+//   waves 8 .. 11 form out, 16 of the chunk's rows each: A by K Q^T, so that a lane holds four keys of one row per tile
 //   and A is the operand of the next product where it lies, if that one takes V's rows in the same order.
-// While a chunk is worked on the next one goes from registers into the other half of LDS and the one behind it is on
-// its way from memory; one barrier a chunk.
+// One barrier a chunk.  The chain of LDS reads and products from barrier to barrier bounds it: with eight waves that shared the
+// loads, 10 chunks of 64 sequences took 19.9 us (now 15.5), ragged clips of 96 x 80 38.7 (29.3), 113 chunks of 128 x 128 in 256
+// workgroups 280 (270: 3.6 TB/s, where the loads alone take 168).  The waves that form out are the longest, and go first.
 //
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
 // is then half a step off, as out itself); of the fp16 copy a power of two is taken out, so that it stays in
@@ -94,17 +98,17 @@ constexpr int kChunk = 64;
 // every segment but the last adds to a state of zeros, a second one (k_retain_starts) puts together by the decays of whole
 // segments what each starts from, and the third goes on from there as above.
 template <class T, int KP, bool kStates>
-__global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int segments) {
+__global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(RetentionParams p, int segments) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
   constexpr int CH = KP / 8, KT = KP / 16, KS = KP / 32;   // KT: 16-wide tiles of key dimensions, KS: steps of 32
-  constexpr int RP = 512 / CH, NL = kChunk / RP;    // rows per pass of the workgroup over Q or K, passes
+  constexpr int RP = 256 / CH, NL = kChunk / RP, NV = 2;   // rows per pass of the waves that load over Q or K, passes over them and V
   constexpr bool kHalf = __is_same(T, f16);
-  constexpr int kK = kChunk * KP * 2, kV = 2 * kK, kSlot = kV + kChunk * 64 * 2;   // Q, K and V of a chunk
+  constexpr int kParts = kHalf ? 2 : 3, kVTile = kChunk * 64 * 2;
+  constexpr int kK = kChunk * KP * 2, kV = 2 * kK, kP = kV + kVTile, kSlot = kP + kParts * kVTile;   // Q, K, V of a chunk, V's decayed parts
   constexpr int kS = 2 * kSlot, kCopy = 64 * KP * 2;
   __shared__ __align__(16) char lds[kS + 2 * kCopy];
-  __shared__ int exponents[2][4];
-  __shared__ double power[kChunk + 1];
+  __shared__ int exponents[kHalf ? 2 : 1][kHalf ? 4 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w4 = wave & 3, l16 = lane & 15, g = lane >> 4;
   const int blocks = (p.value_dim + 63) / 64;
   int id = xcd_number();
@@ -118,64 +122,11 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
   const bool last = segment == (all_chunks ? (all_chunks - 1) / per_segment : 0);   // the one with the end
   if (kStates ? !chunks || last : !chunks && !last) return;
 
-  // staging: this thread's 16-byte piece of rows r0, r0 + RP, ... of Q and K, and of a row of V (8 pieces).  Rows behind the
-  // last token are read as that one and emptied on their way into LDS.
-  const int r0 = threadIdx.x / CH, ch = threadIdx.x % CH, vr = threadIdx.x / 8, vch = threadIdx.x % 8;
-  const bool in_k = 8 * ch < p.key_dim, in_v = 64 * block + 8 * vch < p.value_dim;
-  const T *qsrc[NL], *ksrc[NL], *vsrc;              // of the chunk that is fetched next
-#pragma unroll
-  for (int e = 0; e < NL; ++e) {
-    const int64_t t = (int64_t)first * kChunk + r0 + e * RP;
-    qsrc[e] = at<T>(p.q, b, t, h) + 8 * ch;
-    ksrc[e] = at<T>(p.k, b, t, hk) + 8 * ch;
-  }
-  vsrc = at<T>(p.v, b, (int64_t)first * kChunk + vr, hk) + 64 * block + 8 * vch;
-  s16x8 qreg[NL] = {}, kreg[NL] = {}, vreg = {};
   auto left_of = [&](int c) { return (int)min((int64_t)n - (int64_t)(first + c) * kChunk, (int64_t)kChunk); };   // tokens of chunk c
-  auto fetch = [&](int c) {                         // chunk c, after the ones before it
-    if (c >= chunks) return;
-    const int left = left_of(c);
-    if (left < kChunk) {
-#pragma unroll
-      for (int e = 0; e < NL; ++e) {
-        const int64_t behind = max(r0 + e * RP - (left - 1), 0);
-        qsrc[e] -= behind * p.q.token;
-        ksrc[e] -= behind * p.k.token;
-      }
-      vsrc -= (int64_t)max(vr - (left - 1), 0) * p.v.token;
-    }
-    if (in_k) {
-#pragma unroll
-      for (int e = 0; e < NL; ++e) {
-        if (!kStates) qreg[e] = *(const s16x8*)qsrc[e];
-        kreg[e] = *(const s16x8*)ksrc[e];
-      }
-    }
-    if (in_v) vreg = *(const s16x8*)vsrc;
-#pragma unroll
-    for (int e = 0; e < NL; ++e) {
-      qsrc[e] += kChunk * p.q.token;
-      ksrc[e] += kChunk * p.k.token;
-    }
-    vsrc += kChunk * p.v.token;
-  };
-  auto store = [&](int c, char* to) {
-    const int left = left_of(c);
-    if (left < kChunk) {
-#pragma unroll
-      for (int e = 0; e < NL; ++e)
-        if (r0 + e * RP >= left) qreg[e] = kreg[e] = s16x8{};
-      if (vr >= left) vreg = s16x8{};
-    }
-#pragma unroll
-    for (int e = 0; e < NL; ++e) {
-      if (!kStates) *(s16x8*)(to + slot<CH>(r0 + e * RP, ch)) = qreg[e];
-      *(s16x8*)(to + kK + slot<CH>(r0 + e * RP, ch)) = kreg[e];
-    }
-    *(s16x8*)(to + kV + slot<8>(vr, vch)) = vreg;
-  };
-  if (chunks) fetch(0);
-  if (threadIdx.x >= 384 && threadIdx.x <= 384 + kChunk) power[threadIdx.x - 384] = exp2(p.log2_decay[h] * (threadIdx.x - 384));
+  // the decay's powers below the chunk's: a wave has one per lane
+  const double power64 = exp2(p.log2_decay[h] * lane);
+  const float power = (float)power64;
+  auto power_of = [&](int steps) { return __shfl(power, steps); };
 
   if (wave < 4) {
     // ---- the state: lane has dimension dv, key dimensions 16 t + 4 g + i
@@ -191,10 +142,6 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
         const int dk = 16 * t + 4 * g + i;
         S[t][i] = from && dv < p.value_dim && dk < p.key_dim ? from[state0 + (int64_t)dk * p.value_dim] : 0.0f;
       }
-    if (chunks) {
-      store(0, lds);
-      fetch(1);
-    }
     // the state's 16-bit copy, [dimension][key dimension]
     auto leave_copy = [&](int to) {
       int exponent = 0;
@@ -223,60 +170,29 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
       }
     };
     if (!kStates) leave_copy(0);
-    __syncthreads();
-    float weight[2][8];                             // decays of v_j in S
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[kChunk - 1 - (32 * s + 8 * g + i)];
     // A chunk's decay in fp32; what that drops is carried to the next one, so that many chunks' decay is as exact.
-    const float keep = (float)power[kChunk], keep_rest = (float)(power[kChunk] - (double)keep);
+    const double half_chunk = __shfl(power64, kChunk / 2), whole = half_chunk * half_chunk;
+    const float keep = (float)whole, keep_rest = (float)(whole - (double)keep);
     float carried = 0.0f;
+    const int r = 8 * g + (lane >> 2 & 3), low8 = (lane & 1) * 8;
+    __syncthreads();
 
     for (int c = 0; c < chunks; ++c) {
       char* const here = lds + (c & 1) * kSlot;
-      if (c + 1 < chunks) {
-        store(c + 1, lds + (~c & 1) * kSlot);
-        fetch(c + 2);
-      }
       carried += keep_rest;
       float now = keep + carried;
       carried -= now - keep;
       const int left = left_of(c);
-      if (left < kChunk) {
+      if (left < kChunk) now = power_of(left);
+      x8 part[2][kParts];                           // decayed values: dimension 16 w4 + l16, tokens 32 s + 8 g + i
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) weight[s][i] = (float)power[max(left - 1 - (32 * s + 8 * g + i), 0)];   // (later values are zeros)
-        now = (float)power[left];
-      }
-      x8 part[2][3];                                // decayed values: dimension 16 w4 + l16, tokens 32 s + 8 g + i
-      const int r = 8 * g + (lane >> 2 & 3), low8 = (lane & 1) * 8;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const char* const from = here + kV + 32 * s * 128 + low8;
-        const int cc = 2 * w4 + (lane >> 1 & 1);
-        const x8 v = join8<T>(read_transposed(from + slot<8>(r, cc)), read_transposed(from + slot<8>(r + 4, cc)));
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] = (float)v[i] * weight[s][i];
-          asm("" : "+v"(x[i]));   // the rounded product: rounded to 16 bits from the exact one in one place and from this in another, a
-                                  // part and what is left of it would not belong together
+        for (int e = 0; e < kParts; ++e) {
+          const char* const from = here + kP + e * kVTile + 32 * s * 128 + low8;
+          const int cc = 2 * w4 + (lane >> 1 & 1);
+          part[s][e] = join8<T>(read_transposed(from + slot<8>(r, cc)), read_transposed(from + slot<8>(r + 4, cc)));
         }
-        part[s][0] = round8<T>(x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] -= (float)part[s][0][i];
-          if (kHalf) x[i] *= 4096.0f;
-        }
-        part[s][1] = round8<T>(x);
-        if (!kHalf) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] -= (float)part[s][1][i];
-          part[s][2] = round8<T>(x);
-        }
-      }
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
 #pragma unroll
@@ -296,6 +212,7 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
           }
         }
         if (kHalf) S[t] += low * (1.0f / 4096.0f);
+        if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (reads further ahead would not fit the registers)
       }
       if (!kStates && c + 1 < chunks) leave_copy(~c & 1);
       __syncthreads();
@@ -310,115 +227,216 @@ __global__ __launch_bounds__(512) void k_retain_chunks(RetentionParams p, int se
         const int dk = 16 * t + 4 * g + i;
         if (dv < p.value_dim && dk < p.key_dim) to[(int64_t)dk * p.value_dim] = S[t][i];
       }
-  } else {
-    // ---- out: rows 16 w4 .. + 15 of the chunk, lane has row 16 w4 + l16
-    if (chunks) {
-      store(0, lds);
-      fetch(1);
-    }
+  } else if (wave < 8) {
+    // ---- loads: this thread's 16-byte pieces of rows r0, r0 + RP, ... of Q and K, and of two rows of V (8 pieces).  Rows behind
+    // the last token are read as that one and emptied on their way into LDS.
+    const int tid = threadIdx.x & 255, r0 = tid / CH, ch = tid % CH, vr = tid / 8, vch = tid % 8;
+    const bool in_k = 8 * ch < p.key_dim, in_v = 64 * block + 8 * vch < p.value_dim;
+    const T* qsrc = at<T>(p.q, b, (int64_t)first * kChunk + r0, h) + 8 * ch;   // of the chunk that is fetched next
+    const T* ksrc = at<T>(p.k, b, (int64_t)first * kChunk + r0, hk) + 8 * ch;
+    const T* vsrc = at<T>(p.v, b, (int64_t)first * kChunk + vr, hk) + 64 * block + 8 * vch;
+    struct Pieces { s16x8 q[NL], k[NL], v[NV]; } even = {}, odd = {};          // of chunks on their way
+    auto fetch = [&](int c, Pieces& to) {           // chunk c, after the ones before it
+      if (c >= chunks) return;
+      const int left = left_of(c);
+      const T *qa[NL], *ka[NL], *va[NV];
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        qa[e] = qsrc + e * RP * p.q.token;
+        ka[e] = ksrc + e * RP * p.k.token;
+      }
+#pragma unroll
+      for (int e = 0; e < NV; ++e) va[e] = vsrc + e * 32 * p.v.token;
+      if (left < kChunk) {
+#pragma unroll
+        for (int e = 0; e < NL; ++e) {
+          const int64_t behind = max(r0 + e * RP - (left - 1), 0);
+          qa[e] -= behind * p.q.token;
+          ka[e] -= behind * p.k.token;
+        }
+#pragma unroll
+        for (int e = 0; e < NV; ++e) va[e] -= (int64_t)max(vr + e * 32 - (left - 1), 0) * p.v.token;
+      }
+      if (in_k) {
+#pragma unroll
+        for (int e = 0; e < NL; ++e) {
+          if (!kStates) to.q[e] = *(const s16x8*)qa[e];
+          to.k[e] = *(const s16x8*)ka[e];
+        }
+      }
+      if (in_v) {
+#pragma unroll
+        for (int e = 0; e < NV; ++e) to.v[e] = *(const s16x8*)va[e];
+      }
+      qsrc += kChunk * p.q.token;
+      ksrc += kChunk * p.k.token;
+      vsrc += kChunk * p.v.token;
+    };
+    float weight[NV];                               // v's decay until the chunk's end
+#pragma unroll
+    for (int e = 0; e < NV; ++e) weight[e] = power_of(kChunk - 1 - vr - e * 32);
+    auto store = [&](int c, Pieces& from) {
+      if (c >= chunks) return;
+      char* const to = lds + (c & 1) * kSlot;
+      const int left = left_of(c);
+      if (left < kChunk) {
+#pragma unroll
+        for (int e = 0; e < NL; ++e)
+          if (r0 + e * RP >= left) from.q[e] = from.k[e] = s16x8{};
+#pragma unroll
+        for (int e = 0; e < NV; ++e) {
+          weight[e] = power_of(max(left - 1 - vr - e * 32, 0));
+          if (vr + e * 32 >= left) from.v[e] = s16x8{};
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        if (!kStates) *(s16x8*)(to + slot<CH>(r0 + e * RP, ch)) = from.q[e];
+        *(s16x8*)(to + kK + slot<CH>(r0 + e * RP, ch)) = from.k[e];
+      }
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        const int at_v = slot<8>(vr + u * 32, vch);
+        if (!kStates) *(s16x8*)(to + kV + at_v) = from.v[u];
+        const x8 v = __builtin_bit_cast(x8, from.v[u]);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] = (float)v[i] * weight[u];
+          asm("" : "+v"(x[i]));   // the rounded product: rounded to 16 bits from the exact one in one place and from this in another,
+                                  // a part and what is left of it would not belong together
+        }
+#pragma unroll
+        for (int e = 0; e < kParts; ++e) {
+          const x8 part = round8<T>(x);
+          *(x8*)(to + kP + e * kVTile + at_v) = part;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = (x[i] - (float)part[i]) * (kHalf ? 4096.0f : 1.0f);
+        }
+      }
+    };
+    fetch(0, even);
+    fetch(1, odd);
+    store(0, even);
+    fetch(2, even);
     __syncthreads();
-    float decay[4][4];                              // of A's tiles: keys 16 cb + 4 g + i
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int apart = 16 * (w4 - cb) + l16 - 4 * g - i;
-        decay[cb][i] = apart < 0 ? 0.0f : p.scale * (float)power[max(apart, 0)];
-      }
-    const float after = p.scale * (float)power[16 * w4 + l16 + 1];
-    const int vrow = 4 * g + (lane >> 2 & 3), low8 = (lane & 1) * 8;
-    for (int c = 0; c < chunks; ++c) {
-      const char* const here = lds + (c & 1) * kSlot;
-      const char* const copy = lds + kS + (c & 1) * kCopy;
-      if (c + 1 < chunks) {
-        store(c + 1, lds + (~c & 1) * kSlot);
-        fetch(c + 2);
-      }
-      if (kStates) {
-        __syncthreads();
-        continue;
-      }
-      x8 q[KS];
-#pragma unroll
-      for (int s = 0; s < KS; ++s) q[s] = *(const x8*)(here + 16 * w4 * CH * 16 + slot<CH>(l16, 4 * s + g));
-      f32x4 o[4];
-      auto from_state = [&](int d) {
-        o[d] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) o[d] = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], o[d]);
-        o[d] *= kHalf ? ldexpf(after, exponents[c & 1][d]) : after;
-      };
-      auto scores = [&](int cb) {
-        f32x4 t = {0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(here + kK + 16 * cb * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] *= decay[cb][i];
-        return t;
-      };
-#pragma unroll
-      for (int d = 0; d < 4; ++d) from_state(d);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {                 // 32 keys
-        if (2 * j > w4) break;
-        x8 a = {};
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int cb = 2 * j + e;
-          if (cb > w4) break;
-          const f32x4 t = scores(cb);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) a[4 * e + i] = (T)t[i];
-        }
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const char* const from = here + kV + 32 * j * 128 + low8;
-          const int cc = 2 * d + (lane >> 1 & 1);
-          o[d] = mfma16(join8<T>(read_transposed(from + slot<8>(vrow, cc)), read_transposed(from + 16 * 128 + slot<8>(vrow, cc))), a, o[d]);
-        }
-      }
-      float finite = 0.0f;                          // zero, or NaN
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) finite = fmaf(o[d][i], 0.0f, finite);
-      if (__any(finite != 0.0f)) {
-        // A product beyond fp16's range, or an input that is not finite, which must not reach earlier tokens through their zeros
-        // in A: term by term, in fp32.
-#pragma unroll
-        for (int d = 0; d < 4; ++d) from_state(d);
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
-          if (cb > w4) break;
-          const f32x4 t = scores(cb);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll 1
-            for (int from = 0; from < 4; ++from) {
-              const int key = 16 * cb + 4 * from + i;
-              const float a = __shfl(t[i], 16 * from + l16);
-              if (key > 16 * w4 + l16) continue;
-#pragma unroll
-              for (int d = 0; d < 4; ++d) {
-                const x4 v = *(const x4*)(here + kV + slot<8>(key, 2 * d + (g >> 1)) + (g & 1) * 8);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[d][e] = fmaf(a, (float)v[e], o[d][e]);
-              }
-            }
-        }
-      }
-      const int64_t t = (int64_t)(first + c) * kChunk + 16 * w4 + l16;
-      if (t < n) {
-        T* const to = at_out<T>(p.out, b, t, h) + 64 * block + 4 * g;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          if (64 * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = round4<T>(o[d]);
-        }
-      }
+    for (int c = 0; c < chunks; c += 2) {
+      store(c + 1, odd);
+      fetch(c + 3, odd);
+      __syncthreads();
+      if (c + 1 >= chunks) break;
+      store(c + 2, even);
+      fetch(c + 4, even);
       __syncthreads();
     }
-    if (last && in_v)
-      for (int64_t t = (int64_t)n + vr - 32; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + 64 * block + 8 * vch) = s16x8{};
+    if (!kStates && last && in_v)
+      for (int64_t t = (int64_t)n + vr; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + 64 * block + 8 * vch) = s16x8{};
+  } else if (!kStates) {
+    // ---- out: rows 16 w4 .. + 15 of the chunk, lane has row 16 w4 + l16
+    __builtin_amdgcn_s_setprio(1);
+    const int vrow = 4 * g + (lane >> 2 & 3), low8 = (lane & 1) * 8;
+    auto run = [&](auto which) {                    // W = w4, so that each wave's share of the triangle is straight code
+      constexpr int W = decltype(which)::value;
+      float decay[W + 1][4];                        // of A's tiles: keys 16 cb + 4 g + i
+#pragma unroll
+      for (int cb = 0; cb <= W; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int apart = 16 * (W - cb) + l16 - 4 * g - i;
+          const float x = p.scale * power_of(max(apart, 0));
+          decay[cb][i] = apart < 0 ? 0.0f : x;
+        }
+      const float after = p.scale * (power_of(16 * W + l16) * p.decay[h]);
+      __syncthreads();
+      for (int c = 0; c < chunks; ++c) {
+        const char* const here = lds + (c & 1) * kSlot;
+        const char* const copy = lds + kS + (c & 1) * kCopy;
+        x8 q[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = *(const x8*)(here + 16 * W * CH * 16 + slot<CH>(l16, 4 * s + g));
+        f32x4 o[4];
+        auto from_state = [&]() {
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            o[d] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) o[d] = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], o[d]);
+            o[d] *= kHalf ? ldexpf(after, exponents[c & 1][d]) : after;
+          }
+        };
+        auto scores = [&](int cb) {
+          f32x4 t = {0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(here + kK + 16 * cb * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
+          return t;
+        };
+        x8 a[W / 2 + 1];                            // 32 keys each
+#pragma unroll
+        for (int j = 0; j <= W / 2; ++j) {
+          float x[8] = {};
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (2 * j + e <= W) {
+              const f32x4 t = scores(2 * j + e);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[4 * e + i] = t[i] * decay[2 * j + e][i];
+            }
+          a[j] = round8<T>(x);
+        }
+        __builtin_amdgcn_sched_barrier(0);          // (as above)
+        from_state();
+#pragma unroll
+        for (int j = 0; j <= W / 2; ++j)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const char* const from = here + kV + 32 * j * 128 + low8;
+            const int cc = 2 * d + (lane >> 1 & 1);
+            o[d] = mfma16(join8<T>(read_transposed(from + slot<8>(vrow, cc)), read_transposed(from + 16 * 128 + slot<8>(vrow, cc))), a[j], o[d]);
+          }
+        float finite = 0.0f;                        // zero, or NaN
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) finite = fmaf(o[d][i], 0.0f, finite);
+        if (__any(finite != 0.0f)) {
+          // A product beyond fp16's range, or an input that is not finite, which must not reach earlier tokens through their
+          // zeros in A: term by term, in fp32.
+          from_state();
+#pragma unroll 1
+          for (int cb = 0; cb <= W; ++cb) {
+            const f32x4 t = scores(cb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+              for (int from = 0; from < 4; ++from) {
+                const int key = 16 * cb + 4 * from + i, apart = 16 * W + l16 - key;
+                const float x = __shfl(t[i], 16 * from + l16) * (p.scale * power_of(max(apart, 0)));
+                if (apart < 0) continue;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                  const x4 v = *(const x4*)(here + kV + slot<8>(key, 2 * d + (g >> 1)) + (g & 1) * 8);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[d][e] = fmaf(x, (float)v[e], o[d][e]);
+                }
+              }
+          }
+        }
+        const int64_t t = (int64_t)(first + c) * kChunk + 16 * W + l16;
+        if (t < n) {
+          T* const to = at_out<T>(p.out, b, t, h) + 64 * block + 4 * g;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            if (64 * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = round4<T>(o[d]);
+        }
+        __syncthreads();
+      }
+    };
+    switch (w4) {
+      case 0: run(std::integral_constant<int, 0>{}); break;
+      case 1: run(std::integral_constant<int, 1>{}); break;
+      case 2: run(std::integral_constant<int, 2>{}); break;
+      default: run(std::integral_constant<int, 3>{}); break;
+    }
   }
 }
 
@@ -490,7 +508,7 @@ hipError_t launch(const RetentionParams& p, hipStream_t stream) {
     const hipError_t joined = launch_kernel((const void*)k_retain_starts, ((int64_t)p.batch * p.q_heads * p.key_dim * p.value_dim / 4 + 255) / 256, 256, args, stream);
     if (joined != hipSuccess) return joined;
   }
-  return launch_kernel(half ? chunks_kernel<f16>(wide, false) : chunks_kernel<bf16>(wide, false), plan.workgroups * plan.segments, 512, args, stream);
+  return launch_kernel(half ? chunks_kernel<f16>(wide, false) : chunks_kernel<bf16>(wide, false), plan.workgroups * plan.segments, 768, args, stream);
 }
 
 }  // namespace hs
