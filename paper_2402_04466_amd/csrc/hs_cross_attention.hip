@@ -40,10 +40,10 @@ template <class T, int DP, int QW, int KW, int BN>
 __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossGrid grid) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
-  constexpr int CH = DP / 8, KS = DP / 16, DT = DP / 32, NB = BN / 32;
+  constexpr int CH = DP > 64 ? 16 : 8, KS = DP / 16, DT = DP / 32, NB = BN / 32;   // CH: 16-byte pieces per row in LDS
   constexpr int NT = 64 * QW;                       // threads that fill a tile together
   constexpr int NL = BN * CH / NT;                  // 16-byte loads per thread for K, and for V
-  constexpr int kTile = BN * DP * 2;                // bytes
+  constexpr int kTile = BN * CH * 16;               // bytes
   constexpr int kBuffers = QW > 1 ? 2 : 1;          // a wave alone needs no second buffer: its accesses are in order
   constexpr int PT = DP + 4;                        // floats per row of a group's part: reads and writes spread over the banks
   constexpr int kTiles = KW * kBuffers * 2 * kTile, kParts = KW > 1 ? KW * QW * 32 * (PT + 2) * 4 : 0;
@@ -283,6 +283,21 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
     return;
   }
   if (!live) return;
+  if (grid.splits > 1) {
+    float* const part = p.parts + ((split * (int64_t)(p.batch * kv_heads) + bh) * rows + row) * (p.dim + 4);
+    if (half == 0) {
+      part[0] = m;
+      part[1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int d0 = 32 * d + 2 * e + 4 * half;
+        if (d0 < p.dim) *(f32x4*)(part + 4 + d0) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+      }
+    return;
+  }
   const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
   T* const dst = at_out<T>(p.out, b, token, head);
 #pragma unroll
@@ -340,7 +355,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
 
 namespace {
 struct CrossPlan {
-  int wide;                     // so many waves with 32 rows each, or
+  int wide;                     // so many waves with 32 rows each and the same keys, or
   int groups;                   // one set of 32 rows whose keys are dealt to so many waves
   CrossGrid grid;
   int64_t workgroups;
@@ -351,20 +366,39 @@ CrossPlan plan_of(const CrossParams& p) {
   // Eight waves share a tile of wide heads, four one of narrow ones: 2040 tokens of 16 heads on 8160 keys, 8 times, take
   // 1095 and 1180 us of 128 dimensions, 757 and 721 of 64.
   const int waves = p.dim > 64 ? 8 : 4, tile = 32 * waves;
+  const int64_t wide_tiles = (rows + tile - 1) / tile, wide = bh * wide_tiles, keys64 = ((int64_t)p.k_tokens + 63) / 64;
+  auto at_most = [](int64_t room, int64_t base, int64_t parts) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({room / std::max<int64_t>(base, 1), parts, kMostSplits}));
+  };
+  // Where those tiles are too few for the device their keys are cut into parts of eight tiles and more, if at least half of the
+  // rows are there and that fills most of it: 300 tokens on 3000 keys (18 heads of 64 in all) 33.4 us, by the form below 38.7;
+  // 500 on 1000 (8 of 64) 9.6 and 12.4; with parts of four tiles 1000 on 2000 (8 heads of 128) takes 29.9 and not 23.3.
+  const int cut = at_most(p.dim > 64 ? 256 : 512, wide, keys64 / 8);
   plan.groups = 0;
-  plan.wide = bh * ((rows + tile - 1) / tile) >= 256 ? waves : 0;
-  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? (rows + tile - 1) / tile : (rows + 31) / 32, INT32_MAX);
-  plan.grid.splits = 1;
+  plan.wide = wide >= 256 || (2 * rows >= wide_tiles * tile && wide * cut >= 192) ? waves : 0;
+  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? wide_tiles : (rows + 31) / 32, INT32_MAX);
+  plan.grid.splits = wide >= 256 ? 1 : cut;
   if (!plan.wide) {
-    // Keys over several workgroups where there are fewer than the device holds at once (two per CU of up to 64 dimensions,
-    // one of more) and at least four tiles per wave; a second launch then joins them.  One workgroup per row tile takes eight
-    // waves instead: 77 tokens on up to 1001 keys of 80 dimensions, 20 times (160 row tiles) 15.1 us, 17.6 in three parts.
+    // Else each wave takes keys of its own: eight of one workgroup, or four of several, joined by a second launch, which costs
+    // as much as three tiles more per wave (77 tokens on up to 1001 keys of 80 dimensions, 20 times: 14.6 us, 19.0 in three parts).
     const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, base = bh * plan.grid.row_tiles;
-    plan.grid.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(p.dim > 64 ? 256 : 512) / std::max<int64_t>(base, 1), tiles / 16, kMostSplits}));
-    plan.groups = plan.grid.splits == 1 ? 8 : 4;
+    const int splits = at_most(512, base, tiles / 16);
+    const bool apart = (tiles + 4 * splits - 1) / (4 * splits) + 3 < (base + 255) / 256 * ((tiles + 7) / 8);
+    plan.grid.splits = apart ? splits : 1;
+    plan.groups = apart ? 4 : 8;
   }
   plan.workgroups = bh * plan.grid.row_tiles * plan.grid.splits;
   return plan;
+}
+// Steps of 32 dimensions from 64 on: 77 tokens on 1001 keys of 80 take 14.6 us, 15.5 as 128.
+template <class T, int DP>
+const void* kernel_of(const CrossPlan& plan) {
+  if (plan.wide) return (const void*)k_cross<T, DP, (DP > 64 ? 8 : 4), 1, 64>;
+  return plan.groups == 8 ? (const void*)k_cross<T, DP, 1, 8, 32> : (const void*)k_cross<T, DP, 1, 4, 32>;
+}
+template <class T>
+const void* kernel_of(const CrossParams& p, const CrossPlan& plan) {
+  return p.dim <= 64 ? kernel_of<T, 64>(plan) : p.dim <= 96 ? kernel_of<T, 96>(plan) : kernel_of<T, 128>(plan);
 }
 }  // namespace
 
@@ -377,14 +411,8 @@ hipError_t launch(const CrossParams& p, hipStream_t stream) {
   CrossParams params = p;
   CrossPlan plan = plan_of(p);
   void* args[] = {&params, &plan.grid};
-  const bool narrow = p.dim <= 64, half = p.dtype == HS_F16;
-  const void* kernel;
-  if (plan.wide) kernel = half ? narrow ? (const void*)k_cross<f16, 64, 4, 1, 64> : (const void*)k_cross<f16, 128, 8, 1, 64>
-                               : narrow ? (const void*)k_cross<bf16, 64, 4, 1, 64> : (const void*)k_cross<bf16, 128, 8, 1, 64>;
-  else if (plan.groups == 8) kernel = half ? narrow ? (const void*)k_cross<f16, 64, 1, 8, 32> : (const void*)k_cross<f16, 128, 1, 8, 32>
-                                           : narrow ? (const void*)k_cross<bf16, 64, 1, 8, 32> : (const void*)k_cross<bf16, 128, 1, 8, 32>;
-  else kernel = half ? narrow ? (const void*)k_cross<f16, 64, 1, 4, 32> : (const void*)k_cross<f16, 128, 1, 4, 32>
-                     : narrow ? (const void*)k_cross<bf16, 64, 1, 4, 32> : (const void*)k_cross<bf16, 128, 1, 4, 32>;
+  const bool half = p.dtype == HS_F16;
+  const void* const kernel = half ? kernel_of<f16>(p, plan) : kernel_of<bf16>(p, plan);
   hipError_t e = launch_kernel(kernel, plan.workgroups, 64 * (plan.wide + plan.groups), args, stream);
   if (e != hipSuccess || plan.grid.splits == 1) return e;
   void* join_args[] = {&params, &plan.grid.splits};

@@ -560,3 +560,24 @@ def test_a_scale_of_zero_averages_whatever_the_scores(hs, ctx, gen):
     out, lse = torch.empty_like(q), torch.empty(b, h, nq, device=DEV)
     cross_call(hs, ctx, q, k, v, out, 0.0, lse=lse)
     cross_check(out, lse, torch.zeros_like(q), k, v, 0.0, torch.ones(b, nk, dtype=torch.bool, device=DEV), "zero")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("nq, group, d, masked", [(100, 1, 64, True), (70, 3, 96, False), (67, 3, 128, True)])
+def test_many_rows_whose_keys_are_cut(hs, ctx, gen, dtype, nq, group, d, masked):
+    """Whole row tiles, of the last of which rows are missing, on parts of the keys, of which short sequences fill few."""
+    t = TYPES[dtype]
+    b, nk, hk = 8, 2053, 8
+    q = normal(gen, b, nq, hk * group, d, dtype=t)
+    k, v = normal(gen, b, nk, hk, d, dtype=t), normal(gen, b, nk, hk, d, dtype=t)
+    lengths = torch.tensor([nk, 0, 1, 64, 65, 600, 2048, 2052], dtype=torch.int32, device=DEV)
+    seen = torch.arange(nk, device=DEV) < lengths[:, None]
+    mask = None
+    if masked:
+        mask = (torch.rand(b, nk, generator=gen, device=DEV) < 0.6).to(torch.uint8)
+        mask[0, 512:1100] = 0
+        seen &= mask != 0
+    k[~seen], v[~seen] = float("inf"), float("nan")
+    out, lse = torch.full_like(q, 7.0), torch.full((b, hk * group, nq), 7.0, device=DEV)
+    assert cross_call(hs, ctx, q, k, v, out, d ** -0.5, lengths, mask, lse).numel() > 0, "meant to be cut"
+    cross_check(out, lse, q, k, v, d ** -0.5, seen, "cut")
