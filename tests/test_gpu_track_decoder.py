@@ -1,0 +1,84 @@
+"""The track decoder's layer: a clip in one call, frame by frame, and from a graph, against the formulas in 64 bits."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def plain(dec, x, maps, mask):
+    """The layer on one stream's clip, in float64 on the host."""
+    f, t, h, d = x.shape[1], dec.tools, dec.heads, dec.head_dim
+    x, maps = x[0].double().cpu(), maps[0].double().cpu()
+    w = {n: getattr(dec, n).double().cpu() for n in ("w_qkv", "w_o", "w_q2", "w_kv", "w_o2", "w_norm", "frequencies")}
+
+    def norm(y, weight):
+        return y / (y.square().mean(-1, keepdim=True) + 1e-6).sqrt() * weight
+
+    def turn(y):
+        angle = torch.arange(f, dtype=torch.float64)[:, None, None, None] * w["frequencies"]
+        a, b = y[..., :d // 2], y[..., d // 2:]
+        return torch.cat((a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos()), -1)
+    q, k, v = (x @ w["w_qkv"]).view(f, t, 3, h, d).unbind(2)
+    q, k = turn(norm(q, w["w_norm"][0])), turn(norm(k, w["w_norm"][1]))
+    S, mixed = torch.zeros(t, h, d, d, dtype=torch.float64), []
+    decay = torch.tensor(dec.decay, dtype=torch.float64)[:, None, None]
+    for i in range(f):
+        S = decay * S + k[i][..., None] * v[i][..., None, :]
+        mixed.append((q[i][..., None, :] @ S).squeeze(-2) * d ** -0.5)
+    x = x + torch.stack(mixed).flatten(-2) @ w["w_o"]
+    q = norm((x @ w["w_q2"]).view(f, t, h, d), w["w_norm"][2])
+    k, v = (maps @ w["w_kv"]).view(f, -1, 2, h, d).unbind(2)
+    score = torch.einsum("fthd,fchd->fhtc", q, k) * d ** -0.5
+    if mask is not None:
+        score = score.masked_fill(mask[0].cpu()[:, None, None] == 0, -torch.inf)
+    looked = torch.einsum("fhtc,fchd->fthd", torch.softmax(score, -1), v)
+    return x + looked.flatten(-2) @ w["w_o2"], S
+
+
+@pytest.fixture(scope="module")
+def ctx(hs):
+    c = hs.hs_init(0)
+    yield c
+    hs.hs_shutdown(c)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_clip_frames_and_graph_follow_the_formulas(ctx, dtype):
+    from paper_2402_04466_amd.track_decoder import TrackDecoder
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    frames, cells, kw = 90, 135, dict(streams=1, heads=4, dtype=dtype)
+    clip, one = TrackDecoder(ctx, **kw), TrackDecoder(ctx, **kw)
+    x = torch.randn(1, frames, 8, clip.channels, generator=g, device="cuda:0").to(dtype)
+    maps = torch.randn(1, frames, cells, clip.channels, generator=g, device="cuda:0").to(dtype)
+    mask = (torch.rand(1, frames, cells, generator=g, device="cuda:0") < 0.7).to(torch.uint8)
+    # fourteen roundings to 16 bits on the way, each at most half a step of its values
+    bound = 14 * torch.finfo(dtype).eps / 2
+
+    def near(got, want):
+        assert (got.double().cpu() - want).norm() <= bound * want.norm()
+    want, S = plain(clip, x, maps, mask)
+    near(clip.forward(x, maps, mask)[0], want)
+    near(clip.state, S)
+    want, S = plain(one, x, maps, None)
+    eager = torch.cat([one.forward(x[:, i:i + 1], maps[:, i:i + 1]) for i in range(frames)], 1)
+    near(eager[0], want)
+    near(one.state, S)
+    assert one.frame.item() == frames
+    # several streams from a graph: every stream and every replay as the one alone
+    many = TrackDecoder(ctx, **{**kw, "streams": 3})
+    live = many.live(cells)
+    for i in range(frames):
+        live.x.copy_(x[:, i:i + 1].expand_as(live.x))
+        live.maps.copy_(maps[:, i:i + 1].expand_as(live.maps))
+        out = live.step()
+        if i % 29 == 0:
+            for s in range(3):
+                near(out[s, 0], want[i])
+    near(many.state.view(3, *S.shape)[2], S)
+
+
+def test_shapes_that_do_not_fit_are_refused(ctx):
+    from paper_2402_04466_amd.track_decoder import TrackDecoder
+    dec = TrackDecoder(ctx, streams=2, heads=1)
+    with pytest.raises(ValueError):
+        dec.forward(torch.zeros(2, 2, 8, 64, dtype=torch.float16, device="cuda:0"), None)
