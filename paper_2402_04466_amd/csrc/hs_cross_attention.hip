@@ -117,8 +117,8 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
     if (in_dim) {
 #pragma unroll
       for (int e = 0; e < NL; ++e) {
-        kreg[e] = *(const s16x8*)ka[e];
-        vreg[e] = *(const s16x8*)va[e];
+        kreg[e] = load16(ka[e]);
+        vreg[e] = load16(va[e]);
       }
     }
     if (mask) seen = mask[j0 + (lane & (BN - 1)) < n ? j0 + (lane & (BN - 1)) : (int64_t)n - 1];

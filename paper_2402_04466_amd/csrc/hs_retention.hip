@@ -260,13 +260,13 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
       if (in_k) {
 #pragma unroll
         for (int e = 0; e < NL; ++e) {
-          if (!kStates) to.q[e] = *(const s16x8*)qa[e];
-          to.k[e] = *(const s16x8*)ka[e];
+          if (!kStates) to.q[e] = load16(qa[e]);
+          to.k[e] = load16(ka[e]);
         }
       }
       if (in_v) {
 #pragma unroll
-        for (int e = 0; e < NV; ++e) to.v[e] = *(const s16x8*)va[e];
+        for (int e = 0; e < NV; ++e) to.v[e] = load16(va[e]);
       }
       qsrc += kChunk * p.q.token;
       ksrc += kChunk * p.k.token;

@@ -107,6 +107,12 @@ __device__ __forceinline__ T* at_out(const Heads& h, int64_t batch, int64_t toke
   return (T*)h.p + batch * h.batch + token * h.token + head * h.head;
 }
 
+// A 16-byte load that is known to be of global memory wherever its address comes from: one that might be of LDS (flat) is counted
+// with the LDS accesses, so that a wait for those waits for memory.
+__device__ __forceinline__ s16x8 load16(const void* from) {
+  return *(const __attribute__((address_space(1))) s16x8*)from;
+}
+
 // A sequence's length as the caller gives it, taken into its range.  `batch` is the same for the whole wave, and so, said
 // aloud, is the length: loops over it are the scalar unit's then.
 __device__ __forceinline__ int length_of(const int32_t* lengths, int batch, int longest) {
