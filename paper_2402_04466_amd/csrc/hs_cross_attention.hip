@@ -32,6 +32,18 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float positive_scale(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale); }
 
+// The order of the products before it and of the LDS reads that they take one each: two groups of reads, then each group's products
+// before the reads of the one after next, so that none waits for a read that has only just been issued.
+template <int GROUP, int GROUPS>
+__device__ __forceinline__ void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, 2 * GROUP, 0);
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) {
+    __builtin_amdgcn_sched_group_barrier(0x8, GROUP, 0);
+    if (g + 2 < GROUPS) __builtin_amdgcn_sched_group_barrier(0x100, GROUP, 0);
+  }
+}
+
 struct CrossGrid {
   int row_tiles, splits;
 };
@@ -172,6 +184,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
 #pragma unroll
       for (int k = 0; k < KS; ++k) s[kb] = mfma32(*(const x8*)(here + koff[k] + kb * 32 * CH * 16), q[k], s[kb]);
     }
+    if (QW > 1) reads_ahead<KS / 2, 2 * NB>();      // (2040 tokens on 8160 keys 1070 us, 1084 without)
     if (visible != kAll) {
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb) {
