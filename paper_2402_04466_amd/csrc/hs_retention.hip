@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 // i, j = 0 .. c - 1:
 //   A_ij = scale * decay^(i - j) q_i k_j (j <= i)          out_i = sum_j A_ij v_j + scale * decay^(i + 1) S^T q_i
 //   S   <- decay^c S + sum_j k_j (decay^(c - 1 - j) v_j)^T
-// A workgroup has one sequence and head and 64 of the values' dimensions, and waves of three kinds, one of each per SIMD:
+// A workgroup has one sequence and head and 48 or 64 of the values' dimensions, and waves of three kinds, one of each per SIMD:
 //   waves 0 .. 3 carry the state, 16 of the dimensions each, in their accumulators, and leave a 16-bit copy of it in LDS
 //   for the next chunk;
 //   waves 4 .. 7 load: a chunk that is two ahead is on its way from memory into their registers while the next one goes
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 //   waves 8 .. 11 form out, 16 of the chunk's rows each: A by K Q^T, so that a lane holds four keys of one row per tile
 //   and A is the operand of the next product where it lies, if that one takes V's rows in the same order.
 // One barrier a chunk.  The chain of LDS reads and products from barrier to barrier bounds it: with eight waves that shared the
-// loads, 10 chunks of 64 sequences took 19.9 us (now 15.5), ragged clips of 96 x 80 38.7 (29.3), 113 chunks of 128 x 128 in 256
+// loads, 10 chunks of 64 sequences took 19.9 us (now 15.5), ragged clips of 96 x 80 38.7 (26.7), 113 chunks of 128 x 128 in 256
 // workgroups 280 (270: 3.6 TB/s, where the loads alone take 168).  The waves that form out are the longest, and go first.
 //
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
@@ -97,20 +97,21 @@ constexpr int kChunk = 64;
 // Few sequences and heads: their chunks are cut into segments, a workgroup for each.  A first launch (kStates) finds what
 // every segment but the last adds to a state of zeros, a second one (k_retain_starts) puts together by the decays of whole
 // segments what each starts from, and the third goes on from there as above.
-template <class T, int KP, bool kStates>
+template <class T, int KP, int DT, bool kStates>
 __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(RetentionParams p, int segments) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
-  constexpr int CH = KP / 8, KT = KP / 16, KS = KP / 32;   // KT: 16-wide tiles of key dimensions, KS: steps of 32
+  constexpr int CH = KP > 64 ? 16 : 8, KT = KP / 16, KS = KP / 32;   // CH: 16-byte pieces per row in LDS; KT: 16-wide tiles of key dimensions, KS: steps of 32
+  constexpr int kWide = 16 * DT;                    // of the values' dimensions
   constexpr int RP = 256 / CH, NL = kChunk / RP, NV = 2;   // rows per pass of the waves that load over Q or K, passes over them and V
   constexpr bool kHalf = __is_same(T, f16);
   constexpr int kParts = kHalf ? 2 : 3, kVTile = kChunk * 64 * 2;
-  constexpr int kK = kChunk * KP * 2, kV = 2 * kK, kP = kV + kVTile, kSlot = kP + kParts * kVTile;   // Q, K, V of a chunk, V's decayed parts
-  constexpr int kS = 2 * kSlot, kCopy = 64 * KP * 2;
+  constexpr int kK = kChunk * CH * 16, kV = 2 * kK, kP = kV + kVTile, kSlot = kP + kParts * kVTile;   // Q, K, V of a chunk, V's decayed parts
+  constexpr int kS = 2 * kSlot, kCopy = kWide * CH * 16;
   __shared__ __align__(16) char lds[kS + 2 * kCopy];
   __shared__ int exponents[kHalf ? 2 : 1][kHalf ? 4 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w4 = wave & 3, l16 = lane & 15, g = lane >> 4;
-  const int blocks = (p.value_dim + 63) / 64;
+  const int blocks = (p.value_dim + kWide - 1) / kWide;
   int id = xcd_number();
   const int block = id % blocks;
   id /= blocks;
@@ -128,9 +129,11 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
   const float power = (float)power64;
   auto power_of = [&](int steps) { return __shfl(power, steps); };
 
-  if (wave < 4) {
+  if (wave < 4 && w4 >= DT) {
+    for (int c = -1; c < chunks; ++c) __syncthreads();
+  } else if (wave < 4) {
     // ---- the state: lane has dimension dv, key dimensions 16 t + 4 g + i
-    const int dv = 64 * block + 16 * w4 + l16;
+    const int dv = kWide * block + 16 * w4 + l16;
     const int64_t state0 = (int64_t)bh * p.key_dim * p.value_dim + dv;
     const int64_t states = (int64_t)p.batch * p.q_heads * p.key_dim * p.value_dim;
     const float* const from = kStates ? nullptr : segment ? p.parts + (segment - 1) * states : p.state_in;
@@ -231,10 +234,10 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
     // ---- loads: this thread's 16-byte pieces of rows r0, r0 + RP, ... of Q and K, and of two rows of V (8 pieces).  Rows behind
     // the last token are read as that one and emptied on their way into LDS.
     const int tid = threadIdx.x & 255, r0 = tid / CH, ch = tid % CH, vr = tid / 8, vch = tid % 8;
-    const bool in_k = 8 * ch < p.key_dim, in_v = 64 * block + 8 * vch < p.value_dim;
+    const bool in_k = 8 * ch < p.key_dim, in_v = vch < 2 * DT && kWide * block + 8 * vch < p.value_dim;
     const T* qsrc = at<T>(p.q, b, (int64_t)first * kChunk + r0, h) + 8 * ch;   // of the chunk that is fetched next
     const T* ksrc = at<T>(p.k, b, (int64_t)first * kChunk + r0, hk) + 8 * ch;
-    const T* vsrc = at<T>(p.v, b, (int64_t)first * kChunk + vr, hk) + 64 * block + 8 * vch;
+    const T* vsrc = at<T>(p.v, b, (int64_t)first * kChunk + vr, hk) + kWide * block + 8 * vch;
     struct Pieces { s16x8 q[NL], k[NL], v[NV]; } even = {}, odd = {};          // of chunks on their way
     auto fetch = [&](int c, Pieces& to) {           // chunk c, after the ones before it
       if (c >= chunks) return;
@@ -330,7 +333,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
       __syncthreads();
     }
     if (!kStates && last && in_v)
-      for (int64_t t = (int64_t)n + vr; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + 64 * block + 8 * vch) = s16x8{};
+      for (int64_t t = (int64_t)n + vr; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + kWide * block + 8 * vch) = s16x8{};
   } else if (!kStates) {
     // ---- out: rows 16 w4 .. + 15 of the chunk, lane has row 16 w4 + l16
     __builtin_amdgcn_s_setprio(1);
@@ -354,10 +357,10 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
         x8 q[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *(const x8*)(here + 16 * W * CH * 16 + slot<CH>(l16, 4 * s + g));
-        f32x4 o[4];
+        f32x4 o[DT];
         auto from_state = [&]() {
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
+          for (int d = 0; d < DT; ++d) {
             o[d] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int s = 0; s < KS; ++s) o[d] = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], o[d]);
@@ -388,14 +391,14 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
 #pragma unroll
         for (int j = 0; j <= W / 2; ++j)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
+          for (int d = 0; d < DT; ++d) {
             const char* const from = here + kV + 32 * j * 128 + low8;
             const int cc = 2 * d + (lane >> 1 & 1);
             o[d] = mfma16(join8<T>(read_transposed(from + slot<8>(vrow, cc)), read_transposed(from + 16 * 128 + slot<8>(vrow, cc))), a[j], o[d]);
           }
         float finite = 0.0f;                        // zero, or NaN
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i) finite = fmaf(o[d][i], 0.0f, finite);
         if (__any(finite != 0.0f)) {
@@ -413,7 +416,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
                 const float x = __shfl(t[i], 16 * from + l16) * (p.scale * power_of(max(apart, 0)));
                 if (apart < 0) continue;
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
+                for (int d = 0; d < DT; ++d) {
                   const x4 v = *(const x4*)(here + kV + slot<8>(key, 2 * d + (g >> 1)) + (g & 1) * 8);
 #pragma unroll
                   for (int e = 0; e < 4; ++e) o[d][e] = fmaf(x, (float)v[e], o[d][e]);
@@ -423,10 +426,10 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
         }
         const int64_t t = (int64_t)(first + c) * kChunk + 16 * W + l16;
         if (t < n) {
-          T* const to = at_out<T>(p.out, b, t, h) + 64 * block + 4 * g;
+          T* const to = at_out<T>(p.out, b, t, h) + kWide * block + 4 * g;
 #pragma unroll
-          for (int d = 0; d < 4; ++d)
-            if (64 * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = round4<T>(o[d]);
+          for (int d = 0; d < DT; ++d)
+            if (kWide * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = round4<T>(o[d]);
         }
         __syncthreads();
       }
@@ -480,10 +483,18 @@ RetentionPlan plan_of(const RetentionParams& p) {
   return plan;
 }
 
+// Key dimensions in steps of 32 from 64 on, the values' in workgroups of 48 or 64 each, whichever leaves less over: ragged clips of
+// 96 x 80 take 26.7 us, 29.5 as 128 x 128; 500 tokens of 80 x 40, 160 times, 15.2 and 18.1.
+template <class T, int KP>
+const void* chunks_kernel(int value_dim, bool states) {
+  const int blocks = (value_dim + 63) / 64;
+  return value_dim > 48 * blocks ? states ? (const void*)k_retain_chunks<T, KP, 4, true> : (const void*)k_retain_chunks<T, KP, 4, false>
+                                 : states ? (const void*)k_retain_chunks<T, KP, 3, true> : (const void*)k_retain_chunks<T, KP, 3, false>;
+}
 template <class T>
-const void* chunks_kernel(bool wide, bool states) {
-  return wide ? states ? (const void*)k_retain_chunks<T, 128, true> : (const void*)k_retain_chunks<T, 128, false>
-              : states ? (const void*)k_retain_chunks<T, 64, true> : (const void*)k_retain_chunks<T, 64, false>;
+const void* chunks_kernel(const RetentionParams& p, bool states) {
+  return p.key_dim <= 64 ? chunks_kernel<T, 64>(p.value_dim, states)
+                         : p.key_dim <= 96 ? chunks_kernel<T, 96>(p.value_dim, states) : chunks_kernel<T, 128>(p.value_dim, states);
 }
 }  // namespace
 
@@ -503,12 +514,12 @@ hipError_t launch(const RetentionParams& p, hipStream_t stream) {
     return launch_kernel(kernel, plan.workgroups, 256, args, stream);
   }
   if (plan.segments > 1) {
-    const hipError_t e = launch_kernel(half ? chunks_kernel<f16>(wide, true) : chunks_kernel<bf16>(wide, true), plan.workgroups * (plan.segments - 1), 512, args, stream);
+    const hipError_t e = launch_kernel(half ? chunks_kernel<f16>(p, true) : chunks_kernel<bf16>(p, true), plan.workgroups * (plan.segments - 1), 512, args, stream);
     if (e != hipSuccess) return e;
     const hipError_t joined = launch_kernel((const void*)k_retain_starts, ((int64_t)p.batch * p.q_heads * p.key_dim * p.value_dim / 4 + 255) / 256, 256, args, stream);
     if (joined != hipSuccess) return joined;
   }
-  return launch_kernel(half ? chunks_kernel<f16>(wide, false) : chunks_kernel<bf16>(wide, false), plan.workgroups * plan.segments, 768, args, stream);
+  return launch_kernel(half ? chunks_kernel<f16>(p, false) : chunks_kernel<bf16>(p, false), plan.workgroups * plan.segments, 768, args, stream);
 }
 
 }  // namespace hs
