@@ -491,8 +491,8 @@ hs_status hs_partition_copy(hs_app* app, void* d_dst, const void* d_src, size_t 
  * heads: query head h uses key and value head h / (q_heads / kv_heads).  dims are multiples of 8,
  * 8..128; pointers 16-byte aligned and strides multiples of 8 elements, both where more than
  * nothing is read.  Strides of inputs may be 0 (one tensor for all) or negative; an output's rows
- * must not overlap.  Offsets are 64-bit.  Sums, norms, softmax statistics and states are fp32; every
- * output is rounded once. */
+ * must not overlap, and but for the cases named below no output overlaps an input.  Offsets are
+ * 64-bit.  Sums, norms, softmax statistics and states are fp32; every output is rounded once. */
 typedef enum { HS_F16 = 1, HS_BF16 = 2 } hs_dtype;
 typedef struct {
   void* d;                      /* first value of batch 0, token 0, head 0 (inputs are only read)  */
@@ -533,6 +533,7 @@ hs_status hs_norm_rotate(hs_ctx* ctx, const hs_norm_rotate_desc* desc, void* hip
  * out is zero for the tokens behind it, whose q, k and v are not used whatever they hold.
  * One call serves a whole clip (tokens = its frames) or one frame of every live stream
  * (tokens = 1); a clip cut into calls gives the same results up to the order of fp32 sums.
+ * An infinity or NaN in a token reaches later tokens and the state as the formula has it, and no earlier token.
  * state_in may be NULL (zeros) or be state_out itself; tokens = 0 copies the state. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k, v, out                                        */

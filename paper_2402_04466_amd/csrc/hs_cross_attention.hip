@@ -354,7 +354,6 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
   f32x4 sum = {0, 0, 0, 0};
-#pragma unroll 4
   for (int s = 0; s < splits; s += 2) {
     const float w = __shfl(f, s + half);            // (of a part that is not there, or saw no key: 0)
     if (d0 < p.dim && w != 0.0f) sum += w * *(const f32x4*)(parts + (s + half) * all * pitch + 4 + d0);

@@ -171,3 +171,10 @@ def test_workspace_queries_need_no_pointers_and_refuse_what_the_calls_refuse():
 def test_binding_refuses_a_decay_of_another_length():
     with pytest.raises(ValueError):
         retention(decay=[0.9] * 7)
+
+
+def test_counts_beyond_one_call_are_refused():
+    """Products of two counts that would not fit the kernels' numbers."""
+    far = heads(batch=1 << 40, token=1 << 20, head=64)
+    refused("hs_norm_rotate", norm_rotate(batch=1 << 16, tokens=1 << 16, q=far, k=far, q_out=far, k_out=far), "too many tokens")
+    refused("hs_cross_attention", cross(batch=1 << 20, q_heads=1 << 14, kv_heads=1), "too many heads")
