@@ -7,7 +7,7 @@ namespace hs {
 
 // y = x * rsqrt(mean(x^2) + eps) * w; pairs (a, b) of the first `rotary` values turned by t = position * frequency.
 //
-// Bound by reading and writing every value once.  A head is held by LANES = 2, 4, 8 or 16 lanes with 8 values (16
+// Bound by reading and writing every value once (345600 tokens of 16 heads of 64: 263 us, 5.4 TB/s).  A head is held by LANES = 2, 4, 8 or 16 lanes with 8 values (16
 // bytes) each; a group of LANES lanes takes one token and some of its heads, four at a time, so that the token's
 // sines and cosines, folded into the weights (own value times A plus partner's times B), are formed once and stay in
 // registers, behind the loads of the first four heads.  The partner's values come from the lane that has them (half layout)

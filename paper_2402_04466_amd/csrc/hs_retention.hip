@@ -9,7 +9,7 @@ namespace hs {
 // Recurrent form: S = decay * S + k v^T, out = scale * q S, token by token.  A workgroup holds key_dim x 64 values of
 // one sequence's and head's state in registers: 16 lanes side by side have 4 values of 16 bytes each, so a row of
 // the state is read in 256-byte pieces, and thread group g of 16 has ROWS rows from ROWS * g on.  Bound by reading and
-// writing the state (5.2 TB/s at 128 tracks of 16 heads of 128 x 128); for few tracks by the chain of loads, so the first token's
+// writing the state (5.6 TB/s at 128 tracks of 16 heads of 128 x 128); for few tracks by the chain of loads, so the first token's
 // are issued beside the state's and the length's, and each further token's beside the sums of the one before.
 template <class T, int ROWS>
 __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
