@@ -136,7 +136,8 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
     const int dv = kWide * block + 16 * w4 + l16;
     const int64_t state0 = (int64_t)bh * p.key_dim * p.value_dim + dv;
     const int64_t states = (int64_t)p.batch * p.q_heads * p.key_dim * p.value_dim;
-    const float* const from = kStates ? nullptr : segment ? p.parts + (segment - 1) * states : p.state_in;
+    // (the first segment's, where the last one may have written over it already: as k_retain_starts has kept it)
+    const float* const from = kStates ? nullptr : segment ? p.parts + (segment - 1) * states : segments > 1 && p.state_in == p.state_out ? p.parts + (segments - 1) * states : p.state_in;
     f32x4 S[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t)
@@ -443,7 +444,8 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
   }
 }
 
-// parts[s], s < segments - 1: what segment s adds, replaced by the state behind it.  Four values per thread.
+// parts[s], s < segments - 1: what segment s adds, replaced by the state behind it.  A state that is replaced in place is kept behind
+// them, since the workgroups of one launch may end before others begin.  Four values per thread.
 __global__ __launch_bounds__(256) void k_retain_starts(RetentionParams p, int segments) {
   const int64_t size = (int64_t)p.key_dim * p.value_dim, states = (int64_t)p.batch * p.q_heads * size;
   const int64_t at_value = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
@@ -456,6 +458,7 @@ __global__ __launch_bounds__(256) void k_retain_starts(RetentionParams p, int se
   f32x4 S = {0, 0, 0, 0};
   if (p.state_in) S = *(const f32x4*)(p.state_in + at_value);
   float* part = p.parts + at_value;
+  if (p.state_in == p.state_out) *(f32x4*)(part + (segments - 1) * states) = S;
 #pragma unroll 4
   for (int s = 0; s < used; ++s, part += states) {
     const f32x4 add = *(const f32x4*)part;
@@ -500,7 +503,7 @@ const void* chunks_kernel(const RetentionParams& p, bool states) {
 
 size_t retention_workspace(const RetentionParams& p) {
   const RetentionPlan plan = plan_of(p);
-  return (size_t)(plan.segments - 1) * p.batch * p.q_heads * p.key_dim * p.value_dim * sizeof(float);
+  return plan.segments == 1 ? 0 : (size_t)plan.segments * p.batch * p.q_heads * p.key_dim * p.value_dim * sizeof(float);
 }
 
 hipError_t launch(const RetentionParams& p, hipStream_t stream) {

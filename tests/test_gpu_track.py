@@ -581,3 +581,20 @@ def test_many_rows_whose_keys_are_cut(hs, ctx, gen, dtype, nq, group, d, masked)
     out, lse = torch.full_like(q, 7.0), torch.full((b, hk * group, nq), 7.0, device=DEV)
     assert cross_call(hs, ctx, q, k, v, out, d ** -0.5, lengths, mask, lse).numel() > 0, "meant to be cut"
     cross_check(out, lse, q, k, v, d ** -0.5, seen, "cut")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_cut_sequences_take_their_state_in_place(hs, ctx, gen, dtype):
+    """Segments of a sequence run side by side, and the last one's state goes where the first one's came from."""
+    t = TYPES[dtype]
+    b, n, h, d = 2, 2000, 3, 64
+    q, k, v, state, decay = retention_inputs(gen, b, n, h, h, d, d, t)
+    lengths = torch.tensor([n, 40], dtype=torch.int32, device=DEV)
+    out, end = torch.empty(b, n, h, d, dtype=t, device=DEV), torch.empty_like(state)
+    work = retention_call(hs, ctx, q, k, v, out, state, end, decay, 0.125, lengths)
+    assert work.numel() >= 2 * state.numel() * 4, "meant to be cut, with room for the state itself"
+    again, keep = torch.empty_like(out), state.clone()
+    retention_call(hs, ctx, q, k, v, again, keep, keep, decay, 0.125, lengths)
+    assert torch.equal(again, out) and torch.equal(keep, end)
+    ref = retention_reference(q, k, v, state, decay, 0.125, lengths)
+    retention_check(out, end, ref, t, n, "in place")
