@@ -391,15 +391,18 @@ CrossPlan plan_of(const CrossParams& p) {
   // 500 on 1000 (8 of 64) 9.6 and 12.4; with parts of four tiles 1000 on 2000 (8 heads of 128) takes 29.9 and not 23.3.
   const int cut = at_most(p.dim > 64 ? 256 : 512, wide, keys64 / 8);
   plan.groups = 0;
-  plan.wide = wide >= 256 || (2 * rows >= wide_tiles * tile && wide * cut >= 192) ? waves : 0;
+  // And where the form below would need several rounds of workgroups for so few keys that most of its waves had none: 1755 tokens on
+  // 5 keys (12 heads of 72) 7.6 us, 17.9; 113 on 4 (13 times, 6 heads of 96) 7.9, 12.3; 660 on 5 (3 times, 12 heads of 64) 7.3, 6.6.
+  const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, few = bh * ((rows + 31) / 32);
+  const bool short_keys = 2 * ((wide + 255) / 256) * keys64 < (few + 255) / 256 * ((tiles + 7) / 8 + 1);
+  plan.wide = wide >= 256 || (2 * rows >= wide_tiles * tile && wide * cut >= 192) || short_keys ? waves : 0;
   plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? wide_tiles : (rows + 31) / 32, INT32_MAX);
   plan.grid.splits = wide >= 256 ? 1 : cut;
   if (!plan.wide) {
     // Else each wave takes keys of its own: eight of one workgroup, or four of several, joined by a second launch, which costs
     // as much as three tiles more per wave (77 tokens on up to 1001 keys of 80 dimensions, 20 times: 14.6 us, 19.0 in three parts).
-    const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, base = bh * plan.grid.row_tiles;
-    const int splits = at_most(512, base, tiles / 16);
-    const bool apart = (tiles + 4 * splits - 1) / (4 * splits) + 3 < (base + 255) / 256 * ((tiles + 7) / 8);
+    const int splits = at_most(512, few, tiles / 16);
+    const bool apart = (tiles + 4 * splits - 1) / (4 * splits) + 3 < (few + 255) / 256 * ((tiles + 7) / 8);
     plan.grid.splits = apart ? splits : 1;
     plan.groups = apart ? 4 : 8;
   }
