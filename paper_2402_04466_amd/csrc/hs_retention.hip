@@ -91,7 +91,8 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
 // is then half a step off, as out itself); of the fp16 copy a power of two is taken out, so that it stays in
 // that type's range whatever the state has grown to.  The state takes no such rounding: decayed values enter as a sum of
-// three bf16 or two fp16 parts (the second scaled by 2^12, out of fp16's subnormal numbers).
+// three bf16 or two fp16 parts.  The second of these is scaled by 2^11, out of fp16's subnormal numbers and no further: what a first
+// part leaves is up to 16, of values from 32768 on.  So two parts keep 22 bits of what is above 2^-14, and 2^-36 of the rest.
 constexpr int kChunk = 64;
 
 // Few sequences and heads: their chunks are cut into segments, a workgroup for each.  A first launch (kStates) finds what
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
             S[t] = mfma16(k, part[s][2], S[t]);
           }
         }
-        if (kHalf) S[t] += low * (1.0f / 4096.0f);
+        if (kHalf) S[t] += low * (1.0f / 2048.0f);
         if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (reads further ahead would not fit the registers)
       }
       if (!kStates && c + 1 < chunks) leave_copy(~c & 1);
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
           const x8 part = round8<T>(x);
           *(x8*)(to + kP + e * kVTile + at_v) = part;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = (x[i] - (float)part[i]) * (kHalf ? 4096.0f : 1.0f);
+          for (int i = 0; i < 8; ++i) x[i] = (x[i] - (float)part[i]) * (kHalf ? 2048.0f : 1.0f);
         }
       }
     };

@@ -598,3 +598,23 @@ def test_cut_sequences_take_their_state_in_place(hs, ctx, gen, dtype):
     assert torch.equal(again, out) and torch.equal(keep, end)
     ref = retention_reference(q, k, v, state, decay, 0.125, lengths)
     retention_check(out, end, ref, t, n, "in place")
+
+
+# ---- retention: magnitudes ------------------------------------------------------------------------------
+def retention_of(hs, ctx, q, k, v, state, decay, scale, what, lengths=None):
+    ref = retention_reference(q, k, v, state, decay, scale, lengths)
+    assert ref[0].abs().max() < 60000, "meant to be in range"
+    out = torch.full_like(ref[0], 7.0, dtype=q.dtype)
+    end = torch.full_like(ref[1], 7.0, dtype=torch.float32)
+    retention_call(hs, ctx, q, k, v, out, state, end, decay, scale, lengths)
+    retention_check(out, end, ref, q.dtype, q.shape[1], what)
+
+
+@pytest.mark.parametrize("n", [9, 64, 150, 2600])
+def test_values_near_the_end_of_fp16_do_not_leave_its_range(hs, ctx, gen, n):
+    """Decayed values of 32768 and more: what their first 16-bit part leaves is up to 16, and exactly 16 in one place."""
+    b, h, d, t = 2, 3, 64, torch.float16
+    q, k, v, state, _ = retention_inputs(gen, b, n, h, h, d, d, t)
+    v = (33000 + 32504 * torch.rand(v.shape, generator=gen, device=DEV)).copysign(v).to(t)
+    v[0, min(n, 64) - 2, 1, ::5] = 43712.0             # 0.75 of it: 32784, halfway between two fp16 numbers
+    retention_of(hs, ctx, q * 0.01, k * 0.01, v, state, [1.0, 0.75, 0.99], 0.125, "large values")
