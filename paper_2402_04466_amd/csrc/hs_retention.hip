@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 
 // Chunked form: 64 tokens at a time, products on the matrix pipe.  With c tokens in a chunk, S the state before it and
 // i, j = 0 .. c - 1:
-//   A_ij = scale * decay^(i - j) q_i k_j (j <= i)          out_i = sum_j A_ij v_j + scale * decay^(i + 1) S^T q_i
+//   A_ij = decay^(i - j) q_i k_j (j <= i)                  out_i = scale * (sum_j A_ij v_j + decay^(i + 1) S^T q_i)
 //   S   <- decay^c S + sum_j k_j (decay^(c - 1 - j) v_j)^T
 // A workgroup has one sequence and head and 48 or 64 of the values' dimensions, and waves of three kinds, one of each per SIMD:
 //   waves 0 .. 3 carry the state, 16 of the dimensions each, in their accumulators, and leave a 16-bit copy of it in LDS
@@ -89,8 +89,9 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 // workgroups 280 (270: 3.6 TB/s, where the loads alone take 168).  The waves that form out are the longest, and go first.
 //
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
-// is then half a step off, as out itself); of the fp16 copy a power of two is taken out, so that it stays in
-// that type's range whatever the state has grown to.  The state takes no such rounding: decayed values enter as a sum of
+// is then half a step off, as out itself).  In fp16 a power of two is taken out of each row of A, so that its largest is below 2^15
+// and those of up to 2^-29 of that keep all their bits, and one out of the copy, so that it stays in that type's range
+// whatever the state has grown to.  The state takes no such rounding: decayed values enter as a sum of
 // three bf16 or two fp16 parts.  The second of these is scaled by 2^11, out of fp16's subnormal numbers and no further: what a first
 // part leaves is up to 16, of values from 32768 on.  So two parts keep 22 bits of what is above 2^-14, and 2^-36 of the rest.
 constexpr int kChunk = 64;
@@ -348,10 +349,10 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int apart = 16 * (W - cb) + l16 - 4 * g - i;
-          const float x = p.scale * power_of(max(apart, 0));
+          const float x = power_of(max(apart, 0));
           decay[cb][i] = apart < 0 ? 0.0f : x;
         }
-      const float after = p.scale * (power_of(16 * W + l16) * p.decay[h]);
+      const float after = power_of(16 * W + l16) * p.decay[h];
       __syncthreads();
       for (int c = 0; c < chunks; ++c) {
         const char* const here = lds + (c & 1) * kSlot;
@@ -359,14 +360,14 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
         x8 q[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *(const x8*)(here + 16 * W * CH * 16 + slot<CH>(l16, 4 * s + g));
-        f32x4 o[DT];
-        auto from_state = [&]() {
+        f32x4 o[DT] = {};
+        auto add_from_state = [&]() {
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
-            o[d] = f32x4{0, 0, 0, 0};
+            f32x4 t = {0, 0, 0, 0};
 #pragma unroll
-            for (int s = 0; s < KS; ++s) o[d] = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], o[d]);
-            o[d] *= kHalf ? ldexpf(after, exponents[c & 1][d]) : after;
+            for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
+            o[d] += t * (kHalf ? ldexpf(after, exponents[c & 1][d]) : after);
           }
         };
         auto scores = [&](int cb) {
@@ -375,21 +376,32 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
           for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(here + kK + 16 * cb * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
           return t;
         };
-        x8 a[W / 2 + 1];                            // 32 keys each
+        float x[W / 2 + 1][8] = {};                 // A, 32 keys each
 #pragma unroll
-        for (int j = 0; j <= W / 2; ++j) {
-          float x[8] = {};
+        for (int cb = 0; cb <= W; ++cb) {
+          const f32x4 t = scores(cb);
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (2 * j + e <= W) {
-              const f32x4 t = scores(2 * j + e);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) x[4 * e + i] = t[i] * decay[2 * j + e][i];
-            }
-          a[j] = round8<T>(x);
+          for (int i = 0; i < 4; ++i) x[cb / 2][cb % 2 * 4 + i] = t[i] * decay[cb][i];
         }
+        float up = 1.0f;                            // the power of two that is out of this lane's row
+        if (kHalf) {
+          float most = 0.0f;
+#pragma unroll
+          for (int cb = 0; cb <= W; ++cb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(x[cb / 2][cb % 2 * 4 + i]));
+          const int exponent = max(__builtin_amdgcn_frexp_expf(column_max(most)) - 15, -100);
+          const float down = ldexpf(1.0f, -exponent);
+          up = ldexpf(1.0f, exponent);
+#pragma unroll
+          for (int cb = 0; cb <= W; ++cb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[cb / 2][cb % 2 * 4 + i] *= down;
+        }
+        x8 a[W / 2 + 1];
+#pragma unroll
+        for (int j = 0; j <= W / 2; ++j) a[j] = round8<T>(x[j]);
         __builtin_amdgcn_sched_barrier(0);          // (as above)
-        from_state();
 #pragma unroll
         for (int j = 0; j <= W / 2; ++j)
 #pragma unroll
@@ -398,15 +410,21 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
             const int cc = 2 * d + (lane >> 1 & 1);
             o[d] = mfma16(join8<T>(read_transposed(from + slot<8>(vrow, cc)), read_transposed(from + 16 * 128 + slot<8>(vrow, cc))), a[j], o[d]);
           }
+        if (kHalf) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[d] *= up;
+        }
+        add_from_state();
         float finite = 0.0f;                        // zero, or NaN
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i) finite = fmaf(o[d][i], 0.0f, finite);
         if (__any(finite != 0.0f)) {
-          // A product beyond fp16's range, or an input that is not finite, which must not reach earlier tokens through their
+          // A product beyond fp32's range, or an input that is not finite, which must not reach earlier tokens through their
           // zeros in A: term by term, in fp32.
-          from_state();
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[d] = f32x4{0, 0, 0, 0};
 #pragma unroll 1
           for (int cb = 0; cb <= W; ++cb) {
             const f32x4 t = scores(cb);
@@ -415,7 +433,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
 #pragma unroll 1
               for (int from = 0; from < 4; ++from) {
                 const int key = 16 * cb + 4 * from + i, apart = 16 * W + l16 - key;
-                const float x = __shfl(t[i], 16 * from + l16) * (p.scale * power_of(max(apart, 0)));
+                const float x = __shfl(t[i], 16 * from + l16) * power_of(max(apart, 0));
                 if (apart < 0) continue;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
@@ -425,13 +443,14 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
                 }
               }
           }
+          add_from_state();
         }
         const int64_t t = (int64_t)(first + c) * kChunk + 16 * W + l16;
         if (t < n) {
           T* const to = at_out<T>(p.out, b, t, h) + kWide * block + 4 * g;
 #pragma unroll
           for (int d = 0; d < DT; ++d)
-            if (kWide * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = round4<T>(o[d]);
+            if (kWide * block + 16 * d + 4 * g < p.value_dim) *(x4*)(to + 16 * d) = round4<T>(p.scale * o[d]);
         }
         __syncthreads();
       }

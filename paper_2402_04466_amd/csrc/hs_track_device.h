@@ -78,6 +78,17 @@ __device__ __forceinline__ void both_halves(float x, float& lower, float& upper)
   upper = __builtin_bit_cast(float, r1);
 }
 
+// The largest of lanes l, l ^ 16, l ^ 32 and l ^ 48 (NaN is left out), in each of them.
+__device__ __forceinline__ float column_max(float x) {
+  const unsigned bits = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+  const unsigned r0 = r[0], r1 = r[1];
+  x = fmaxf(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
+  float lower, upper;
+  both_halves(x, lower, upper);
+  return fmaxf(lower, upper);
+}
+
 // The largest of a wave's values (NaN is left out), in all lanes: rows of 16 by neighbours, pairs and mirrored halves, then
 // pairs of rows and the wave's halves.
 template <int CONTROL>
@@ -89,13 +100,7 @@ __device__ __forceinline__ float wave_max(float x) {
   x = fmaxf(x, moved<0x4e>(x));                     // lane ^ 2
   x = fmaxf(x, moved<0x141>(x));                    // 7 - lane
   x = fmaxf(x, moved<0x140>(x));                    // 15 - lane
-  const unsigned bits = __builtin_bit_cast(unsigned, x);
-  const auto r = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
-  const unsigned r0 = r[0], r1 = r[1];
-  x = fmaxf(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
-  float lower, upper;
-  both_halves(x, lower, upper);
-  return fmaxf(lower, upper);
+  return column_max(x);
 }
 
 template <class T>

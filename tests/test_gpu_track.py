@@ -618,3 +618,14 @@ def test_values_near_the_end_of_fp16_do_not_leave_its_range(hs, ctx, gen, n):
     v = (33000 + 32504 * torch.rand(v.shape, generator=gen, device=DEV)).copysign(v).to(t)
     v[0, min(n, 64) - 2, 1, ::5] = 43712.0             # 0.75 of it: 32784, halfway between two fp16 numbers
     retention_of(hs, ctx, q * 0.01, k * 0.01, v, state, [1.0, 0.75, 0.99], 0.125, "large values")
+
+
+@pytest.mark.parametrize("n", [9, 64, 150, 1100])
+@pytest.mark.parametrize("qk, value, scale", [(2.0 ** -8, 256, 0.125), (2.0 ** -10, 256, 0.125), (2.0 ** -11, 4096, 0.125), (1, 256, 1e-6),
+                                              (100, 1, 1e-7), (2.0 ** -6, 1, 1000.0)])
+def test_small_products_of_queries_and_keys_keep_their_bits(hs, ctx, gen, n, qk, value, scale):
+    """scale q k among fp16's subnormal numbers, what it weighs not."""
+    b, h, d, t = 2, 3, 64, torch.float16
+    q, k, v, state, _ = retention_inputs(gen, b, n, h, h, d, d, t)
+    q, k, v, state = (q * qk).to(t), (k * qk).to(t), v * value, state * (qk * value)
+    retention_of(hs, ctx, q, k, v, state, [0.5, 0.9, 0.99], scale, "small products")
