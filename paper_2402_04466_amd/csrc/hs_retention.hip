@@ -90,8 +90,8 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 //
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
 // is then half a step off, as out itself).  In fp16 a power of two is taken out of each row of A, so that its largest is below 2^15
-// and those of up to 2^-29 of that keep all their bits, and one out of the copy, so that it stays in that type's range
-// whatever the state has grown to.  The state takes no such rounding: decayed values enter as a sum of
+// and those of up to 2^-29 of that keep all their bits, and one out of each column of the copy, which lies
+// in the same range then whatever the state has grown to.  The state takes no such rounding: decayed values enter as a sum of
 // three bf16 or two fp16 parts.  The second of these is scaled by 2^11, out of fp16's subnormal numbers and no further: what a first
 // part leaves is up to 16, of values from 32768 on.  So two parts keep 22 bits of what is above 2^-14, and 2^-36 of the rest.
 constexpr int kChunk = 64;
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
   constexpr int kK = kChunk * CH * 16, kV = 2 * kK, kP = kV + kVTile, kSlot = kP + kParts * kVTile;   // Q, K, V of a chunk, V's decayed parts
   constexpr int kS = 2 * kSlot, kCopy = kWide * CH * 16;
   __shared__ __align__(16) char lds[kS + 2 * kCopy];
-  __shared__ int exponents[kHalf ? 2 : 1][kHalf ? 4 : 1];
+  __shared__ int4 exponents[kHalf ? 2 : 1][kHalf ? kWide / 4 : 1];   // of the copies' columns
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w4 = wave & 3, l16 = lane & 15, g = lane >> 4;
   const int blocks = (p.value_dim + kWide - 1) / kWide;
   int id = xcd_number();
@@ -157,17 +157,17 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
         for (int t = 0; t < KT; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(S[t][i]));
-        most = wave_max(most);
-        if (most == INFINITY) {                     // (the finite values keep theirs)
+        most = column_max(most);
+        if (__any(most == INFINITY)) {              // (the finite values keep theirs)
           most = 0.0f;
 #pragma unroll
           for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(S[t][i]) < INFINITY ? fabsf(S[t][i]) : 0.0f);
-          most = wave_max(most);
+          most = column_max(most);
         }
-        exponent = max(min(__builtin_amdgcn_frexp_expf(most) - 12, 100), -100);
-        if (lane == 0) exponents[to][w4] = exponent;
+        exponent = max(__builtin_amdgcn_frexp_expf(most) - 15, -100);
+        if (g == 0) ((int*)exponents[to])[16 * w4 + l16] = exponent;
       }
       const float small = ldexpf(1.0f, -exponent);
 #pragma unroll
@@ -367,7 +367,13 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
             f32x4 t = {0, 0, 0, 0};
 #pragma unroll
             for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
-            o[d] += t * (kHalf ? ldexpf(after, exponents[c & 1][d]) : after);
+            if (kHalf) {
+              const int4 e = exponents[c & 1][4 * d + g];
+              t *= after;
+              o[d] += f32x4{ldexpf(t[0], e.x), ldexpf(t[1], e.y), ldexpf(t[2], e.z), ldexpf(t[3], e.w)};
+            } else {
+              o[d] += t * after;
+            }
           }
         };
         auto scores = [&](int cb) {

@@ -89,18 +89,9 @@ __device__ __forceinline__ float column_max(float x) {
   return fmaxf(lower, upper);
 }
 
-// The largest of a wave's values (NaN is left out), in all lanes: rows of 16 by neighbours, pairs and mirrored halves, then
-// pairs of rows and the wave's halves.
 template <int CONTROL>
 __device__ __forceinline__ float moved(float x) {   // from another lane of the row of 16
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float wave_max(float x) {
-  x = fmaxf(x, moved<0xb1>(x));                     // lane ^ 1
-  x = fmaxf(x, moved<0x4e>(x));                     // lane ^ 2
-  x = fmaxf(x, moved<0x141>(x));                    // 7 - lane
-  x = fmaxf(x, moved<0x140>(x));                    // 15 - lane
-  return column_max(x);
 }
 
 template <class T>

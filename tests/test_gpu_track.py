@@ -629,3 +629,29 @@ def test_small_products_of_queries_and_keys_keep_their_bits(hs, ctx, gen, n, qk,
     q, k, v, state, _ = retention_inputs(gen, b, n, h, h, d, d, t)
     q, k, v, state = (q * qk).to(t), (k * qk).to(t), v * value, state * (qk * value)
     retention_of(hs, ctx, q, k, v, state, [0.5, 0.9, 0.99], scale, "small products")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n", [9, 70, 150, 1100])
+def test_value_columns_of_different_magnitude_keep_their_bits(hs, ctx, gen, dtype, n):
+    """Columns of 2^-17 beside ones of 2^12, at a scale that brings the largest output between 2^14 and 2^15."""
+    b, h, d, t = 2, 3, 64, TYPES[dtype]
+    q, k, v, state, _ = retention_inputs(gen, b, n, h, h, d, d, t)
+    size, decay = 2.0 ** (torch.arange(d, device=DEV) * 11 % 30 - 17.0), [0.9, 0.99, 0.999]
+    v, state = (v * size).to(t), state * size
+    most = retention_reference(q, k, v, state, decay, 1.0, None)[0].abs().max().item()
+    retention_of(hs, ctx, q, k, v, state, decay, 2.0 ** (15 - math.frexp(most)[1]), "columns")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n", [1, 20, 100])
+def test_states_of_every_magnitude(hs, ctx, gen, dtype, n):
+    """From 2^-90 to 2^117, each column by a power of its own; scales that bring the outputs of one head into the type's range."""
+    b, h, d, t = 1, 4, 64, TYPES[dtype]
+    q, k, v, state, _ = retention_inputs(gen, b, n, h, h, d, d, t)
+    for power, scale in ((-90, 2.0 ** 88), (-30, 2.0 ** 24), (40, 2.0 ** -42), (117, 2.0 ** -120)):
+        size = 2.0 ** (power - torch.arange(d, device=DEV) % 8.0)
+        ref = retention_reference(q, k, v * 0, state * size, [1.0, 0.5, 0.9, 0.99], scale, None)
+        out, end = torch.full_like(v, 7.0), torch.full_like(state, 7.0)
+        retention_call(hs, ctx, q, k, v * 0, out, state * size, end, [1.0, 0.5, 0.9, 0.99], scale)
+        retention_check(out, end, ref, t, n, f"2^{power}")
