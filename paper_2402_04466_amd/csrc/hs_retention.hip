@@ -1,10 +1,17 @@
 // hs_retention: linear attention with a decay for each head.
 #include "hs_track_device.h"
 
+#include <float.h>
+
 #include <algorithm>
 #include <type_traits>
 
 namespace hs {
+
+// Infinities of the state stay what they are (but for a decay of zero), as the recurrence has it: a correction to their decay would make
+// NaN of them, and so would a power of the decay that underflows.
+__device__ __forceinline__ float finite(float x) { return __builtin_amdgcn_fmed3f(x, -FLT_MAX, FLT_MAX); }
+__device__ __forceinline__ float least_power(float decay) { return decay > 0.0f ? FLT_TRUE_MIN : 0.0f; }
 
 // Recurrent form: S = decay * S + k v^T, out = scale * q S, token by token.  A workgroup holds key_dim x 64 values of
 // one sequence's and head's state in registers: 16 lanes side by side have 4 values of 16 bytes each, so a row of
@@ -36,11 +43,10 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
   xr qq = {}, kk = {};
   x4 vv = {};
   auto fetch = [&](int64_t t) {                     // (also of a token behind the sequence's end: then not used)
-    if (in_k) {
-      qq = *(const xr*)(q + t * p.q.token);
-      kk = *(const xr*)(k + t * p.k.token);
-    }
-    if (in_v) vv = *(const x4*)(v + t * p.v.token);
+    if (!there) return;                             // (zeros: a value that is not finite is not multiplied by what is not there)
+    qq = *(const xr*)(q + t * p.q.token);
+    kk = *(const xr*)(k + t * p.k.token);
+    vv = *(const x4*)(v + t * p.v.token);
   };
   if (p.tokens > 0) fetch(0);
   const int n = length_of(p.lengths, b, p.tokens);
@@ -52,7 +58,7 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        S[r][i] = fmaf(decay, S[r][i], fmaf(rest, S[r][i], (float)kk[r] * (float)vv[i]));
+        S[r][i] = fmaf(decay, S[r][i], fmaf(rest, finite(S[r][i]), (float)kk[r] * (float)vv[i]));
         o[i] = fmaf((float)qq[r], S[r][i], o[i]);
       }
     if (t + 1 < n) fetch(t + 1);
@@ -84,6 +90,9 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 //   from there into the other half of LDS, with the values' decayed parts;
 //   waves 8 .. 11 form out, 16 of the chunk's rows each: A by K Q^T, so that a lane holds four keys of one row per tile
 //   and A is the operand of the next product where it lies, if that one takes V's rows in the same order.
+// An infinity or NaN among the tokens would reach earlier ones through their zeros in A, and has no parts.  The waves that load
+// multiply everything by zero on the side; where that has given NaN, the waves that carry the state go over the tokens a second
+// time, one by one, and write what the recurrence has.
 // One barrier a chunk.  The chain of LDS reads and products from barrier to barrier bounds it: with eight waves that shared the
 // loads, 10 chunks of 64 sequences took 19.9 us (now 15.5), ragged clips of 96 x 80 38.7 (26.7), 113 chunks of 128 x 128 in 256
 // workgroups 280 (270: 3.6 TB/s, where the loads alone take 168).  The waves that form out are the longest, and go first.
@@ -128,11 +137,19 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
   auto left_of = [&](int c) { return (int)min((int64_t)n - (int64_t)(first + c) * kChunk, (int64_t)kChunk); };   // tokens of chunk c
   // the decay's powers below the chunk's: a wave has one per lane
   const double power64 = exp2(p.log2_decay[h] * lane);
-  const float power = (float)power64;
+  const float least = least_power(p.decay[h]), power = fmaxf((float)power64, least);
   auto power_of = [&](int steps) { return __shfl(power, steps); };
 
-  if (wave < 4 && w4 >= DT) {
+  // Behind the last chunk's barrier: whether a wave that loads has met an infinity or NaN.  (Where a further chunk would have its parts.)
+  int* const met = (int*)(lds + (chunks & 1) * kSlot + kP);
+  auto any_met = [&]() { return (met[0] | met[1] | met[2] | met[3]) != 0; };
+  auto wait_for_chunks = [&]() {
     for (int c = -1; c < chunks; ++c) __syncthreads();
+  };
+
+  if (wave < 4 && w4 >= DT) {
+    wait_for_chunks();
+    if (any_met()) wait_for_chunks();
   } else if (wave < 4) {
     // ---- the state: lane has dimension dv, key dimensions 16 t + 4 g + i
     const int dv = kWide * block + 16 * w4 + l16;
@@ -141,13 +158,16 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
     // (the first segment's, where the last one may have written over it already: as k_retain_starts has kept it)
     const float* const from = kStates ? nullptr : segment ? p.parts + (segment - 1) * states : segments > 1 && p.state_in == p.state_out ? p.parts + (segments - 1) * states : p.state_in;
     f32x4 S[KT];
+    auto begin = [&](const float* from) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+      for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int dk = 16 * t + 4 * g + i;
-        S[t][i] = from && dv < p.value_dim && dk < p.key_dim ? from[state0 + (int64_t)dk * p.value_dim] : 0.0f;
-      }
+        for (int i = 0; i < 4; ++i) {
+          const int dk = 16 * t + 4 * g + i;
+          S[t][i] = from && dv < p.value_dim && dk < p.key_dim ? from[state0 + (int64_t)dk * p.value_dim] : 0.0f;
+        }
+    };
+    begin(from);
     // the state's 16-bit copy, [dimension][key dimension]
     auto leave_copy = [&](int to) {
       int exponent = 0;
@@ -188,6 +208,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
       carried += keep_rest;
       float now = keep + carried;
       carried -= now - keep;
+      now = fmaxf(now, least);
       const int left = left_of(c);
       if (left < kChunk) now = power_of(left);
       x8 part[2][kParts];                           // decayed values: dimension 16 w4 + l16, tokens 32 s + 8 g + i
@@ -222,6 +243,40 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
       }
       if (!kStates && c + 1 < chunks) leave_copy(~c & 1);
       __syncthreads();
+    }
+    if (any_met()) {                                // token by token from the start
+      const float decay = p.decay[h], rest = p.decay_rest[h];
+      const float* start = from;
+      asm("" : "+s"(start));                        // (its addresses are formed here, not kept through the chunks)
+      begin(start);
+      __syncthreads();
+      for (int c = 0; c < chunks; ++c) {
+        const char* const here = lds + (c & 1) * kSlot;
+        const int left = left_of(c);
+#pragma unroll 1
+        for (int j = 0; j < left; ++j) {
+          const float v = (float)*(const T*)(here + kV + slot<8>(j, 2 * w4 + (l16 >> 3)) + (l16 & 7) * 2);
+          float o = 0.0f;
+#pragma unroll
+          for (int t = 0; t < KT; ++t) {
+            if (16 * t + 4 * g >= p.key_dim) continue;
+            const int at_k = slot<CH>(j, 2 * t + (g >> 1)) + (g & 1) * 8;
+            const x4 k = *(const x4*)(here + kK + at_k);
+            x4 q = {};
+            if (!kStates) q = *(const x4*)(here + at_k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              S[t][i] = fmaf(decay, S[t][i], fmaf(rest, finite(S[t][i]), (float)k[i] * v));
+              if (!kStates) o = fmaf((float)q[i], S[t][i], o);
+            }
+          }
+          if (kStates) continue;
+          o += __shfl_xor(o, 16);
+          o += __shfl_xor(o, 32);
+          if (g == 0 && dv < p.value_dim) at_out<T>(p.out, b, (int64_t)(first + c) * kChunk + j, h)[dv] = (T)(p.scale * o);
+        }
+        __syncthreads();
+      }
     }
     float* to = p.state_out + state0;
     if (kStates) to = p.parts + segment * states + state0;
@@ -281,6 +336,8 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
     float weight[NV];                               // v's decay until the chunk's end
 #pragma unroll
     for (int e = 0; e < NV; ++e) weight[e] = power_of(kChunk - 1 - vr - e * 32);
+    f32x4 zero = {0, 0, 0, 0};                      // what is loaded, times zero (on the matrix pipe 113 chunks of 128 x 128 take
+                                                    // 249 us, 243 without; on the vector pipe 10 of 64 x 64 take 4 % more)
     auto store = [&](int c, Pieces& from) {
       if (c >= chunks) return;
       char* const to = lds + (c & 1) * kSlot;
@@ -300,6 +357,13 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
         if (!kStates) *(s16x8*)(to + slot<CH>(r0 + e * RP, ch)) = from.q[e];
         *(s16x8*)(to + kK + slot<CH>(r0 + e * RP, ch)) = from.k[e];
       }
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        if (!kStates) zero = mfma16(__builtin_bit_cast(x8, from.q[e]), x8{}, zero);
+        zero = mfma16(__builtin_bit_cast(x8, from.k[e]), x8{}, zero);
+      }
+#pragma unroll
+      for (int e = 0; e < NV; ++e) zero = mfma16(__builtin_bit_cast(x8, from.v[e]), x8{}, zero);
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
         const int at_v = slot<8>(vr + u * 32, vch);
@@ -321,19 +385,46 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
         }
       }
     };
+    auto tell = [&]() {
+      const bool it = __any((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.0f);
+      if (lane == 0) met[w4] = it;
+    };
     fetch(0, even);
     fetch(1, odd);
     store(0, even);
     fetch(2, even);
+    if (chunks == 0) tell();
     __syncthreads();
     for (int c = 0; c < chunks; c += 2) {
       store(c + 1, odd);
       fetch(c + 3, odd);
+      if (c + 1 == chunks) tell();
       __syncthreads();
       if (c + 1 >= chunks) break;
       store(c + 2, even);
       fetch(c + 4, even);
+      if (c + 2 == chunks) tell();
       __syncthreads();
+    }
+    if (any_met()) {                                // the chunks as they are, one after the other
+      auto bring = [&](int c) {
+        char* const to = lds + (c & 1) * kSlot;
+        const int64_t t0 = (int64_t)(first + c) * kChunk;
+        const int left = c < chunks ? left_of(c) : 0;
+        if (in_k)
+          for (int r = r0; r < left; r += RP) {
+            if (!kStates) *(s16x8*)(to + slot<CH>(r, ch)) = load16(at<T>(p.q, b, t0 + r, h) + 8 * ch);
+            *(s16x8*)(to + kK + slot<CH>(r, ch)) = load16(at<T>(p.k, b, t0 + r, hk) + 8 * ch);
+          }
+        if (in_v)
+          for (int r = vr; r < left; r += 32) *(s16x8*)(to + kV + slot<8>(r, vch)) = load16(at<T>(p.v, b, t0 + r, hk) + kWide * block + 8 * vch);
+      };
+      bring(0);
+      __syncthreads();
+      for (int c = 0; c < chunks; ++c) {
+        bring(c + 1);
+        __syncthreads();
+      }
     }
     if (!kStates && last && in_v)
       for (int64_t t = (int64_t)n + vr; t < p.tokens; t += 32) *(s16x8*)(at_out<T>(p.out, b, t, h) + kWide * block + 8 * vch) = s16x8{};
@@ -349,10 +440,9 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int apart = 16 * (W - cb) + l16 - 4 * g - i;
-          const float x = power_of(max(apart, 0));
-          decay[cb][i] = apart < 0 ? 0.0f : x;
+          decay[cb][i] = power_of(max(apart, 0));
         }
-      const float after = power_of(16 * W + l16) * p.decay[h];
+      const float after = fmaxf(power_of(16 * W + l16) * p.decay[h], least);
       __syncthreads();
       for (int c = 0; c < chunks; ++c) {
         const char* const here = lds + (c & 1) * kSlot;
@@ -361,20 +451,14 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *(const x8*)(here + 16 * W * CH * 16 + slot<CH>(l16, 4 * s + g));
         f32x4 o[DT] = {};
-        auto add_from_state = [&]() {
+        auto from_state = [&](int d) {
+          f32x4 t = {0, 0, 0, 0};
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            f32x4 t = {0, 0, 0, 0};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
-            if (kHalf) {
-              const int4 e = exponents[c & 1][4 * d + g];
-              t *= after;
-              o[d] += f32x4{ldexpf(t[0], e.x), ldexpf(t[1], e.y), ldexpf(t[2], e.z), ldexpf(t[3], e.w)};
-            } else {
-              o[d] += t * after;
-            }
-          }
+          for (int s = 0; s < KS; ++s) t = mfma16(*(const x8*)(copy + 16 * d * CH * 16 + slot<CH>(l16, 4 * s + g)), q[s], t);
+          t *= after;
+          if (!kHalf) return t;
+          const int4 e = exponents[c & 1][4 * d + g];
+          return f32x4{ldexpf(t[0], e.x), ldexpf(t[1], e.y), ldexpf(t[2], e.z), ldexpf(t[3], e.w)};
         };
         auto scores = [&](int cb) {
           f32x4 t = {0, 0, 0, 0};
@@ -387,8 +471,11 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
         for (int cb = 0; cb <= W; ++cb) {
           const f32x4 t = scores(cb);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[cb / 2][cb % 2 * 4 + i] = t[i] * decay[cb][i];
+          for (int i = 0; i < 4; ++i) x[cb / 2][cb % 2 * 4 + i] = cb == W && l16 < 4 * g + i ? 0.0f : t[i] * decay[cb][i];
         }
+        f32x4 before[DT];                           // the state's part of out
+#pragma unroll
+        for (int d = 0; d < DT; ++d) before[d] = from_state(d);
         float up = 1.0f;                            // the power of two that is out of this lane's row
         if (kHalf) {
           float most = 0.0f;
@@ -408,6 +495,10 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
 #pragma unroll
         for (int j = 0; j <= W / 2; ++j) a[j] = round8<T>(x[j]);
         __builtin_amdgcn_sched_barrier(0);          // (as above)
+        if (!kHalf) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[d] = before[d];
+        }
 #pragma unroll
         for (int j = 0; j <= W / 2; ++j)
 #pragma unroll
@@ -418,38 +509,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
           }
         if (kHalf) {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) o[d] *= up;
-        }
-        add_from_state();
-        float finite = 0.0f;                        // zero, or NaN
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) finite = fmaf(o[d][i], 0.0f, finite);
-        if (__any(finite != 0.0f)) {
-          // A product beyond fp32's range, or an input that is not finite, which must not reach earlier tokens through their
-          // zeros in A: term by term, in fp32.
-#pragma unroll
-          for (int d = 0; d < DT; ++d) o[d] = f32x4{0, 0, 0, 0};
-#pragma unroll 1
-          for (int cb = 0; cb <= W; ++cb) {
-            const f32x4 t = scores(cb);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll 1
-              for (int from = 0; from < 4; ++from) {
-                const int key = 16 * cb + 4 * from + i, apart = 16 * W + l16 - key;
-                const float x = __shfl(t[i], 16 * from + l16) * power_of(max(apart, 0));
-                if (apart < 0) continue;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                  const x4 v = *(const x4*)(here + kV + slot<8>(key, 2 * d + (g >> 1)) + (g & 1) * 8);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) o[d][e] = fmaf(x, (float)v[e], o[d][e]);
-                }
-              }
-          }
-          add_from_state();
+          for (int d = 0; d < DT; ++d) o[d] = o[d] * up + before[d];
         }
         const int64_t t = (int64_t)(first + c) * kChunk + 16 * W + l16;
         if (t < n) {
@@ -467,6 +527,7 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
       case 2: run(std::integral_constant<int, 2>{}); break;
       default: run(std::integral_constant<int, 3>{}); break;
     }
+    if (any_met()) wait_for_chunks();               // (the waves that carry the state write what is right)
   }
 }
 
@@ -480,7 +541,7 @@ __global__ __launch_bounds__(256) void k_retain_starts(RetentionParams p, int se
   const int n = p.lengths ? min(max(p.lengths[b], 0), p.tokens) : p.tokens, chunks = (int)(((int64_t)n + kChunk - 1) / kChunk), per_segment = (chunks + segments - 1) / segments;
   const int used = per_segment ? (chunks - 1) / per_segment : 0;   // segments before the sequence's last one
   const double far = exp2(p.log2_decay[bh % p.q_heads] * ((double)per_segment * kChunk));
-  const float keep = (float)far, keep_rest = (float)(far - (double)keep);
+  const float keep = fmaxf((float)far, least_power(p.decay[bh % p.q_heads])), keep_rest = (float)(far - (double)keep);
   f32x4 S = {0, 0, 0, 0};
   if (p.state_in) S = *(const f32x4*)(p.state_in + at_value);
   float* part = p.parts + at_value;
@@ -489,7 +550,7 @@ __global__ __launch_bounds__(256) void k_retain_starts(RetentionParams p, int se
   for (int s = 0; s < used; ++s, part += states) {
     const f32x4 add = *(const f32x4*)part;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) S[i] = fmaf(S[i], keep, fmaf(S[i], keep_rest, add[i]));
+    for (int i = 0; i < 4; ++i) S[i] = fmaf(S[i], keep, fmaf(finite(S[i]), keep_rest, add[i]));
     *(f32x4*)part = S;
   }
 }

@@ -1,6 +1,8 @@
 // The track decoder's operators behind the C boundary: checks of the descriptions, and launches on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include <float.h>
+
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
@@ -203,7 +205,7 @@ RetentionParams params_of(const hs_retention_desc* d) {
   p.scale = d->scale;
   p.parts = (float*)d->d_workspace;
   for (int h = 0; h < d->q_heads; ++h) {
-    p.decay[h] = (float)d->decay[h];
+    p.decay[h] = d->decay[h] > 0.0 ? std::max((float)d->decay[h], FLT_TRUE_MIN) : 0.0f;   // (only a decay of 0 ends an infinity)
     p.decay_rest[h] = (float)(d->decay[h] - (double)p.decay[h]);
     p.log2_decay[h] = std::max(std::log2(d->decay[h]), -1e4);   // (a decay of 0: 2^0 = 1 after no step, 0 after one)
   }

@@ -36,7 +36,7 @@ struct RetentionParams {
   float* state_out;
   int dtype, batch, tokens, q_heads, group, key_dim, value_dim;   // group: query heads per key head
   float scale;
-  float decay[HS_MAX_HEADS], decay_rest[HS_MAX_HEADS];   // the decay in two parts, 48 bits of it together
+  float decay[HS_MAX_HEADS], decay_rest[HS_MAX_HEADS];   // the decay in two parts, 48 bits of it together; 0 only for 0
   double log2_decay[HS_MAX_HEADS];
   float* parts;                  // workspace: retention_workspace() bytes
 };

@@ -655,3 +655,42 @@ def test_states_of_every_magnitude(hs, ctx, gen, dtype, n):
         out, end = torch.full_like(v, 7.0), torch.full_like(state, 7.0)
         retention_call(hs, ctx, q, k, v * 0, out, state * size, end, [1.0, 0.5, 0.9, 0.99], scale)
         retention_check(out, end, ref, t, n, f"2^{power}")
+
+
+# ---- retention: what is not finite -------------------------------------------------------------------------
+def formula_check(got, want, bound, what):
+    """NaN and infinities where the definition has them, of its sign, and the finite values within the bound."""
+    got = got.double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what + ": NaN"
+    far = torch.isinf(want)
+    assert torch.equal(torch.isinf(got), far) and torch.equal(got[far], want[far]), what + ": infinities"
+    finite_check(got, want, bound, what)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("dk, dv", [(64, 64), (72, 40), (128, 72)])
+@pytest.mark.parametrize("n, spot", [(1, 0), (5, 3), (70, 1), (70, 66), (200, 63), (200, 64), (1500, 700)])
+@pytest.mark.parametrize("which", ["q", "k", "v", "state"])
+def test_infinities_and_nan_are_where_the_recurrence_has_them(hs, ctx, gen, dtype, dk, dv, n, spot, which):
+    """Also for decays that fp32 holds exactly, whose rest is negative, and that underflow."""
+    t = TYPES[dtype]
+    decay = [1.0, 0.96875, 0.99, 0.9, 1e-60, 0.0]
+    b, h = 4, len(decay)
+    q, k, v, state, _ = retention_inputs(gen, b, n, h, h, dk, dv, t)
+    u, steps = half_step(t), (64 + 2 * n) * F32
+    x = {"q": q, "k": k, "v": v, "state": state}[which]
+    at = (lambda i: x[i, :, 3]) if which == "state" else (lambda i: x[i, spot])      # [h, dim]
+    at(0)[:, 5] = float("inf")
+    at(1)[:, 7] = float("-inf")
+    at(2)[:, 9] = float("nan")
+    if n > 5 and which != "state":
+        at(0)[:, 6] = float("-inf")
+        x[1, spot + 1, :, 7] = float("inf")            # the two signs in the same place, one token apart
+    want, S, size, A = retention_reference(q, k, v, state, decay, 0.125, None)
+    out, end = torch.full_like(want, 7.0, dtype=t), torch.full_like(state, 7.0)
+    retention_call(hs, ctx, q, k, v, out, state, end, decay, 0.125)
+    formula_check(out, want, u * want.abs() + (u + steps) * (1 + u) * size + 2.0 ** -25, "out")
+    formula_check(end, S, steps * A + 2.0 ** -40, "state")
+    keep = state.clone()
+    retention_call(hs, ctx, q, k, v, out, keep, keep, decay, 0.125)
+    assert torch.equal(keep.isnan(), end.isnan()) and torch.equal(keep[~keep.isnan()], end[~end.isnan()])
