@@ -40,12 +40,13 @@ class TrackDecoder:
         self.frequencies = 10000.0 ** (-torch.arange(0, head_dim, 2, dtype=torch.float64, device=device) / head_dim)
         # half-lives from 22 frames on
         self.decay = [1.0 - 2.0 ** (-5.0 - 7.0 * h / max(1, heads - 1)) for h in range(heads)]
-        self.reset()
+        self.state = torch.zeros(streams * tools, heads, head_dim, head_dim, device=device)
+        self.frame = torch.zeros(1, dtype=torch.int64, device=device)
 
     def reset(self) -> None:
-        """All tracks begin: no state, frame 0."""
-        self.state = torch.zeros(self.streams * self.tools, self.heads, self.head_dim, self.head_dim, device=self.device)
-        self.frame = torch.zeros(1, dtype=torch.int64, device=self.device)
+        """All tracks begin again: no state, frame 0.  In place, since captured graphs work on this memory."""
+        self.state.zero_()
+        self.frame.zero_()
 
     def _norm_rotate(self, stream, q, k, w_q, w_k, positions):
         side = dict(q=heads_of(q), q_out=heads_of(q), q_heads=q.shape[2], d_q_weight=w_q.data_ptr(), k_heads=0)

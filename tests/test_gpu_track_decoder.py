@@ -82,3 +82,26 @@ def test_shapes_that_do_not_fit_are_refused(ctx):
     dec = TrackDecoder(ctx, streams=2, heads=1)
     with pytest.raises(ValueError):
         dec.forward(torch.zeros(2, 2, 8, 64, dtype=torch.float16, device="cuda:0"), None)
+
+
+def test_live_streams_begin_again_after_a_reset(ctx):
+    """The graph that was captured before goes on with the tracks that begin again, bit by bit as one captured after."""
+    from paper_2402_04466_amd.track_decoder import TrackDecoder
+    g = torch.Generator(device="cuda:0").manual_seed(5)
+    kw = dict(streams=2, heads=2)
+    dec, fresh = TrackDecoder(ctx, **kw), TrackDecoder(ctx, **kw)
+    live, other = dec.live(60), fresh.live(60)
+    x = torch.randn(4, *live.x.shape, generator=g, device="cuda:0").to(dec.dtype)
+    live.maps.normal_()
+    other.maps.copy_(live.maps)
+    for i in range(3):
+        live.x.copy_(x[i])
+        live.step()
+    dec.reset()
+    held = [torch.full_like(dec.state, 9.0) for _ in range(4)]     # takes memory that is free now
+    for i in (3, 0, 1):
+        live.x.copy_(x[i])
+        other.x.copy_(x[i])
+        assert torch.equal(live.step(), other.step())
+    assert torch.equal(dec.state, fresh.state) and dec.frame.item() == fresh.frame.item() == 3
+    assert all(bool((h == 9.0).all()) for h in held)

@@ -178,3 +178,16 @@ def test_counts_beyond_one_call_are_refused():
     far = heads(batch=1 << 40, token=1 << 20, head=64)
     refused("hs_norm_rotate", norm_rotate(batch=1 << 16, tokens=1 << 16, q=far, k=far, q_out=far, k_out=far), "too many tokens")
     refused("hs_cross_attention", cross(batch=1 << 20, q_heads=1 << 14, kv_heads=1), "too many heads")
+
+
+def test_a_decoders_reset_keeps_the_memory_that_graphs_work_on():
+    import torch
+    from paper_2402_04466_amd.track_decoder import TrackDecoder
+    dec = TrackDecoder(0, streams=2, heads=1, device="cpu")
+    state, frame = dec.state, dec.frame
+    state.fill_(3.0)
+    frame.fill_(5)
+    dec.reset()
+    assert dec.state is state and dec.frame is frame
+    assert not state.any() and not frame.any()
+    assert state.dtype == torch.float32 and frame.dtype == torch.int64
