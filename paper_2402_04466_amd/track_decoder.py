@@ -63,10 +63,21 @@ class TrackDecoder:
         return work
 
     def forward(self, x: torch.Tensor, maps: torch.Tensor, mask: torch.Tensor | None = None) -> torch.Tensor:
-        """The next frames of every track.  mask: [streams, frames, cells] uint8, 0 where a cell is hidden."""
-        s, f, t, c = x.shape
-        if s != self.streams or t != self.tools or c != self.channels or (s > 1 and f > 1):
+        """The next frames of every track.  mask: [streams, frames, cells] uint8 or bool, 0 where a cell is hidden."""
+        def must_be(name, t, shape, *dtypes):
+            if t.shape != shape or t.dtype not in dtypes or t.device != self.state.device:
+                raise ValueError(f"{name} must be {list(shape)}, {' or '.join(map(str, dtypes))} on {self.state.device}, "
+                                 f"got {list(t.shape)}, {t.dtype} on {t.device}")
+        s, t, c = self.streams, self.tools, self.channels
+        f = x.shape[1] if x.dim() == 4 else 0
+        must_be("x", x, (s, f, t, c), self.dtype)
+        if s > 1 and f > 1:
             raise ValueError("need one stream, or one frame of every stream")
+        cells = maps.shape[2] if maps.dim() == 4 else 0
+        must_be("maps", maps, (s, f, cells, c), self.dtype)
+        if mask is not None:
+            must_be("mask", mask, (s, f, cells), torch.uint8, torch.bool)
+            mask = mask.contiguous()
         h, d, stream = self.heads, self.head_dim, torch.cuda.current_stream().cuda_stream
 
         def tracks(y):                              # [s, f, t, ...] as [s * t, f, ...], without a copy
@@ -86,12 +97,12 @@ class TrackDecoder:
 
         q = (x @ self.w_q2).view(s * f, t, h, d)
         self._norm_rotate(stream, q, None, self.w_norm[2], None, None)
-        kv = (maps @ self.w_kv).view(s * f, -1, 2, h, d)
+        kv = (maps @ self.w_kv).view(s * f, cells, 2, h, d)
         looked = torch.empty(s * f, t, h, d, dtype=self.dtype, device=self.device)
         desc = api.make_cross_attention_desc(
-            dtype=DTYPES[self.dtype], batch=s * f, q_tokens=t, k_tokens=kv.shape[1], q_heads=h, kv_heads=h, head_dim=d,
+            dtype=DTYPES[self.dtype], batch=s * f, q_tokens=t, k_tokens=cells, q_heads=h, kv_heads=h, head_dim=d,
             scale=d ** -0.5, q=heads_of(q), k=heads_of(kv[:, :, 0]), v=heads_of(kv[:, :, 1]), out=heads_of(looked),
-            d_mask=0 if mask is None else mask.data_ptr(), mask_batch_stride=kv.shape[1])
+            d_mask=0 if mask is None else mask.data_ptr(), mask_batch_stride=cells)
         work2 = self._workspace(desc, api.hs_query_cross_attention_workspace(desc))
         api.hs_cross_attention(self.ctx, desc, stream)
         self.frame += f

@@ -105,3 +105,24 @@ def test_live_streams_begin_again_after_a_reset(ctx):
         assert torch.equal(live.step(), other.step())
     assert torch.equal(dec.state, fresh.state) and dec.frame.item() == fresh.frame.item() == 3
     assert all(bool((h == 9.0).all()) for h in held)
+
+
+def test_masks_of_any_strides_and_maps_without_cells(ctx):
+    from paper_2402_04466_amd.track_decoder import TrackDecoder
+    g = torch.Generator(device="cuda:0").manual_seed(6)
+    frames, cells, kw = 3, 70, dict(streams=1, heads=2)
+    a = TrackDecoder(ctx, **kw)
+    x = torch.randn(1, frames, 8, a.channels, generator=g, device="cuda:0").to(a.dtype)
+    maps = torch.randn(1, frames, cells, a.channels, generator=g, device="cuda:0").to(a.dtype)
+    one = torch.rand(cells, generator=g, device="cuda:0") < 0.6
+    wide = torch.zeros(1, frames, 2 * cells, dtype=torch.uint8, device="cuda:0")
+    wide[:, :, ::2] = one.to(torch.uint8)
+    want = a.forward(x, maps, one.to(torch.uint8).expand(1, frames, cells).contiguous())
+    for mask in (one.expand(1, frames, cells), one.to(torch.uint8).expand(1, frames, cells), wide[:, :, ::2], wide[:, :, ::2] * 5):
+        a.reset()
+        assert torch.equal(a.forward(x, maps, mask), want)
+    # nothing to look at: what the tracks carry alone
+    a.reset()
+    none = a.forward(x, maps, torch.zeros(1, frames, cells, dtype=torch.bool, device="cuda:0"))
+    a.reset()
+    assert torch.equal(a.forward(x, maps[:, :, :0]), none)

@@ -191,3 +191,25 @@ def test_a_decoders_reset_keeps_the_memory_that_graphs_work_on():
     assert dec.state is state and dec.frame is frame
     assert not state.any() and not frame.any()
     assert state.dtype == torch.float32 and frame.dtype == torch.int64
+
+
+def test_a_decoder_refuses_inputs_that_do_not_fit_before_any_work():
+    import torch
+    from paper_2402_04466_amd.track_decoder import TrackDecoder
+    dec = TrackDecoder(0, streams=1, heads=1, device="cpu")
+    half = dict(dtype=torch.float16)
+    x, maps, mask = torch.zeros(1, 3, 8, 64, **half), torch.zeros(1, 3, 405, 64, **half), torch.ones(1, 3, 405, dtype=torch.uint8)
+    for bad in (x[0], x[:, :, :7], x.float(), x.to("meta"), torch.zeros(2, 3, 8, 64, **half), torch.zeros(1, 3, 8, 32, **half)):
+        with pytest.raises(ValueError, match="x must be"):
+            dec.forward(bad, maps, mask)
+    for bad in (maps[0], maps[:, :1], torch.zeros(1, 1, 405 * 3, 64, **half), torch.zeros(1, 3, 405, 32, **half), maps.to(torch.bfloat16),
+                maps.to("meta")):
+        with pytest.raises(ValueError, match="maps must be"):
+            dec.forward(x, bad, mask)
+    for bad in (mask[0], mask[:, :1], mask[:, :, :404], mask.long(), mask.to(torch.float16), mask.to("meta")):
+        with pytest.raises(ValueError, match="mask must be"):
+            dec.forward(x, maps, bad)
+    several = TrackDecoder(0, streams=2, heads=1, device="cpu")
+    with pytest.raises(ValueError, match="one stream"):
+        several.forward(torch.zeros(2, 2, 8, 64, **half), torch.zeros(2, 2, 5, 64, **half))
+    assert not dec.frame.any() and not several.frame.any()
