@@ -694,3 +694,54 @@ def test_infinities_and_nan_are_where_the_recurrence_has_them(hs, ctx, gen, dtyp
     keep = state.clone()
     retention_call(hs, ctx, q, k, v, out, keep, keep, decay, 0.125)
     assert torch.equal(keep.isnan(), end.isnan()) and torch.equal(keep[~keep.isnan()], end[~end.isnan()])
+
+
+# ---- forms that the tests above do not reach ------------------------------------------------------------
+def cross_case(hs, ctx, gen, t, b, nq, nk, hq, hk, d, cut):
+    """One call with ragged lengths and a mask, its log-sum-exp too.  cut: whether its keys are shared out, so that it has a workspace."""
+    q, k, v = normal(gen, b, nq, hq, d, dtype=t), normal(gen, b, nk, hk, d, dtype=t), normal(gen, b, nk, hk, d, dtype=t)
+    lengths = torch.randint(0, nk + 1, (b,), generator=gen, device=DEV, dtype=torch.int32)
+    lengths[0] = nk
+    mask = (torch.rand(b, nk, generator=gen, device=DEV) < 0.7).to(torch.uint8)
+    mask[-1] = 0
+    seen = (torch.arange(nk, device=DEV) < lengths[:, None]) & (mask != 0)
+    k[~seen], v[~seen] = float("nan"), float("inf")
+    out, lse = torch.full_like(q, 7.0), torch.full((b, hq, nq), 7.0, device=DEV)
+    work = cross_call(hs, ctx, q, k, v, out, d ** -0.5, lengths, mask, lse)
+    assert (work.numel() > 0) == cut
+    cross_check(out, lse, q, k, v, d ** -0.5, seen, "cross")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("d", [40, 64, 96, 104, 128])
+@pytest.mark.parametrize("b, nq, nk, hq, hk", [(16, 20, 333, 16, 16), (8, 150, 190, 32, 16), (40, 3, 64, 24, 8), (32, 8, 405, 8, 8)])
+def test_whole_row_tiles_enough_for_the_device(hs, ctx, gen, dtype, d, b, nq, nk, hq, hk):
+    """Row tiles of 128 or 256 that write their outputs themselves, the last of each key head with rows missing."""
+    cross_case(hs, ctx, gen, TYPES[dtype], b, nq, nk, hq, hk, d, False)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("b, nq, nk, hq, hk, d", [(13, 113, 4, 6, 6, 96), (1, 1755, 5, 12, 12, 72), (3, 660, 40, 12, 12, 64), (9, 250, 33, 8, 4, 128)])
+def test_many_rows_on_few_keys(hs, ctx, gen, dtype, b, nq, nk, hq, hk, d):
+    cross_case(hs, ctx, gen, TYPES[dtype], b, nq, nk, hq, hk, d, False)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("d", [64, 72, 96, 120])
+def test_few_rows_on_many_keys(hs, ctx, gen, dtype, d):
+    cross_case(hs, ctx, gen, TYPES[dtype], 3, 9, 6481, 8, 4, d, True)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("dk, dv", [(40, 48), (64, 96), (72, 64), (80, 48), (96, 56), (96, 128), (104, 40), (128, 112)])
+@pytest.mark.parametrize("b, n, h", [(3, 140, 2), (2, 1300, 2)])
+def test_retention_of_every_width(hs, ctx, gen, dtype, dk, dv, b, n, h):
+    """Keys and values of each pair of widths that the chunks have a form for, whole sequences and cut ones."""
+    t = TYPES[dtype]
+    q, k, v, state, decay = retention_inputs(gen, b, n, h, h, dk, dv, t)
+    lengths = torch.tensor([n, n - 77, 65][:b], dtype=torch.int32, device=DEV)
+    ref = retention_reference(q, k, v, state, decay, dk ** -0.5, lengths)
+    out, end = torch.full((b, n, h, dv), 7.0, dtype=t, device=DEV), torch.full_like(state, 7.0)
+    work = retention_call(hs, ctx, q, k, v, out, state, end, decay, dk ** -0.5, lengths)
+    assert (work.numel() > 0) == (n > 1000)
+    retention_check(out, end, ref, t, n, "widths")
