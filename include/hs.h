@@ -492,7 +492,12 @@ hs_status hs_partition_copy(hs_app* app, void* d_dst, const void* d_src, size_t 
  * 8..128; pointers 16-byte aligned and strides multiples of 8 elements, both where more than
  * nothing is read.  Strides of inputs may be 0 (one tensor for all) or negative; an output's rows
  * must not overlap, and but for the cases named below no output overlaps an input.  Offsets are
- * 64-bit.  Sums, norms, softmax statistics and states are fp32; every output is rounded once. */
+ * 64-bit.  Sums, norms, softmax statistics and states are fp32; every output is rounded once.
+ * What goes through the matrix pipe on the way is 16 bits wide, each term off by half a step of the
+ * inputs' type at most: softmax weights and, in a retention of more than 8 tokens, the weights that
+ * tokens have for each other and the state that queries are multiplied by.  In fp16 these keep all
+ * their bits down to 2^-28 of the largest of their row (a token and head, or a column of the state;
+ * softmax weights down to 2^-21); what is smaller is off by 2^-32 of the largest. */
 typedef enum { HS_F16 = 1, HS_BF16 = 2 } hs_dtype;
 typedef struct {
   void* d;                      /* first value of batch 0, token 0, head 0 (inputs are only read)  */
@@ -532,8 +537,11 @@ hs_status hs_norm_rotate(hs_ctx* ctx, const hs_norm_rotate_desc* desc, void* hip
  * 0..tokens are taken as the nearer end).  state_out is the state behind the sequence's last token;
  * out is zero for the tokens behind it, whose q, k and v are not used whatever they hold.
  * One call serves a whole clip (tokens = its frames) or one frame of every live stream
- * (tokens = 1); a clip cut into calls gives the same results up to the order of fp32 sums.
- * An infinity or NaN in a token reaches later tokens and the state as the formula has it, and no earlier token.
+ * (tokens = 1).  A clip cut into calls carries the same state up to the order of fp32 sums and, in calls
+ * of more than 8 tokens, the parts in which values enter it (in bf16 24 bits of each value and its
+ * decay, in fp16 22 and down to 2^-36); its outputs agree within the roundings above.
+ * An infinity or NaN in a token or in the state reaches later tokens and the state as the formula has it,
+ * and no earlier token; a sequence with one in its tokens takes several times as long.
  * state_in may be NULL (zeros) or be state_out itself; tokens = 0 copies the state. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k, v, out                                        */

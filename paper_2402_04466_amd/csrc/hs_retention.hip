@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 //
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
 // is then half a step off, as out itself).  In fp16 a power of two is taken out of each row of A, so that its largest is below 2^15
-// and those of up to 2^-29 of that keep all their bits, and one out of each column of the copy, which lies
+// and those of up to 2^-28 of that keep all their bits, and one out of each column of the copy, which lies
 // in the same range then whatever the state has grown to.  The state takes no such rounding: decayed values enter as a sum of
 // three bf16 or two fp16 parts.  The second of these is scaled by 2^11, out of fp16's subnormal numbers and no further: what a first
 // part leaves is up to 16, of values from 32768 on.  So two parts keep 22 bits of what is above 2^-14, and 2^-36 of the rest.
