@@ -541,7 +541,8 @@ hs_status hs_norm_rotate(hs_ctx* ctx, const hs_norm_rotate_desc* desc, void* hip
  * of more than 8 tokens, the parts in which values enter it (in bf16 24 bits of each value and its
  * decay, in fp16 22 and down to 2^-36); its outputs agree within the roundings above.
  * An infinity or NaN in a token or in the state reaches later tokens and the state as the formula has it,
- * and no earlier token; a sequence with one in its tokens takes several times as long.
+ * and no earlier token; in calls of more than 8 tokens a sequence with one in its tokens is gone over
+ * again token by token, up to a microsecond each.
  * state_in may be NULL (zeros) or be state_out itself; tokens = 0 copies the state. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k, v, out                                        */

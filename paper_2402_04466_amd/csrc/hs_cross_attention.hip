@@ -391,6 +391,9 @@ CrossPlan plan_of(const CrossParams& p) {
   // 500 on 1000 (8 of 64) 9.6 and 12.4; with parts of four tiles 1000 on 2000 (8 heads of 128) takes 29.9 and not 23.3.
   const int cut = at_most(p.dim > 64 ? 256 : 512, wide, keys64 / 8);
   plan.groups = 0;
+  // Row tiles enough for the device are taken whatever their rows: 40 tokens on 405 keys (64 times, 8 heads of 64) 15.4 us, 17.9 by the form
+  // below, 8 tokens on 405 keys 14.5 and 16.0, 8 on 64 keys (40 times) 5.4 and 7.9.  With many more heads or keys than that and few rows it
+  // is the slower one: 8 tokens on 405 keys (600 times) 112 and 95, (32 times) 10.6 and 7.9, of heads of 128 dimensions (600 times) 315 and 181.
   // And where the form below would need several rounds of workgroups for so few keys that most of its waves had none: 1755 tokens on
   // 5 keys (12 heads of 72) 7.6 us, 17.9; 113 on 4 (13 times, 6 heads of 96) 7.9, 12.3; 660 on 5 (3 times, 12 heads of 64) 7.3, 6.6.
   const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, few = bh * ((rows + 31) / 32);

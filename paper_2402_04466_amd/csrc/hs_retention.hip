@@ -93,9 +93,10 @@ __global__ __launch_bounds__(256) void k_retain_steps(RetentionParams p) {
 // An infinity or NaN among the tokens would reach earlier ones through their zeros in A, and has no parts.  The waves that load
 // multiply everything by zero on the side; where that has given NaN, the waves that carry the state go over the tokens a second
 // time, one by one, and write what the recurrence has.
-// One barrier a chunk.  The chain of LDS reads and products from barrier to barrier bounds it: with eight waves that shared the
-// loads, 10 chunks of 64 sequences took 19.9 us (now 15.5), ragged clips of 96 x 80 38.7 (26.7), 113 chunks of 128 x 128 in 256
-// workgroups 280 (270: 3.6 TB/s, where the loads alone take 168).  The waves that form out are the longest, and go first.
+// One barrier a chunk.  The chain of LDS reads and products from barrier to barrier bounds it: 10 chunks of 64 sequences and heads of
+// 64 x 64 take 16.1 us (19.9 with eight waves that shared the loads), 40 ragged clips of up to 257 tokens of 8 heads of 96 x 80 24.3 to 26
+// (38.7), 113 chunks of 128 x 128 in 256 workgroups 240 to 259 by device, 3.7 to 4.0 TB/s (in one trace 285, of which the loads alone
+// take 168).  The waves that form out are the longest, and go first.
 //
 // Rounded to 16 bits, as the matrix pipe takes them: A, and the copy of S that multiplies q (each term of out
 // is then half a step off, as out itself).  In fp16 a power of two is taken out of each row of A, so that its largest is below 2^15
@@ -256,18 +257,21 @@ __global__ __launch_bounds__(kStates ? 512 : 768) void k_retain_chunks(Retention
 #pragma unroll 1
         for (int j = 0; j < left; ++j) {
           const float v = (float)*(const T*)(here + kV + slot<8>(j, 2 * w4 + (l16 >> 3)) + (l16 & 7) * 2);
+          x4 k[KT], q[KT] = {};
+#pragma unroll
+          for (int t = 0; t < KT; ++t) {
+            const int at_k = slot<CH>(j, 2 * t + (g >> 1)) + (g & 1) * 8;
+            k[t] = *(const x4*)(here + kK + at_k);
+            if (!kStates) q[t] = *(const x4*)(here + at_k);
+          }
           float o = 0.0f;
 #pragma unroll
           for (int t = 0; t < KT; ++t) {
-            if (16 * t + 4 * g >= p.key_dim) continue;
-            const int at_k = slot<CH>(j, 2 * t + (g >> 1)) + (g & 1) * 8;
-            const x4 k = *(const x4*)(here + kK + at_k);
-            x4 q = {};
-            if (!kStates) q = *(const x4*)(here + at_k);
+            const float in = 16 * t + 4 * g < p.key_dim ? v : 0.0f;   // (behind the keys there are zeros, as the first time)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              S[t][i] = fmaf(decay, S[t][i], fmaf(rest, finite(S[t][i]), (float)k[i] * v));
-              if (!kStates) o = fmaf((float)q[i], S[t][i], o);
+              S[t][i] = fmaf(decay, S[t][i], fmaf(rest, finite(S[t][i]), (float)k[t][i] * in));
+              if (!kStates) o = fmaf((float)q[t][i], S[t][i], o);
             }
           }
           if (kStates) continue;
@@ -564,7 +568,13 @@ struct RetentionPlan {
 RetentionPlan plan_of(const RetentionParams& p) {
   RetentionPlan plan;
   plan.workgroups = (int64_t)p.batch * p.q_heads * ((p.value_dim + 63) / 64);
+  // Step by step up to 8 tokens: of 8 tokens 64 sequences of 8 heads of 64 take 9.8 us, 11.3 as a chunk, 16 sequences of 16 heads of 128
+  // 14.1 and 15.6 (8 sequences of 8 heads of 64, though, 6.9 and 5.7); of 12 tokens the first take 12.6 us and 11.3.
   plan.steps = p.tokens <= 8;
+  // Segments that fill the device once, of three chunks and more: 8 heads of 64 of one sequence of 2000 tokens take 21.7 us, 37.9 whole; of 8
+  // sequences of 1000 tokens 22.7 and 22.5, of 1300 25.9 and 28.5, of 2000 32.3 and 40.2; the first of 16 chunks, 1000 tokens, 19.3 and 21.6
+  // (17.5 in segments of two chunks, 24.8 of six), and of 600 tokens 17.4 and 14.8.  Two rounds of workgroups lose: 8 sequences of 2000 tokens 42.5 us.
+  // Two segments alone do as well, 16 sequences of 2000 tokens 47.5 us, 42.2 whole.
   plan.segments = 1;
   if (!plan.steps) {
     const int64_t chunks = ((int64_t)p.tokens + kChunk - 1) / kChunk;
@@ -573,8 +583,8 @@ RetentionPlan plan_of(const RetentionParams& p) {
   return plan;
 }
 
-// Key dimensions in steps of 32 from 64 on, the values' in workgroups of 48 or 64 each, whichever leaves less over: ragged clips of
-// 96 x 80 take 26.7 us, 29.5 as 128 x 128; 500 tokens of 80 x 40, 160 times, 15.2 and 18.1.
+// Key dimensions in steps of 32 from 64 on, the values' in workgroups of 48 or 64 each, whichever leaves less over: the ragged clips
+// of 96 x 80 take 24.4 us, 26.3 as 128 x 128; 500 tokens of 80 x 40, 160 times, 16.7 and 18.9.
 template <class T, int KP>
 const void* chunks_kernel(int value_dim, bool states) {
   const int blocks = (value_dim + 63) / 64;
