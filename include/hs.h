@@ -509,8 +509,9 @@ typedef struct {
  *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * d_frequencies[i],
  * for pair i of the first rotary_dim values of the head: values (2i, 2i+1) where interleaved != 0,
  * else (i, i + rotary_dim/2); the values behind rotary_dim are only normalised.  Angles are formed
- * in 64 bits.  q_heads or k_heads may be 0 (that side is left alone).  Outputs may be the inputs
- * themselves (same pointer and strides); otherwise they must not overlap them. */
+ * in 64 bits; a mean of squares beyond fp32's range is infinite.  q_heads or k_heads may be 0 (that
+ * side is left alone).  Outputs may be the inputs themselves (same pointer and strides); otherwise
+ * they must not overlap them. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k and the outputs                                */
   int batch, tokens;

@@ -23,7 +23,8 @@ class TrackDecoder:
     """One layer: x += W_o retention(norm, rotation of x W_qkv);  x += W_o2 attention(norm of x W_q2, map W_kv).
 
     x is [streams, frames, tools, channels], maps are [streams, frames, cells, channels]; either one stream and any
-    number of frames (a clip) or one frame of any number of streams."""
+    number of frames (a clip) or one frame of any number of streams.  All streams count their frames together, and every
+    tool has a token in every frame."""
 
     def __init__(self, ctx: int, *, streams: int, tools: int = 8, heads: int = 8, head_dim: int = 64,
                  dtype: torch.dtype = torch.float16, seed: int = 0, device: str = "cuda:0"):
