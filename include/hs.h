@@ -591,6 +591,111 @@ typedef struct {
 hs_status hs_query_cross_attention_workspace(const hs_cross_attention_desc* desc, size_t* bytes);
 hs_status hs_cross_attention(hs_ctx* ctx, const hs_cross_attention_desc* desc, void* hip_stream);
 
+/* Linear attention whose state gives up what it holds for a key before it takes the key's new value (gated delta
+ * rule): with gates g_t = exp(log_decay_t) and beta_t of each token and head,
+ *   u_t = beta_t * (v_t - g_t * S_(t-1)^T k_t)
+ *   S_t = g_t * S_(t-1) + k_t u_t^T             S_0 = state_in, [key_dim][value_dim] fp32
+ *   out_t = scale * S_t^T q_t
+ * for the first lengths[b] tokens of sequence b, as hs_retention: state_out is the state behind the sequence's last
+ * token, out is zero for the tokens behind it, whose q, k, v and gates are not used whatever they hold; one call serves
+ * a clip or one frame of every live stream.  There is a state for each of `heads` value heads; head h has the query and
+ * key of head h / (heads / qk_heads).  Keys are used as they are: of length 1 (hs_norm_rotate with a weight of
+ * 1 / sqrt(key_dim)) and beta in [0, 1] the state stays bounded; with longer ones it grows as the formula has it.
+ * The state and what enters it are fp32 or, where they go through the matrix pipe, carry 24 bits; queries are multiplied by
+ * as much.  A clip cut into calls carries the same state up to the order of these sums.
+ * Columns of the state (value dimensions) are apart: what is not finite in a value stays in its column, of the
+ * outputs and the state, from its token on; in a key, a gate or a column of the state, every value from there on
+ * is infinite or NaN that would be by the formula (which of the two is open); in a query, that token's outputs.  Finite
+ * results do not change.  Calls of more than 8 tokens go over the affected parts of a sequence token by token. */
+typedef struct {
+  const float* d;               /* DEVICE, 4-byte aligned: first value of batch 0, token 0, head 0 */
+  int64_t batch, token, head;   /* strides in elements: any                                        */
+} hs_gates;
+typedef struct {
+  int dtype;                    /* hs_dtype of q, k, v, out                                        */
+  int batch, tokens;
+  int heads, qk_heads;          /* of v, out, gates and state; of q and k: a divisor of heads      */
+  int key_dim, value_dim;
+  float scale;
+  hs_heads q, k, v, out;
+  hs_gates log_decay;           /* natural logarithm of g, at most 0 in use (minus infinity: g = 0); d NULL: g = 1 */
+  hs_gates beta;                /* d NULL: 1                                                       */
+  const int32_t* d_lengths;     /* DEVICE [batch] or NULL                                          */
+  const float* d_state_in;      /* DEVICE [batch][heads][key_dim][value_dim], NULL: zeros; may be state_out */
+  float* d_state_out;           /* DEVICE, same shape                                              */
+  void* d_workspace;            /* DEVICE, 256-byte aligned                                        */
+  size_t workspace_bytes;
+} hs_delta_rule_desc;
+/* As hs_query_retention_workspace. */
+hs_status hs_query_delta_rule_workspace(const hs_delta_rule_desc* desc, size_t* bytes);
+hs_status hs_delta_rule(hs_ctx* ctx, const hs_delta_rule_desc* desc, void* hip_stream);
+
+/* Attention to an encoder's states by the difference of two softmax maps (what both maps have in common, the
+ * unspecific part, goes):
+ *   y = softmax(scale * q_0 K_0^T) V - lambda[h] * softmax(scale * q_1 K_1^T) V     over the visible keys
+ *   out = y                                                                           (norm == 0)
+ *   out = y / sqrt(mean(y^2) + eps) * weight                                          (norm != 0)
+ * q has 2 * q_heads heads, q_0 and q_1 of head h being heads 2h and 2h + 1, k has 2 * kv_heads likewise, v has kv_heads
+ * and out q_heads heads; head h has the keys and values of head h / (q_heads / kv_heads).  Visible keys as in
+ * hs_cross_attention (lengths, mask; hidden keys and values are not used whatever they hold); a token that sees no key gets zeros.
+ * The difference is formed and normalised in fp32. */
+typedef struct {
+  int dtype;                    /* hs_dtype of q, k, v, out                                        */
+  int batch, q_tokens, k_tokens;
+  int q_heads, kv_heads;        /* heads of out and of v                                           */
+  int head_dim, value_dim;      /* of q and k; of v and out                                        */
+  float scale;
+  hs_heads q, k, v, out;
+  const float* d_lambda;        /* DEVICE [q_heads]                                                */
+  int norm;
+  float eps;                    /* >= 0                                                            */
+  const float* d_norm_weight;   /* DEVICE [value_dim], NULL: ones                                  */
+  const int32_t* d_lengths;     /* DEVICE [batch] or NULL                                          */
+  const uint8_t* d_mask;        /* DEVICE, key j of batch b: d_mask[b*mask_batch_stride + j], or NULL */
+  int64_t mask_batch_stride;    /* 0: one mask for all                                             */
+  void* d_workspace;            /* DEVICE, 256-byte aligned                                        */
+  size_t workspace_bytes;
+} hs_differential_attention_desc;
+/* As hs_query_retention_workspace. */
+hs_status hs_query_differential_attention_workspace(const hs_differential_attention_desc* desc, size_t* bytes);
+hs_status hs_differential_attention(hs_ctx* ctx, const hs_differential_attention_desc* desc, void* hip_stream);
+
+/* A layer of small networks (experts) of which each token passes through the few that a router picks, for the
+ * tokens of one frame of all live streams:
+ *   s = router x;  the `top` experts with the largest s (ties: the lower index), e_1 first
+ *   p_i = exp(s[e_i]) / sum of exp(s) over all experts, or over the chosen ones      (renormalise != 0)
+ *   out = sum of p_i * W_out[e_i] (silu(W_gate[e_i] x) * (W_up[e_i] x)),   silu(a) = a / (1 + exp(-a))
+ * Scores are compared as summed in 64 bits.  The products' sums are fp32, what the second product takes is rounded to the
+ * inputs' type once (in fp16 with a power of two out of each token's row, so that it keeps its bits down to 2^-28 of the
+ * row's largest).  Tokens with mask 0 pass through none, whatever they hold: out zero, chosen -1, weights 0.  A
+ * token that is not finite changes no other token's output.  A score of NaN ranks last. */
+typedef struct {
+  int dtype;                    /* hs_dtype of x, out and the weights                              */
+  int tokens;                   /* 0 .. HS_MAX_EXPERT_TOKENS                                       */
+  int channels, hidden;         /* multiples of 8, 8 .. HS_MAX_CHANNELS                            */
+  int experts, top;             /* 1 .. HS_MAX_EXPERTS; 1 .. HS_MAX_TOP, at most experts           */
+  int renormalise;
+  const void* d_x;              /* DEVICE, token t: d_x + t * x_stride, channels side by side      */
+  int64_t x_stride;             /* in elements, a multiple of 8; 0 and negative ones are allowed    */
+  void* d_out;                  /* DEVICE, rows must not overlap each other nor an input           */
+  int64_t out_stride;
+  const void* d_router;         /* DEVICE [experts][channels]                                      */
+  const void* d_w_in;           /* DEVICE [experts][2][hidden][channels]: W_gate, W_up             */
+  const void* d_w_out;          /* DEVICE [experts][channels][hidden]                              */
+  const uint8_t* d_mask;        /* DEVICE [tokens], NULL: all ones                                 */
+  int32_t* d_chosen;            /* DEVICE [tokens][top]: e_1, e_2, .., or NULL                     */
+  float* d_weights;             /* DEVICE [tokens][top]: p_1, p_2, .., or NULL                     */
+  void* d_workspace;            /* DEVICE, 256-byte aligned                                        */
+  size_t workspace_bytes;
+} hs_expert_layer_desc;
+#define HS_MAX_EXPERT_TOKENS 1024
+#define HS_MAX_CHANNELS 16384
+#define HS_MAX_EXPERTS 256
+#define HS_MAX_TOP 8
+/* As hs_query_retention_workspace. */
+hs_status hs_query_expert_layer_workspace(const hs_expert_layer_desc* desc, size_t* bytes);
+hs_status hs_expert_layer(hs_ctx* ctx, const hs_expert_layer_desc* desc, void* hip_stream);
+
 /* Thread-local, never NULL; valid until the next failing call on this thread. */
 const char* hs_last_error(void);
 /* Library version string. */

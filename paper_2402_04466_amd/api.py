@@ -26,6 +26,10 @@ __all__ = [
     "HS_MAX_GROUP", "hs_feed", "hs_run_feeds", "hs_create_mux", "hs_destroy_mux", "hs_mux_submit",
     "hs_mux_poll", "hs_mux_wait", "hs_latency_metrics_compute", "hs_mann_whitney_u", "hs_set_cpu_affinity", "hs_set_kernel_timing", "hs_set_launch_mode", "HS_LAUNCH_GRAPH", "HS_LAUNCH_EAGER",
     "hs_get_kernel_times", "hs_device_copy", "hs_partition_copy", "hs_last_error", "hs_version", "make_desc", "cu_mask_words",
+    "HS_MAX_EXPERT_TOKENS", "HS_MAX_CHANNELS", "HS_MAX_EXPERTS", "HS_MAX_TOP", "hs_gates", "hs_delta_rule_desc",
+    "hs_differential_attention_desc", "hs_expert_layer_desc", "hs_query_delta_rule_workspace", "hs_delta_rule",
+    "hs_query_differential_attention_workspace", "hs_differential_attention", "hs_query_expert_layer_workspace",
+    "hs_expert_layer", "make_delta_rule_desc", "make_differential_attention_desc", "make_expert_layer_desc",
     "HS_F16", "HS_BF16", "HS_MAX_HEADS", "hs_heads", "hs_norm_rotate_desc", "hs_retention_desc", "hs_cross_attention_desc",
     "hs_norm_rotate", "hs_query_retention_workspace", "hs_retention", "hs_query_cross_attention_workspace",
     "hs_cross_attention", "make_norm_rotate_desc", "make_retention_desc", "make_cross_attention_desc",
@@ -38,6 +42,7 @@ HS_NUM_TOOLS, HS_MAX_CU_WORDS = 8, 8
 HS_LAUNCH_GRAPH, HS_LAUNCH_EAGER = 0, 1
 HS_MAX_GROUP = 4
 HS_F16, HS_BF16 = 1, 2
+HS_MAX_EXPERT_TOKENS, HS_MAX_CHANNELS, HS_MAX_EXPERTS, HS_MAX_TOP = 1024, 16384, 256, 8
 HS_MAX_HEADS = 64
 
 _STATUS_NAME = {0: "HS_OK", -1: "HS_E_INVAL", -2: "HS_E_NOMEM", -3: "HS_E_OVERSUBSCRIBED",
@@ -127,6 +132,42 @@ class hs_cross_attention_desc(C.Structure):
     ]
 
 
+class hs_gates(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class hs_delta_rule_desc(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("batch", C.c_int), ("tokens", C.c_int), ("heads", C.c_int),
+        ("qk_heads", C.c_int), ("key_dim", C.c_int), ("value_dim", C.c_int), ("scale", C.c_float),
+        ("q", hs_heads), ("k", hs_heads), ("v", hs_heads), ("out", hs_heads), ("log_decay", hs_gates),
+        ("beta", hs_gates), ("d_lengths", C.c_void_p), ("d_state_in", C.c_void_p),
+        ("d_state_out", C.c_void_p), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class hs_differential_attention_desc(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("batch", C.c_int), ("q_tokens", C.c_int), ("k_tokens", C.c_int),
+        ("q_heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("value_dim", C.c_int),
+        ("scale", C.c_float), ("q", hs_heads), ("k", hs_heads), ("v", hs_heads), ("out", hs_heads),
+        ("d_lambda", C.c_void_p), ("norm", C.c_int), ("eps", C.c_float), ("d_norm_weight", C.c_void_p),
+        ("d_lengths", C.c_void_p), ("d_mask", C.c_void_p), ("mask_batch_stride", C.c_int64),
+        ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class hs_expert_layer_desc(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int), ("tokens", C.c_int), ("channels", C.c_int), ("hidden", C.c_int),
+        ("experts", C.c_int), ("top", C.c_int), ("renormalise", C.c_int), ("d_x", C.c_void_p),
+        ("x_stride", C.c_int64), ("d_out", C.c_void_p), ("out_stride", C.c_int64),
+        ("d_router", C.c_void_p), ("d_w_in", C.c_void_p), ("d_w_out", C.c_void_p), ("d_mask", C.c_void_p),
+        ("d_chosen", C.c_void_p), ("d_weights", C.c_void_p), ("d_workspace", C.c_void_p),
+        ("workspace_bytes", C.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -206,6 +247,12 @@ def load() -> C.CDLL:
         "hs_norm_rotate": (C.c_int, [C.c_void_p, P(hs_norm_rotate_desc), C.c_void_p]),
         "hs_query_retention_workspace": (C.c_int, [P(hs_retention_desc), P(C.c_size_t)]),
         "hs_retention": (C.c_int, [C.c_void_p, P(hs_retention_desc), C.c_void_p]),
+        "hs_query_delta_rule_workspace": (C.c_int, [P(hs_delta_rule_desc), P(C.c_size_t)]),
+        "hs_delta_rule": (C.c_int, [C.c_void_p, P(hs_delta_rule_desc), C.c_void_p]),
+        "hs_query_differential_attention_workspace": (C.c_int, [P(hs_differential_attention_desc), P(C.c_size_t)]),
+        "hs_differential_attention": (C.c_int, [C.c_void_p, P(hs_differential_attention_desc), C.c_void_p]),
+        "hs_query_expert_layer_workspace": (C.c_int, [P(hs_expert_layer_desc), P(C.c_size_t)]),
+        "hs_expert_layer": (C.c_int, [C.c_void_p, P(hs_expert_layer_desc), C.c_void_p]),
         "hs_query_cross_attention_workspace": (C.c_int, [P(hs_cross_attention_desc),
                                                          P(C.c_size_t)]),
         "hs_cross_attention": (C.c_int, [C.c_void_p, P(hs_cross_attention_desc), C.c_void_p]),
@@ -627,3 +674,68 @@ def hs_query_cross_attention_workspace(desc: hs_cross_attention_desc) -> int:
 
 def hs_cross_attention(ctx: int, desc: hs_cross_attention_desc, hip_stream: int = 0) -> None:
     _check(load().hs_cross_attention(ctx, C.byref(desc), hip_stream))
+
+
+def make_delta_rule_desc(*, dtype, batch, tokens, heads, qk_heads, key_dim, value_dim, scale, q=None, k=None,
+                         v=None, out=None, log_decay=None, beta=None, d_lengths=0, d_state_in=0,
+                         d_state_out=0, d_workspace=0, workspace_bytes=0) -> hs_delta_rule_desc:
+    """log_decay, beta: hs_gates (device pointer and strides) or None."""
+    none = hs_heads()
+    return hs_delta_rule_desc(
+        int(dtype), int(batch), int(tokens), int(heads), int(qk_heads), int(key_dim), int(value_dim),
+        float(scale), q or none, k or none, v or none, out or none, log_decay or hs_gates(),
+        beta or hs_gates(), d_lengths or None, d_state_in or None, d_state_out or None,
+        d_workspace or None, int(workspace_bytes))
+
+
+def make_differential_attention_desc(*, dtype, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim,
+                                     value_dim, scale, q=None, k=None, v=None, out=None, d_lambda=0,
+                                     norm=True, eps=1e-5, d_norm_weight=0, d_lengths=0, d_mask=0,
+                                     mask_batch_stride=0, d_workspace=0,
+                                     workspace_bytes=0) -> hs_differential_attention_desc:
+    none = hs_heads()
+    return hs_differential_attention_desc(
+        int(dtype), int(batch), int(q_tokens), int(k_tokens), int(q_heads), int(kv_heads), int(head_dim),
+        int(value_dim), float(scale), q or none, k or none, v or none, out or none, d_lambda or None,
+        int(bool(norm)), float(eps), d_norm_weight or None, d_lengths or None, d_mask or None,
+        int(mask_batch_stride), d_workspace or None, int(workspace_bytes))
+
+
+def make_expert_layer_desc(*, dtype, tokens, channels, hidden, experts, top, renormalise=True, d_x=0,
+                           x_stride=0, d_out=0, out_stride=0, d_router=0, d_w_in=0, d_w_out=0, d_mask=0,
+                           d_chosen=0, d_weights=0, d_workspace=0, workspace_bytes=0) -> hs_expert_layer_desc:
+    return hs_expert_layer_desc(
+        int(dtype), int(tokens), int(channels), int(hidden), int(experts), int(top),
+        int(bool(renormalise)), d_x or None, int(x_stride), d_out or None, int(out_stride),
+        d_router or None, d_w_in or None, d_w_out or None, d_mask or None, d_chosen or None,
+        d_weights or None, d_workspace or None, int(workspace_bytes))
+
+
+def hs_query_delta_rule_workspace(desc: hs_delta_rule_desc) -> int:
+    n = C.c_size_t()
+    _check(load().hs_query_delta_rule_workspace(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def hs_delta_rule(ctx: int, desc: hs_delta_rule_desc, hip_stream: int = 0) -> None:
+    _check(load().hs_delta_rule(ctx, C.byref(desc), hip_stream))
+
+
+def hs_query_differential_attention_workspace(desc: hs_differential_attention_desc) -> int:
+    n = C.c_size_t()
+    _check(load().hs_query_differential_attention_workspace(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def hs_differential_attention(ctx: int, desc: hs_differential_attention_desc, hip_stream: int = 0) -> None:
+    _check(load().hs_differential_attention(ctx, C.byref(desc), hip_stream))
+
+
+def hs_query_expert_layer_workspace(desc: hs_expert_layer_desc) -> int:
+    n = C.c_size_t()
+    _check(load().hs_query_expert_layer_workspace(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def hs_expert_layer(ctx: int, desc: hs_expert_layer_desc, hip_stream: int = 0) -> None:
+    _check(load().hs_expert_layer(ctx, C.byref(desc), hip_stream))

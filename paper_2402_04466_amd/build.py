@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libhs.so")
 
 SOURCES = ["hs_host.cpp", "hs_lib.cpp", "hs_driver.cpp", "hs_track.cpp", "hs_kernels.hip",
-           "hs_norm_rotate.hip", "hs_retention.hip", "hs_cross_attention.hip"]
+           "hs_norm_rotate.hip", "hs_retention.hip", "hs_cross_attention.hip",
+           "hs_delta_rule.hip", "hs_differential_attention.hip", "hs_expert_layer.hip"]
 
 
 def hipcc() -> str:

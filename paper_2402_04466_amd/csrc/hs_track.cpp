@@ -245,6 +245,124 @@ CrossParams params_of(const hs_cross_attention_desc* d) {
   return p;
 }
 
+// ---- delta rule ----------------------------------------------------------------------------------
+hs_status check(const char* fn, const hs_delta_rule_desc* d) {   // all but the pointers
+  if (!d) { set_error("%s: NULL description", fn); return HS_E_INVAL; }
+  HS_TRY(check_type(fn, d->dtype));
+  HS_TRY(check_sizes(fn, d->batch, d->tokens, 0));
+  if (d->heads < 1 || d->qk_heads < 1 || d->heads % d->qk_heads) {
+    set_error("%s: heads (%d) must be a positive multiple of qk_heads (%d)", fn, d->heads, d->qk_heads);
+    return HS_E_INVAL;
+  }
+  HS_TRY(check_dim(fn, "key_dim", d->key_dim));
+  HS_TRY(check_dim(fn, "value_dim", d->value_dim));
+  if (!std::isfinite(d->scale)) { set_error("%s: scale must be finite", fn); return HS_E_INVAL; }
+  if ((int64_t)d->batch * d->heads > INT32_MAX) {
+    set_error("%s: too many heads of sequences for one call (%d x %d)", fn, d->batch, d->heads);
+    return HS_E_INVAL;
+  }
+  return HS_OK;
+}
+
+DeltaParams params_of(const hs_delta_rule_desc* d) {
+  DeltaParams p = {};
+  p.q = view(d->q); p.k = view(d->k); p.v = view(d->v); p.out = view(d->out);
+  p.log_decay = d->log_decay; p.beta = d->beta;
+  p.lengths = d->d_lengths;
+  p.state_in = d->d_state_in;
+  p.state_out = d->d_state_out;
+  p.dtype = d->dtype; p.batch = d->batch; p.tokens = d->tokens;
+  p.heads = d->heads; p.group = d->heads / d->qk_heads;
+  p.key_dim = d->key_dim; p.value_dim = d->value_dim;
+  p.scale = d->scale;
+  p.parts = d->d_workspace;
+  return p;
+}
+
+// ---- differential attention ----------------------------------------------------------------------
+hs_status check(const char* fn, const hs_differential_attention_desc* d) {   // all but the pointers
+  if (!d) { set_error("%s: NULL description", fn); return HS_E_INVAL; }
+  HS_TRY(check_type(fn, d->dtype));
+  HS_TRY(check_sizes(fn, d->batch, d->q_tokens, d->k_tokens));
+  HS_TRY(check_groups(fn, d->q_heads, d->kv_heads));
+  HS_TRY(check_dim(fn, "head_dim", d->head_dim));
+  HS_TRY(check_dim(fn, "value_dim", d->value_dim));
+  if (!std::isfinite(d->scale)) { set_error("%s: scale must be finite", fn); return HS_E_INVAL; }
+  if (d->norm && !(d->eps >= 0.0f && std::isfinite(d->eps))) {
+    set_error("%s: eps must be finite and >= 0", fn);
+    return HS_E_INVAL;
+  }
+  if ((int64_t)d->batch * d->q_heads * 2 > INT32_MAX) {
+    set_error("%s: too many heads of sequences for one call (%d x 2 x %d)", fn, d->batch, d->q_heads);
+    return HS_E_INVAL;
+  }
+  if ((int64_t)d->q_tokens * (d->q_heads / d->kv_heads) > INT32_MAX / 2 - 1024) {
+    set_error("%s: too many tokens for one call (%d, of %d heads each)", fn, d->q_tokens, d->q_heads / d->kv_heads);
+    return HS_E_INVAL;
+  }
+  return HS_OK;
+}
+
+DifferentialParams params_of(const hs_differential_attention_desc* d) {
+  DifferentialParams p = {};
+  p.q = view(d->q); p.k = view(d->k); p.v = view(d->v); p.out = view(d->out);
+  p.lambda = d->d_lambda;
+  p.weight = d->norm ? d->d_norm_weight : nullptr;
+  p.lengths = d->d_lengths;
+  p.mask = d->d_mask; p.mask_batch = d->mask_batch_stride;
+  p.dtype = d->dtype; p.batch = d->batch; p.q_tokens = d->q_tokens; p.k_tokens = d->k_tokens;
+  p.q_heads = d->q_heads; p.group = d->q_heads / d->kv_heads;
+  p.dim = d->head_dim; p.value_dim = d->value_dim;
+  p.norm = d->norm != 0; p.eps = d->eps;
+  p.scale = d->scale;
+  p.parts = (float*)d->d_workspace;
+  return p;
+}
+
+// ---- expert layer --------------------------------------------------------------------------------
+hs_status check_range(const char* fn, const char* name, int value, int least, int most, int step) {
+  if (value >= least && value <= most && value % step == 0) return HS_OK;
+  if (step > 1) set_error("%s: %s must be a multiple of %d in %d..%d, got %d", fn, name, step, least, most, value);
+  else set_error("%s: %s must be in %d..%d, got %d", fn, name, least, most, value);
+  return HS_E_INVAL;
+}
+
+hs_status check(const char* fn, const hs_expert_layer_desc* d) {   // all but the pointers
+  if (!d) { set_error("%s: NULL description", fn); return HS_E_INVAL; }
+  HS_TRY(check_type(fn, d->dtype));
+  HS_TRY(check_range(fn, "tokens", d->tokens, 0, HS_MAX_EXPERT_TOKENS, 1));
+  HS_TRY(check_range(fn, "channels", d->channels, 8, HS_MAX_CHANNELS, 8));
+  HS_TRY(check_range(fn, "hidden", d->hidden, 8, HS_MAX_CHANNELS, 8));
+  HS_TRY(check_range(fn, "experts", d->experts, 1, HS_MAX_EXPERTS, 1));
+  HS_TRY(check_range(fn, "top", d->top, 1, std::min(HS_MAX_TOP, d->experts), 1));
+  return HS_OK;
+}
+
+ExpertParams params_of(const hs_expert_layer_desc* d) {
+  ExpertParams p = {};
+  p.x = d->d_x; p.x_stride = d->x_stride;
+  p.out = d->d_out; p.out_stride = d->out_stride;
+  p.router = d->d_router; p.w_in = d->d_w_in; p.w_out = d->d_w_out;
+  p.mask = d->d_mask;
+  p.chosen = d->d_chosen; p.weights = d->d_weights;
+  p.dtype = d->dtype; p.tokens = d->tokens; p.channels = d->channels; p.hidden = d->hidden;
+  p.experts = d->experts; p.top = d->top; p.renormalise = d->renormalise != 0;
+  p.parts = (char*)d->d_workspace;
+  return p;
+}
+
+hs_status check_rows(const char* fn, const char* name, const void* d, int64_t stride) {
+  if (!d || !aligned(d, 16)) {
+    set_error("%s: %s must be a 16-byte aligned device pointer", fn, name);
+    return HS_E_INVAL;
+  }
+  if (stride % 8) {
+    set_error("%s: the stride of %s must be a multiple of 8 elements", fn, name);
+    return HS_E_INVAL;
+  }
+  return HS_OK;
+}
+
 }  // namespace
 }  // namespace hs
 
@@ -334,6 +452,109 @@ hs_status hs_cross_attention(hs_ctx* ctx, const hs_cross_attention_desc* desc, v
   HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, cross_workspace(params_of(desc))));
   HS_TRY(check_context(fn, ctx));
   if (!any) return HS_OK;
+  return run(fn, ctx, params_of(desc), hip_stream);
+  });
+}
+
+hs_status hs_query_delta_rule_workspace(const hs_delta_rule_desc* desc, size_t* bytes) {
+  const char* const fn = "hs_query_delta_rule_workspace";
+  return guarded(fn, [&]() -> hs_status {
+  if (!bytes) { set_error("%s: NULL bytes", fn); return HS_E_INVAL; }
+  HS_TRY(check(fn, desc));
+  *bytes = delta_workspace(params_of(desc));
+  return HS_OK;
+  });
+}
+
+hs_status hs_delta_rule(hs_ctx* ctx, const hs_delta_rule_desc* desc, void* hip_stream) {
+  const char* const fn = "hs_delta_rule";
+  return guarded(fn, [&]() -> hs_status {
+  HS_TRY(check(fn, desc));
+  if (desc->batch > 0) {
+    if (desc->tokens > 0) {
+      HS_TRY(check_heads(fn, "q", desc->q));
+      HS_TRY(check_heads(fn, "k", desc->k));
+      HS_TRY(check_heads(fn, "v", desc->v));
+      HS_TRY(check_output(fn, "out", desc->out, desc->batch, desc->tokens, desc->heads, desc->value_dim));
+      HS_TRY(check_pointer(fn, "log_decay", desc->log_decay.d, 4));
+      HS_TRY(check_pointer(fn, "beta", desc->beta.d, 4));
+    }
+    if (!desc->d_state_out) { set_error("%s: NULL d_state_out", fn); return HS_E_INVAL; }
+    HS_TRY(check_pointer(fn, "d_state_in", desc->d_state_in, 16));
+    HS_TRY(check_pointer(fn, "d_state_out", desc->d_state_out, 16));
+    HS_TRY(check_pointer(fn, "d_lengths", desc->d_lengths, 4));
+  }
+  HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, delta_workspace(params_of(desc))));
+  HS_TRY(check_context(fn, ctx));
+  if (desc->batch == 0) return HS_OK;
+  return run(fn, ctx, params_of(desc), hip_stream);
+  });
+}
+
+hs_status hs_query_differential_attention_workspace(const hs_differential_attention_desc* desc, size_t* bytes) {
+  const char* const fn = "hs_query_differential_attention_workspace";
+  return guarded(fn, [&]() -> hs_status {
+  if (!bytes) { set_error("%s: NULL bytes", fn); return HS_E_INVAL; }
+  HS_TRY(check(fn, desc));
+  *bytes = differential_workspace(params_of(desc));
+  return HS_OK;
+  });
+}
+
+hs_status hs_differential_attention(hs_ctx* ctx, const hs_differential_attention_desc* desc, void* hip_stream) {
+  const char* const fn = "hs_differential_attention";
+  return guarded(fn, [&]() -> hs_status {
+  HS_TRY(check(fn, desc));
+  const bool any = desc->batch > 0 && desc->q_tokens > 0;
+  if (any) {
+    HS_TRY(check_heads(fn, "q", desc->q));
+    if (desc->k_tokens > 0) {
+      HS_TRY(check_heads(fn, "k", desc->k));
+      HS_TRY(check_heads(fn, "v", desc->v));
+    }
+    HS_TRY(check_output(fn, "out", desc->out, desc->batch, desc->q_tokens, desc->q_heads, desc->value_dim));
+    if (!desc->d_lambda) { set_error("%s: NULL d_lambda", fn); return HS_E_INVAL; }
+    HS_TRY(check_pointer(fn, "d_lambda", desc->d_lambda, 4));
+    HS_TRY(check_pointer(fn, "d_norm_weight", desc->norm ? desc->d_norm_weight : nullptr, 4));
+    HS_TRY(check_pointer(fn, "d_lengths", desc->d_lengths, 4));
+  }
+  HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, differential_workspace(params_of(desc))));
+  HS_TRY(check_context(fn, ctx));
+  if (!any) return HS_OK;
+  return run(fn, ctx, params_of(desc), hip_stream);
+  });
+}
+
+hs_status hs_query_expert_layer_workspace(const hs_expert_layer_desc* desc, size_t* bytes) {
+  const char* const fn = "hs_query_expert_layer_workspace";
+  return guarded(fn, [&]() -> hs_status {
+  if (!bytes) { set_error("%s: NULL bytes", fn); return HS_E_INVAL; }
+  HS_TRY(check(fn, desc));
+  *bytes = expert_workspace(params_of(desc));
+  return HS_OK;
+  });
+}
+
+hs_status hs_expert_layer(hs_ctx* ctx, const hs_expert_layer_desc* desc, void* hip_stream) {
+  const char* const fn = "hs_expert_layer";
+  return guarded(fn, [&]() -> hs_status {
+  HS_TRY(check(fn, desc));
+  if (desc->tokens > 0) {
+    HS_TRY(check_rows(fn, "d_x", desc->d_x, desc->x_stride));
+    HS_TRY(check_rows(fn, "d_out", desc->d_out, desc->out_stride));
+    if (desc->tokens > 1 && desc->out_stride > -desc->channels && desc->out_stride < desc->channels) {
+      set_error("%s: rows of d_out overlap", fn);
+      return HS_E_INVAL;
+    }
+    HS_TRY(check_rows(fn, "d_router", desc->d_router, 0));
+    HS_TRY(check_rows(fn, "d_w_in", desc->d_w_in, 0));
+    HS_TRY(check_rows(fn, "d_w_out", desc->d_w_out, 0));
+    HS_TRY(check_pointer(fn, "d_chosen", desc->d_chosen, 4));
+    HS_TRY(check_pointer(fn, "d_weights", desc->d_weights, 4));
+  }
+  HS_TRY(check_workspace(fn, desc->d_workspace, desc->workspace_bytes, expert_workspace(params_of(desc))));
+  HS_TRY(check_context(fn, ctx));
+  if (desc->tokens == 0) return HS_OK;
   return run(fn, ctx, params_of(desc), hip_stream);
   });
 }

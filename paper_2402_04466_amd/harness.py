@@ -25,6 +25,13 @@ def heads_of(t: torch.Tensor) -> api.hs_heads:
     return api.hs_heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
 
 
+def gates_of(t: torch.Tensor) -> api.hs_gates:
+    """A float32 tensor [batch, tokens, heads] as the delta rule takes its gates."""
+    if t.dim() != 3 or t.dtype != torch.float32:
+        raise ValueError("need float32 [batch, tokens, heads]")
+    return api.hs_gates(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
 class AppStream:
     def __init__(self, ctx: int, *, net: int, frame_w: int, frame_h: int, net_w: int, net_h: int,
                  blob: np.ndarray, palette: np.ndarray, queue_depth: int = 2,
