@@ -25,29 +25,6 @@ namespace hs {
 // Large products (2040 tokens of 16 heads of 128 on 8160 keys, 8 times) take 1030 to 1080 us, 1.0 PFLOP/s: the matrix pipe is busy in
 // 51 % of the cycles, the vector pipe in 47 %, most of it exponentials.  Few rows are bound by their keys and values (8 tokens on up
 // to 6480 keys of 64, 96 heads: 3.8 TB/s in the first launch), the smallest by the chain of loads, products and join (7 us).
-constexpr float kLog2e = 1.44269504088896340736f;
-// A row's maximum is only raised, and what it has summed only rescaled, when the scores have grown by
-// more than this many powers of two: weights then stay below 2^8, as exact as weights below 1.
-constexpr float kSlack = 8.0f;
-// fp16 weights are formed 2^7 times as large, below 2^15 then: those of up to 2^-21 of the largest keep all their bits, and
-// what is lost of the others stays below 2^-32 of it.
-template <class T> constexpr float kRaise = __is_same(T, f16) ? 7.0f : 0.0f;
-constexpr float kLn2 = 0.69314718055994530942f;
-
-__device__ __forceinline__ float positive_scale(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale); }
-
-// The order of the products before it and of the LDS reads that they take one each: two groups of reads, then each group's products
-// before the reads of the one after next, so that none waits for a read that has only just been issued.
-template <int GROUP, int GROUPS>
-__device__ __forceinline__ void reads_ahead() {
-  __builtin_amdgcn_sched_group_barrier(0x100, 2 * GROUP, 0);
-#pragma unroll
-  for (int g = 0; g < GROUPS; ++g) {
-    __builtin_amdgcn_sched_group_barrier(0x8, GROUP, 0);
-    if (g + 2 < GROUPS) __builtin_amdgcn_sched_group_barrier(0x100, GROUP, 0);
-  }
-}
-
 struct CrossGrid {
   int row_tiles, splits;
 };

@@ -7,87 +7,466 @@
 
 namespace hs {
 
-// A wave per token and head: 64 keys at a time, a key per lane for the scores, two values per lane for the sums.
-template <class T>
-__global__ __launch_bounds__(64) void k_differential(DifferentialParams p) {
-  typedef typename Vec<T>::x8 x8;
-  __shared__ float q[2][128], w[2][64];
-  const int lane = threadIdx.x;
-  const int64_t id = blockIdx.x;
-  const int h = id % p.q_heads, hk = h / p.group;
-  const int64_t token = id / p.q_heads % p.q_tokens, b = id / p.q_heads / p.q_tokens;
-  const int n = length_of(p.lengths, b, p.k_tokens);
-  for (int i = lane; i < 2 * p.dim; i += 64) q[i / p.dim][i % p.dim] = (float)at<T>(p.q, b, token, 2 * h + i / p.dim)[i % p.dim];
-  __syncthreads();
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {}, o[2][2] = {};
-  for (int64_t j0 = 0; j0 < n; j0 += 64) {
-    const int64_t j = j0 + lane;
-    const bool seen = j < n && (!p.mask || p.mask[b * p.mask_batch + j]);
-    const uint64_t visible = __ballot(seen);
-    if (!visible) continue;
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      float s = -INFINITY;
-      if (seen) {
-        const T* const k = at<T>(p.k, b, j, 2 * hk + a);
-        s = 0.0f;
-        for (int d = 0; d < p.dim; d += 8) {
-          const x8 kk = *(const x8*)(k + d);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s = fmaf((float)kk[i], q[a][d + i], s);
-        }
-        s *= p.scale;
-      }
-      float top = s;
-      for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-      const float raised = fmaxf(m[a], top), keep = m[a] == -INFINITY ? 0.0f : expf(m[a] - raised);
-      const float e = !seen ? 0.0f : expf(s - (raised == -INFINITY ? 0.0f : raised));
-      float sum = e;
-      for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-      l[a] = l[a] * keep + sum;
-      o[a][0] *= keep;
-      o[a][1] *= keep;
-      m[a] = raised;
-      w[a][lane] = e;
-    }
-    __syncthreads();
-    for (int i = 0; i < 64; ++i) {
-      if (!(visible >> i & 1)) continue;
-      const T* const v = at<T>(p.v, b, j0 + i, hk);
-#pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        if (lane + 64 * d >= p.value_dim) continue;
-        const float x = (float)v[lane + 64 * d];
-        o[0][d] = fmaf(w[0][i], x, o[0][d]);
-        o[1][d] = fmaf(w[1][i], x, o[1][d]);
-      }
-    }
-    __syncthreads();
-  }
-  const float lambda = p.lambda[h];
-  float y[2] = {}, square = 0.0f;
-  const bool none = l[0] == 0.0f && l[1] == 0.0f;
-#pragma unroll
-  for (int d = 0; d < 2; ++d)
-    if (!none && lane + 64 * d < p.value_dim) {
-      y[d] = o[0][d] / l[0] - lambda * (o[1][d] / l[1]);
-      square = fmaf(y[d], y[d], square);
-    }
-  for (int d = 1; d < 64; d *= 2) square += __shfl_xor(square, d);
-  const float inv = !p.norm ? 1.0f : none ? 0.0f : rsqrtf(square / (float)p.value_dim + p.eps);
-  T* const out = at_out<T>(p.out, b, token, h);
-#pragma unroll
-  for (int d = 0; d < 2; ++d)
-    if (lane + 64 * d < p.value_dim) out[lane + 64 * d] = (T)(y[d] * inv * (p.weight ? p.weight[lane + 64 * d] : 1.0f));
+// y = softmax(scale Q_0 K_0^T) V - lambda softmax(scale Q_1 K_1^T) V, out = y or its norm, by tiles of keys with a
+// running maximum and sum for each map.  As in hs_cross_attention a wave has 32 rows (a row is a token and one of the heads that
+// share keys), S^T = K Q^T leaves each row's scores in one lane pair, and O^T += V^T P^T takes them, rounded to 16 bits
+// once, from the lanes that have them.
+//
+// Many rows (MAPS = 2): QW waves have other rows and share the tiles; a wave forms both maps of its rows, so that each value
+// that it reads from LDS is used twice: with a map per wave LDS would be busy as long as the matrix pipe.
+// Few rows (MAPS = 1): the waves of a workgroup have the same rows; four take the keys in turn for the first map, four for
+// the second (half the registers, and twice the loads in flight), and are joined in LDS.  Where that leaves the device
+// idle the keys are cut further, over `splits` workgroups, which k_differential_join puts together.
+struct DifferentialGrid {
+  int row_tiles, splits;
+};
+
+// The sum over 16 lanes side by side, in each of them.
+__device__ __forceinline__ float sum16(float x) {
+  x += moved<0xb1>(x);                     // lane ^ 1
+  x += moved<0x4e>(x);                     // lane ^ 2
+  x += moved<0x141>(x);                    // 7 - lane
+  return x + moved<0x140>(x);              // 15 - lane
 }
 
-size_t differential_workspace(const DifferentialParams&) { return 0; }
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
+// What a row's values are multiplied by: its norm's inverse, 0 for a row that saw nothing.
+__device__ __forceinline__ float row_factor(const DifferentialParams& p, float squares, bool saw) {
+  return !saw ? 0.0f : p.norm ? rsqrtf(squares / (float)p.value_dim + p.eps) : 1.0f;
+}
+
+// a fa - b fb with both products rounded, so that equal maps leave nothing.
+template <class V>
+__device__ __forceinline__ V difference(V a, float fa, V b, float fb) {
+#pragma clang fp contract(off)
+  return a * fa - b * fb;
+}
+
+template <class T, int DP, int VP, int MAPS, int QW, int KW, int BN>
+__global__ __launch_bounds__(64 * QW * KW * (3 - MAPS), 2) void k_differential(DifferentialParams p, DifferentialGrid grid) {
+  typedef typename Vec<T>::x8 x8;
+  typedef typename Vec<T>::x4 x4;
+  constexpr int WAVES = QW * KW * (3 - MAPS);
+  constexpr int CK = DP > 64 ? 16 : 8, CV = VP > 64 ? 16 : 8, KS = DP / 16, DT = VP / 32, NB = BN / 32;   // CK, CV: 16-byte pieces per row in LDS
+  constexpr int NT = 64 * QW;                       // threads that fill a tile together
+  constexpr int NK = BN * CK / NT, NV = BN * CV / NT;   // 16-byte loads per thread for one map's keys, and for values
+  constexpr int kKeys = BN * CK * 16, kTile = MAPS * kKeys + BN * CV * 16;   // bytes
+  constexpr int kBuffers = QW > 1 ? 2 : 1;          // a wave alone needs no second buffer: its accesses are in order
+  constexpr int PT = VP + 4;                        // floats per row of a wave's part: reads and writes spread over the banks
+  constexpr int kTiles = WAVES / QW * kBuffers * kTile, kParts = MAPS == 1 ? WAVES * 32 * (PT + 2) * 4 : 0;
+  constexpr int kLds = kTiles > kParts ? kTiles : kParts;
+  __shared__ __align__(16) char lds[kLds];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qw = MAPS == 2 ? wave : 0, kw = MAPS == 2 ? 0 : wave >> 1, map = MAPS == 2 ? 0 : wave & 1;
+  const int row_in_wave = lane & 31, half = lane >> 5;
+  char* const tiles = lds + (MAPS == 2 ? 0 : wave * kTile);
+
+  // the workgroups of one batch and key head read the same keys: on the same XCD
+  int id = xcd_number();
+  const int row_tile = id % grid.row_tiles;
+  id /= grid.row_tiles;
+  const int split = id % grid.splits;
+  const int bh = id / grid.splits, kv_heads = p.q_heads / p.group, hk = bh % kv_heads, b = bh / kv_heads;
+  const uint32_t rows = (uint32_t)p.q_tokens * p.group, group = p.group;   // below 2^30
+  const uint32_t row = (row_tile * QW + qw) * 32 + row_in_wave;
+  const bool live = row < rows;
+  const uint32_t token = live ? row / group : 0;
+  const int head = hk * p.group + (live ? (int)(row - token * group) : 0);
+
+  // the keys of this workgroup: tiles first .. last - 1, of which group kw takes every KW-th
+  const int n = length_of(p.lengths, b, p.k_tokens);
+  const int all_tiles = (int)(((int64_t)n + BN - 1) / BN);
+  const int first = (int)((int64_t)all_tiles * split / grid.splits), last = (int)((int64_t)all_tiles * (split + 1) / grid.splits);
+
+  // the scale's sign, and a scale of zero, are taken into Q: maxima of scores are maxima of exponents
+  const float c = positive_scale(p.scale) * kLog2e;
+  x8 q[MAPS][KS];
+#pragma unroll
+  for (int a = 0; a < MAPS; ++a) {
+    const T* const src = at<T>(p.q, b, token, 2 * head + a + map);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      q[a][k] = x8{};
+      const int d0 = 16 * k + 8 * half;
+      if (live && d0 < p.dim) q[a][k] = *(const x8*)(src + d0);
+      if (p.scale < 0.0f) q[a][k] = -q[a][k];
+      if (p.scale == 0.0f) q[a][k] = x8{};
+    }
+  }
+  f32x16 o[MAPS][DT] = {};
+  float m[MAPS], l[MAPS];
+#pragma unroll
+  for (int a = 0; a < MAPS; ++a) m[a] = -INFINITY, l[a] = 0.0f;
+
+  // staging: this thread's chunk of rows r0, r0 + NT / CK, ...  Rows behind the last key are read as that one, so that every
+  // tile's loads are the same instructions.
+  const int tg = threadIdx.x % NT, kr = tg / CK, kc = tg % CK, vr = tg / CV, vc = tg % CV;
+  const bool in_k = 8 * kc < p.dim, in_v = 8 * vc < p.value_dim;
+  const T* const ksrc = at<T>(p.k, b, 0, 2 * hk + map) + 8 * kc;
+  const T* const vsrc = at<T>(p.v, b, 0, hk) + 8 * vc;
+  const uint8_t* const mask = p.mask ? p.mask + b * p.mask_batch : nullptr;
+  s16x8 kreg[MAPS][NK] = {}, vreg[NV] = {};
+  uint8_t seen = 0;
+  auto fetch = [&](int tile) {
+    const int64_t j0 = (int64_t)tile * BN, end = (int64_t)n - 1;
+    const T *ka[NK], *va[NV];
+#pragma unroll
+    for (int e = 0; e < NK; ++e) ka[e] = ksrc + std::min(j0 + kr + e * (NT / CK), end) * p.k.token;
+#pragma unroll
+    for (int e = 0; e < NV; ++e) va[e] = vsrc + std::min(j0 + vr + e * (NT / CV), end) * p.v.token;
+    if (in_k) {
+#pragma unroll
+      for (int e = 0; e < NK; ++e)
+#pragma unroll
+        for (int a = 0; a < MAPS; ++a) kreg[a][e] = load16(ka[e] + a * p.k.head);
+    }
+    if (in_v) {
+#pragma unroll
+      for (int e = 0; e < NV; ++e) vreg[e] = load16(va[e]);
+    }
+    if (mask) seen = mask[std::min(j0 + (lane & (BN - 1)), end)];
+  };
+  // the tile's keys as a bit set, and its values in LDS: hidden values as zeros, whatever they hold
+  constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
+  auto store = [&](int tile, char* at_tile) -> uint64_t {
+    uint64_t visible = kAll;
+    const int64_t left = n - (int64_t)tile * BN;
+    if (left < BN) visible = (1ull << left) - 1;
+    if (mask) visible &= __ballot(seen != 0);
+    if (visible != kAll) {
+#pragma unroll
+      for (int e = 0; e < NV; ++e)
+        if (!(visible >> (vr + e * (NT / CV)) & 1)) vreg[e] = s16x8{};
+    }
+#pragma unroll
+    for (int e = 0; e < NK; ++e)
+#pragma unroll
+      for (int a = 0; a < MAPS; ++a) *(s16x8*)(at_tile + a * kKeys + slot<CK>(kr + e * (NT / CK), kc)) = kreg[a][e];
+#pragma unroll
+    for (int e = 0; e < NV; ++e) *(s16x8*)(at_tile + MAPS * kKeys + slot<CV>(vr + e * (NT / CV), vc)) = vreg[e];
+    return visible;
+  };
+  int koff[KS], voff[DT][2];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) koff[k] = slot<CK>(row_in_wave, 2 * k + half);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int r = 8 * s + 4 * half + (lane >> 2 & 3), cc = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+      voff[d][s] = MAPS * kKeys + slot<CV>(r, cc) + (lane & 1) * 8;
+    }
+
+  const int rounds = (last - first + KW - 1) / KW;
+  if (first + kw < last) fetch(first + kw);
+  for (int i = 0; i < rounds; ++i) {
+    const int tile = first + kw + i * KW;
+    char* const here = tiles + (kBuffers == 2 ? (i & 1) * kTile : 0);
+    uint64_t visible = 0;
+    if (tile < last) visible = store(tile, here);
+    if (QW > 1) __syncthreads();
+    if (tile + KW < last) fetch(tile + KW);
+    if (!visible) continue;
+
+#pragma unroll 1
+    for (int kb = 0; kb < NB; ++kb) {
+      const uint32_t bits = (uint32_t)(visible >> (32 * kb));
+      if (BN > 32 && !bits) continue;
+      x8 w[MAPS][2];                                 // the maps' weights: 16 keys each
+#pragma unroll
+      for (int a = 0; a < MAPS; ++a) {
+        const char* const at_k = here + a * kKeys + kb * 32 * CK * 16;
+        f32x16 s = {};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) s = mfma32(*(const x8*)(at_k + koff[k]), q[a][k], s);
+        if (bits != ~0u) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(bits >> (4 * half) >> (8 * (e / 4) + e % 4) & 1)) s[e] = -INFINITY;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        float lo, hi;
+        both_halves(top, lo, hi);
+        top = fmaxf(lo, hi);
+        if (__any((top - m[a]) * c > kSlack)) {
+          const float raised = fmaxf(m[a], top), keep = m[a] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m[a] - raised) * c);
+          l[a] *= keep;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[a][d] *= keep;
+          m[a] = raised;
+        }
+        const float mc = m[a] == -INFINITY ? 0.0f : fmaf(m[a], c, -kRaise<T>);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -mc));
+        float part[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[e] = (s[e] + s[4 + e]) + (s[8 + e] + s[12 + e]);
+        l[a] += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float w8[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w8[e] = s[8 * j + e];
+          w[a][j] = round8<T>(w8);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const char* const at_v = here + (32 * kb + 16 * j) * CV * 16;
+          const x8 v = join8<T>(read_transposed(at_v + voff[d][0]), read_transposed(at_v + voff[d][1]));
+#pragma unroll
+          for (int a = 0; a < MAPS; ++a) o[a][d] = mfma32(v, w[a][j], o[a][d]);
+        }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < MAPS; ++a) {
+    float lower, upper;
+    both_halves(l[a], lower, upper);
+    l[a] = lower + upper;
+  }
+
+  if (MAPS == 1) {   // the waves' parts of the same rows
+    float* const part_o = (float*)lds;
+    float* const part_ml = part_o + WAVES * 32 * PT;
+    __syncthreads();
+    if (live) {
+      if (half == 0) {
+        part_ml[2 * (wave * 32 + row_in_wave)] = m[0];
+        part_ml[2 * (wave * 32 + row_in_wave) + 1] = l[0];
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *(f32x4*)(part_o + (wave * 32 + row_in_wave) * PT + 32 * d + 2 * e + 4 * half) = f32x4{o[0][d][e], o[0][d][e + 1], o[0][d][e + 2], o[0][d][e + 3]};
+    }
+    __syncthreads();
+    // thread t: row t / 16, values 4 * (t % 16 + 16 * i)
+    const int r = threadIdx.x / 16;
+    const uint32_t at_row = row_tile * 32 + r;
+    if (at_row >= rows) return;
+    constexpr int NI = (VP + 63) / 64;
+    f32x4 sum[2][NI] = {};
+    float mm[2], ll[2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      mm[a] = -INFINITY;
+      ll[a] = 0.0f;
+#pragma unroll
+      for (int g = 0; g < KW; ++g) mm[a] = fmaxf(mm[a], part_ml[2 * ((2 * g + a) * 32 + r)]);
+#pragma unroll
+      for (int g = 0; g < KW; ++g) {
+        const int at_part = (2 * g + a) * 32 + r;
+        const float mg = part_ml[2 * at_part], f = mg == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mg - mm[a]) * c);
+        ll[a] = fmaf(part_ml[2 * at_part + 1], f, ll[a]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int d0 = 4 * (threadIdx.x % 16) + 64 * i;
+          if (d0 < VP) sum[a][i] += f * *(const f32x4*)(part_o + at_part * PT + d0);
+        }
+      }
+    }
+    const uint32_t tok = at_row / group;
+    const int hh = hk * p.group + (int)(at_row - tok * group);
+    if (grid.splits > 1) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        float* const part = p.parts + (((split * (int64_t)(p.batch * kv_heads) + bh) * rows + at_row) * 2 + a) * (p.value_dim + 4);
+        if (threadIdx.x % 16 == 0) {
+          part[0] = mm[a];
+          part[1] = ll[a];
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int d0 = 4 * (threadIdx.x % 16) + 64 * i;
+          if (d0 < p.value_dim) *(f32x4*)(part + 4 + d0) = sum[a][i];
+        }
+      }
+      return;
+    }
+    const float f0 = inverse_sum(ll[0]), f1 = p.lambda[hh] * inverse_sum(ll[1]);
+    float squares = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      sum[0][i] = difference(sum[0][i], f0, sum[1][i], f1);
+      if (4 * (threadIdx.x % 16) + 64 * i < p.value_dim)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) squares = fmaf(sum[0][i][e], sum[0][i][e], squares);
+    }
+    const float factor = row_factor(p, sum16(squares), ll[0] != 0.0f || ll[1] != 0.0f);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int d0 = 4 * (threadIdx.x % 16) + 64 * i;
+      if (d0 >= p.value_dim) break;
+      x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = (T)(sum[0][i][e] * factor * (p.weight ? p.weight[d0 + e] : 1.0f));
+      *(x4*)(at_out<T>(p.out, b, tok, hh) + d0) = y;
+    }
+    return;
+  }
+  if constexpr (MAPS == 2) {
+    if (grid.splits > 1) {
+      if (!live) return;
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        float* const part = p.parts + (((split * (int64_t)(p.batch * kv_heads) + bh) * rows + row) * 2 + a) * (p.value_dim + 4);
+        if (half == 0) {
+          part[0] = m[a];
+          part[1] = l[a];
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const int d0 = 32 * d + 2 * e + 4 * half;
+            if (d0 < p.value_dim) *(f32x4*)(part + 4 + d0) = f32x4{o[a][d][e], o[a][d][e + 1], o[a][d][e + 2], o[a][d][e + 3]};
+          }
+      }
+      return;
+    }
+    const float f0 = inverse_sum(l[0]), f1 = p.lambda[head] * inverse_sum(l[1]);
+    float squares = 0.0f;                            // (values behind the last are zero)
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      o[0][d] = difference(o[0][d], f0, o[1][d], f1);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) squares = fmaf(o[0][d][e], o[0][d][e], squares);
+    }
+    float lower, upper;
+    both_halves(squares, lower, upper);
+    const float factor = row_factor(p, lower + upper, l[0] != 0.0f || l[1] != 0.0f);
+    if (!live) return;
+    T* const dst = at_out<T>(p.out, b, token, head);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int d0 = 32 * d + 2 * e + 4 * half;
+        if (d0 >= p.value_dim) continue;
+        x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = (T)(o[0][d][e + i] * factor * (p.weight ? p.weight[d0 + i] : 1.0f));
+        *(x4*)(dst + d0) = y;
+      }
+  }
+}
+
+// The splits' parts of a row, for each map a maximum, a sum and a weighted sum of values: a wave per row.  Lane s has what weighs
+// part s; then the wave's halves take even and odd parts, four values per lane.
+constexpr int kMostParts = 64;
+template <class T>
+__global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p, int splits) {
+  typedef typename Vec<T>::x4 x4;
+  const int kv_heads = p.q_heads / p.group, lane = threadIdx.x & 63, half = lane >> 5;
+  const int64_t rows = (int64_t)p.q_tokens * p.group, all = (int64_t)p.batch * kv_heads * rows;
+  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  if (id >= all) return;
+  const float c = positive_scale(p.scale) * kLog2e;
+  const int64_t row = id % rows, bh = id / rows, b = bh / kv_heads, token = row / p.group;
+  const int head = (int)(bh % kv_heads) * p.group + (int)(row % p.group);
+  const int d0 = 4 * (lane & 31), pitch = p.value_dim + 4;
+  f32x4 y = {0, 0, 0, 0};
+  float first = 0.0f;
+  bool saw = false;
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    const float* const parts = p.parts + (id * 2 + a) * pitch;
+    float m = -INFINITY, l = 0.0f;
+    if (lane < splits) {
+      m = parts[lane * all * 2 * pitch];
+      l = parts[lane * all * 2 * pitch + 1];
+    }
+    float top = m;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c);
+    l *= f;                                         // (a part that saw no key has 0, one whose scores are NaN keeps that)
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+    f32x4 sum = {0, 0, 0, 0};
+    for (int s = 0; s < splits; s += 2) {
+      const float w = __shfl(f, s + half);          // (of a part that is not there, or saw no key: 0)
+      if (d0 < p.value_dim && w != 0.0f) sum += w * *(const f32x4*)(parts + (s + half) * all * 2 * pitch + 4 + d0);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], 32);
+    const float inv = inverse_sum(l);
+    if (a == 0) {
+      y = sum;
+      first = inv;
+    } else {
+      y = difference(y, first, sum, p.lambda[head] * inv);
+    }
+    saw = saw || l != 0.0f;
+  }
+  float squares = half ? 0.0f : fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3])));
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) squares += __shfl_xor(squares, d);
+  const float factor = row_factor(p, squares, saw);
+  if (half || d0 >= p.value_dim) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] *= factor * (p.weight ? p.weight[d0 + e] : 1.0f);
+  *(x4*)(at_out<T>(p.out, b, token, head) + d0) = round4<T>(y);
+}
+
+namespace {
+struct DifferentialPlan {
+  bool wide;                    // eight waves with 32 rows each and the same keys, else eight with the same rows
+  DifferentialGrid grid;
+  int64_t workgroups;
+};
+DifferentialPlan plan_of(const DifferentialParams& p) {
+  const int64_t bh = (int64_t)p.batch * (p.q_heads / p.group), rows = (int64_t)p.q_tokens * p.group;
+  DifferentialPlan plan;
+  const int64_t wide_tiles = (rows + 255) / 256, wide = bh * wide_tiles, keys64 = ((int64_t)p.k_tokens + 63) / 64;
+  auto at_most = [](int64_t room, int64_t base, int64_t parts) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({room / std::max<int64_t>(base, 1), parts, kMostParts}));
+  };
+  const int cut = at_most(256, wide, keys64 / 8);
+  const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, few = bh * ((rows + 31) / 32);
+  plan.wide = wide >= 256 || (2 * rows >= wide_tiles * 256 && wide * cut >= 192);
+  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? wide_tiles : (rows + 31) / 32, INT32_MAX);
+  plan.grid.splits = wide >= 256 ? 1 : cut;
+  if (!plan.wide) {
+    const int splits = at_most(512, few, tiles / 8);
+    const bool apart = (tiles + 4 * splits - 1) / (4 * splits) + 3 < (few + 255) / 256 * ((tiles + 3) / 4);
+    plan.grid.splits = apart ? splits : 1;
+  }
+  plan.workgroups = bh * plan.grid.row_tiles * plan.grid.splits;
+  return plan;
+}
+template <class T, int DP, int VP>
+const void* kernel_of(const DifferentialPlan& plan) {
+  return plan.wide ? (const void*)k_differential<T, DP, VP, 2, 8, 1, 64> : (const void*)k_differential<T, DP, VP, 1, 1, 4, 32>;
+}
+template <class T>
+const void* kernel_of(const DifferentialParams& p, const DifferentialPlan& plan) {
+  if (p.dim <= 64) return p.value_dim <= 64 ? kernel_of<T, 64, 64>(plan) : kernel_of<T, 64, 128>(plan);
+  return p.value_dim <= 64 ? kernel_of<T, 128, 64>(plan) : kernel_of<T, 128, 128>(plan);
+}
+}  // namespace
+
+size_t differential_workspace(const DifferentialParams& p) {
+  const DifferentialPlan plan = plan_of(p);
+  return plan.grid.splits == 1 ? 0 : (size_t)plan.grid.splits * p.batch * p.q_heads * p.q_tokens * 2 * (p.value_dim + 4) * sizeof(float);
+}
 
 hipError_t launch(const DifferentialParams& p, hipStream_t stream) {
   DifferentialParams params = p;
-  void* args[] = {&params};
-  return launch_kernel(p.dtype == HS_F16 ? (const void*)k_differential<f16> : (const void*)k_differential<bf16>,
-                       (int64_t)p.batch * p.q_tokens * p.q_heads, 64, args, stream);
+  DifferentialPlan plan = plan_of(p);
+  void* args[] = {&params, &plan.grid};
+  const bool half = p.dtype == HS_F16;
+  hipError_t e = launch_kernel(half ? kernel_of<f16>(p, plan) : kernel_of<bf16>(p, plan), plan.workgroups, 512, args, stream);
+  if (e != hipSuccess || plan.grid.splits == 1) return e;
+  void* join_args[] = {&params, &plan.grid.splits};
+  return launch_kernel(half ? (const void*)k_differential_join<f16> : (const void*)k_differential_join<bf16>,
+                       ((int64_t)p.batch * p.q_heads * p.q_tokens + 3) / 4, 256, join_args, stream);
 }
 
 }  // namespace hs
