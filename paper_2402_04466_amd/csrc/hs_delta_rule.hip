@@ -100,16 +100,502 @@ __global__ __launch_bounds__(256) void k_delta_steps(DeltaParams p) {
     for (int64_t t = n + g; t < p.tokens; t += 16) *(x4*)(out + t * p.out.token) = x4{};
 }
 
-size_t delta_workspace(const DeltaParams&) { return 0; }
+// ---- chunks of 32 tokens on the matrix pipe -------------------------------------------------------
+//
+// With L_i the sum of the decays' logarithms from the chunk's begin to token i, S the state before the chunk and
+// Gamma_ij = 2^(L_i - L_j), the recurrence's u of the chunk's tokens solve a triangular system,
+//   (1 + A) U = diag(beta) (V - diag(2^L) K S),     A_ij = beta_i Gamma_ij k_i.k_j for j < i,
+// and  out = scale (diag(2^L) Q S + P U),           P_ij = Gamma_ij q_i.k_j for j <= i,
+//      S'  = 2^L_end S + K^T diag(2^(L_end - L)) U.
+// M = (1 + A)^-1 diag(beta) and P do not depend on the state: two waves form them for the chunk to come, a third lays its
+// values and gates out, while the state's waves work on this one.  A state wave has all rows of 16 of the state's columns in
+// registers, and needs nothing of the others: in the layout in which products leave their results (rows 4g .. 4g + 3
+// of a column in lane group g) pairs of 16 rows are operands of the next product, once its other operand is read in the order of rows
+// 4g .. 4g + 3, 16 + 4g .. 16 + 4g + 3.
+//
+// Precision.  What enters the state is exact to 24 bits: the state and U go through the matrix pipe as three bf16 parts
+// (8 bits each, split by truncation, which is exact and cannot overflow), fp16 keys and queries as two, M in fp32.
+// Outputs, which are rounded to 16 bits, take two parts of each: 16 bits.
+constexpr int kChunk = 32, kStateWaves = 4, kOtherWaves = 3;
+constexpr int kMPitch = 36;                          // floats per row of M: 16 rows' same 16 bytes lie in different banks
+constexpr int kPPitch = 80;                          // bytes per row of P: as well
 
+typedef Vec<bf16>::x8 b8;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t bits_of(float x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ float upper_half(float x) { return __builtin_bit_cast(float, bits_of(x) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_upper(float even, float odd) { return __builtin_amdgcn_perm(bits_of(odd), bits_of(even), 0x07060302u); }
+
+// Eight values as PARTS bf16 vectors that add up to them (exactly, for three).
+template <int PARTS>
+__device__ __forceinline__ void split8(const float* x, b8* part) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+  for (int n = 0; n < PARTS; ++n) {
+    u32x4 words;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) words[i] = pack_upper(rest[2 * i], rest[2 * i + 1]);
+    part[n] = __builtin_bit_cast(b8, words);
+    if (n + 1 < PARTS)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rest[i] -= upper_half(rest[i]);
+  }
+}
+
+// The accesses of a wave to LDS before this come before those after it, whichever lane they are of.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+struct ChunkGates {                                  // of one chunk
+  float upto_hi[kChunk], upto_lo[kChunk];            // L in two parts
+  float since[kChunk], left[kChunk];                 // 2^L, 2^(L_end - L)
+  float beta[kChunk], decay[kChunk];                 // decay: g itself
+};
+
+struct DeltaGrid {
+  int blocks, waves;                                 // of 16 * waves value columns each
+};
+
+template <class T, int DK>
+__global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chunks(DeltaParams p, DeltaGrid grid) {
+  typedef typename Vec<T>::x8 x8;
+  typedef typename Vec<T>::x4 x4;
+  constexpr int NP = __is_same(T, f16) ? 2 : 1;      // bf16 parts of a key or query
+  constexpr int CH = DK > 64 ? 16 : 8, KS = DK / 32, ST = DK / 16;
+  constexpr int kTile = kChunk * CH * 16, kValues = kChunk * 8 * 16;
+  constexpr int kK = 0, kQ = NP * kTile, kV = 2 * NP * kTile, kM = kV + kValues, kP = kM + kChunk * kMPitch * 4;
+  constexpr int kBuffer = kP + 2 * kChunk * kPPitch;
+  __shared__ __align__(16) char lds[2 * kBuffer];
+  __shared__ ChunkGates gates[3];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = lane & 15, g = lane >> 4;
+  int id = xcd_number();
+  const int block = id % grid.blocks, bh = id / grid.blocks, h = bh % p.heads, hk = h / p.group, b = bh / p.heads;
+  const int n = length_of(p.lengths, b, p.tokens), chunks = (n + kChunk - 1) / kChunk;
+  const int column0 = 16 * grid.waves * block;
+  // roles: the state's waves first, then M, P, and values and gates
+  const int role = wave < grid.waves ? 0 : 1 + wave - grid.waves;
+
+  if (role == 0) {
+    const int column = column0 + 16 * wave + row;
+    const bool there = column < p.value_dim;
+    const int64_t state0 = (int64_t)bh * p.key_dim * p.value_dim + column;
+    f32x4 s[ST];
+#pragma unroll
+    for (int t = 0; t < ST; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = 16 * t + 4 * g + i;
+        s[t][i] = there && p.state_in && k < p.key_dim ? p.state_in[state0 + (int64_t)k * p.value_dim] : 0.0f;
+      }
+    int koff[KS][2], toff[ST], voff;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) koff[k][e] = slot<CH>(row, 4 * k + 2 * e + (g >> 1)) + (g & 1) * 8;
+#pragma unroll
+    for (int t = 0; t < ST; ++t) toff[t] = slot<CH>(4 * g + (row >> 2), 2 * t + (row >> 1 & 1)) + (row & 1) * 8;
+    voff = slot<8>(4 * g + (row >> 2), 2 * wave + (row >> 1 & 1)) + (row & 1) * 8;
+    constexpr int kNext = 16 * CH * 16, kNextV = 16 * 8 * 16;     // 16 tokens further
+    T* const out = at_out<T>(p.out, b, 0, h) + column0 + 16 * wave;
+    const bool stored = column0 + 16 * wave + 4 * g < p.value_dim;
+
+    __syncthreads();
+    __syncthreads();
+    for (int c = 0; c < chunks; ++c) {
+      const char* const here = lds + (c & 1) * kBuffer;
+      const ChunkGates& gate = gates[c % 3];
+      f32x4 ks[2] = {}, qs[2] = {};                  // K S: tokens x columns; (Q S)^T: columns x tokens
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = s[2 * k][i], x[4 + i] = s[2 * k + 1][i];
+        b8 part[3];
+        split8<3>(x, part);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+          b8 kk[NP], qq[NP];
+#pragma unroll
+          for (int e = 0; e < NP; ++e) {
+            const char* const at_k = here + kK + e * kTile + tt * kNext;
+            const char* const at_q = here + kQ + e * kTile + tt * kNext;
+            kk[e] = join8<bf16>(*(const s16x4*)(at_k + koff[k][0]), *(const s16x4*)(at_k + koff[k][1]));
+            qq[e] = join8<bf16>(*(const s16x4*)(at_q + koff[k][0]), *(const s16x4*)(at_q + koff[k][1]));
+          }
+          if (NP == 2) {
+            ks[tt] = mfma16(kk[NP - 1], part[1], ks[tt]);
+            ks[tt] = mfma16(kk[NP - 1], part[0], ks[tt]);
+            qs[tt] = mfma16(part[0], qq[NP - 1], qs[tt]);
+          }
+#pragma unroll
+          for (int e = 2; e >= 0; --e) ks[tt] = mfma16(kk[0], part[e], ks[tt]);
+#pragma unroll
+          for (int e = 1; e >= 0; --e) qs[tt] = mfma16(part[e], qq[0], qs[tt]);
+        }
+      }
+      f32x4 x[2], u[2] = {};
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const s16x4 raw = read_transposed(here + kV + voff + tt * kNextV);
+        const x4 v = __builtin_bit_cast(x4, raw);
+        const f32x4 since = *(const f32x4*)(gate.since + 16 * tt + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[tt][i] = (float)v[i] - since[i] * ks[tt][i];
+      }
+      const float* const m = (const float*)(here + kM) + row * kMPitch + 4 * g;
+      const f32x4 m00 = *(const f32x4*)m, m10 = *(const f32x4*)(m + 16 * kMPitch), m11 = *(const f32x4*)(m + 16 * kMPitch + 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(m00[i], x[0][i], u[0], 0, 0, 0);
+        u[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m10[i], x[0][i], u[1], 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m11[i], x[1][i], u[1], 0, 0, 0);
+
+      // Something is not finite: the recurrence says where it goes, token by token.
+      float most = 0.0f;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most += u[tt][i] * 0.0f;
+      if (__any(most != 0.0f)) {
+        const int here_n = min(kChunk, n - c * kChunk);
+        for (int j = 0; j < here_n; ++j) {
+          const float decay = gate.decay[j], beta = gate.beta[j];
+          float kt[ST][4], a = 0.0f, e = 0.0f;
+          auto value = [&](int tile, int t, int i) {
+            const int at_value = slot<CH>(j, 2 * t + (g >> 1)) + (g & 1) * 8 + 2 * i;
+            float y = (float)*(const bf16*)(here + tile + at_value);
+            if (NP == 2) y += (float)*(const bf16*)(here + tile + kTile + at_value);
+            return y;
+          };
+#pragma unroll
+          for (int t = 0; t < ST; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              kt[t][i] = value(kK, t, i);
+              if (16 * t + 4 * g + i < p.key_dim) a = fmaf(kt[t][i], s[t][i], a);
+            }
+          a += __shfl_xor(a, 16);
+          a += __shfl_xor(a, 32);
+          const float v = (float)*(const T*)(here + kV + slot<8>(j, 2 * wave + (row >> 3)) + (row & 7) * 2);
+          const float uj = beta * (v - decay * a);
+#pragma unroll
+          for (int t = 0; t < ST; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (16 * t + 4 * g + i >= p.key_dim) continue;
+              s[t][i] = fmaf(kt[t][i], uj, decay * s[t][i]);
+              e = fmaf(value(kQ, t, i), s[t][i], e);
+            }
+          e += __shfl_xor(e, 16);
+          e += __shfl_xor(e, 32);
+          if (g == 0 && there) out[(int64_t)(c * kChunk + j) * p.out.token + row] = (T)(p.scale * e);
+        }
+        __syncthreads();
+        continue;
+      }
+
+      float y[8];
+      b8 part[3];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = u[0][i], y[4 + i] = u[1][i];
+      split8<2>(y, part);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        f32x4 o = {0, 0, 0, 0};
+        const char* const at_p = here + kP + (16 * tt + row) * kPPitch + 16 * g;
+        const b8 hi = __builtin_bit_cast(b8, *(const s16x8*)at_p), lo = __builtin_bit_cast(b8, *(const s16x8*)(at_p + kChunk * kPPitch));
+        o = mfma16(part[1], hi, o);
+        o = mfma16(part[0], lo, o);
+        o = mfma16(part[0], hi, o);
+        const int token = c * kChunk + 16 * tt + row;
+        const float since = gate.since[16 * tt + row];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = p.scale * fmaf(since, qs[tt][i], o[i]);
+        if (token < n && stored) *(x4*)(out + (int64_t)token * p.out.token + 4 * g) = round4<T>(o);
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const f32x4 left = *(const f32x4*)(gate.left + 16 * tt + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[4 * tt + i] *= left[i];
+      }
+      split8<3>(y, part);
+      const float whole = gate.since[kChunk - 1];
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        f32x4 fresh = {0, 0, 0, 0};
+        b8 kk[NP];
+#pragma unroll
+        for (int e = 0; e < NP; ++e) {
+          const char* const at_k = here + kK + e * kTile + toff[t];
+          kk[e] = join8<bf16>(read_transposed(at_k), read_transposed(at_k + kNext));
+        }
+        if (NP == 2) {
+          fresh = mfma16(kk[NP - 1], part[1], fresh);
+          fresh = mfma16(kk[NP - 1], part[0], fresh);
+        }
+#pragma unroll
+        for (int e = 2; e >= 0; --e) fresh = mfma16(kk[0], part[e], fresh);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][i] = fmaf(whole, s[t][i], fresh[i]);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int t = 0; t < ST; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = 16 * t + 4 * g + i;
+        if (there && k < p.key_dim) p.state_out[state0 + (int64_t)k * p.value_dim] = s[t][i];
+      }
+    if (stored)
+      for (int64_t t = n + row; t < p.tokens; t += 16) *(x4*)(out + t * p.out.token + 4 * g) = x4{};
+    return;
+  }
+
+  if (role == 3) {   // values of chunk c + 1, gates of chunk c + 2
+    const T* const v = at<T>(p.v, b, 0, h) + column0;
+    const float* const log_decay = gate_at(p.log_decay, b, h);
+    const float* const beta = gate_at(p.beta, b, h);
+    s16x8 reg[4];
+    float l = 0.0f, be = 0.0f;
+    auto fetch_values = [&](int c) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at_row = e * 8 + (lane >> 3), ch = lane & 7;
+        const int64_t t = (int64_t)c * kChunk + at_row;
+        reg[e] = s16x8{};
+        if (t < n && ch < 2 * grid.waves && column0 + 8 * ch < p.value_dim) reg[e] = load16(v + t * p.v.token + 8 * ch);
+      }
+    };
+    auto fetch_gates = [&](int c) {
+      const int64_t t = (int64_t)c * kChunk + (lane & 31);
+      l = 0.0f;
+      be = 0.0f;
+      if (t < n) {
+        if (log_decay) l = log_decay[t * p.log_decay.token];
+        be = beta ? beta[t * p.beta.token] : 1.0f;
+      }
+    };
+    fetch_gates(0);
+    for (int c = -2; c < chunks; ++c) {
+      if (c + 2 < chunks) {
+        ChunkGates& gate = gates[(c + 2) % 3];
+        // A decay of zero is 2^-10000 here: nothing of it is left in 32 bits, and no infinity enters the sums.
+        double upto = (double)l * 1.4426950408889634074;
+        if (upto < -1e4) upto = -1e4;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+          const double before = __shfl_up(upto, d, 32);
+          if ((lane & 31) >= d) upto += before;
+        }
+        const double end = __shfl(upto, 31, 32);
+        const float hi = (float)upto;
+        if (lane < 32) {
+          gate.upto_hi[lane] = hi;
+          gate.upto_lo[lane] = (float)(upto - (double)hi);
+          gate.since[lane] = exp2f(hi);
+          gate.left[lane] = exp2f((float)(end - upto));
+          gate.beta[lane] = be;
+          gate.decay[lane] = expf(l);
+        }
+        fetch_gates(c + 3);
+      }
+      if (c + 1 >= 0 && c + 1 < chunks) {
+        char* const next = lds + ((c + 1) & 1) * kBuffer + kV;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *(s16x8*)(next + slot<8>(e * 8 + (lane >> 3), lane & 7)) = reg[e];
+      }
+      if (c + 2 < chunks) fetch_values(c + 2);
+      __syncthreads();
+    }
+    return;
+  }
+
+  // M (role 1) and P (role 2) of chunk c + 1, and its keys, or queries, in LDS
+  const T* const key = at<T>(p.k, b, 0, hk);
+  const T* const query = at<T>(p.q, b, 0, hk);
+  x8 kk[2][KS], qq[2][KS];
+  auto fetch_rows = [&](const T* from, int64_t stride, int c, x8 (&to)[2][KS]) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const int64_t t = (int64_t)c * kChunk + 16 * tt + row;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const int d0 = 32 * k + 8 * g;
+        to[tt][k] = x8{};
+        if (t < n && d0 < p.key_dim) to[tt][k] = __builtin_bit_cast(x8, load16(from + t * stride + d0));
+      }
+    }
+  };
+  auto lay_out = [&](const x8 (&from)[2][KS], char* to) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        char* const at_row = to + slot<CH>(16 * tt + row, 4 * k + g);
+        if (NP == 1) {
+          *(s16x8*)at_row = __builtin_bit_cast(s16x8, from[tt][k]);
+        } else {
+          float x[8];
+          b8 part[2];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = (float)from[tt][k][i];
+          split8<2>(x, part);
+          *(s16x8*)at_row = __builtin_bit_cast(s16x8, part[0]);
+          *(s16x8*)(at_row + kTile) = __builtin_bit_cast(s16x8, part[1]);
+        }
+      }
+  };
+  // Gamma_ij of token i = 16 it + row and tokens j = 16 jt + 4 g + 0 .. 3
+  auto gamma = [&](const ChunkGates& gate, int it, int jt) {
+    const float hi = gate.upto_hi[16 * it + row], lo = gate.upto_lo[16 * it + row];
+    const f32x4 hj = *(const f32x4*)(gate.upto_hi + 16 * jt + 4 * g), lj = *(const f32x4*)(gate.upto_lo + 16 * jt + 4 * g);
+    f32x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = exp2f((hi - hj[i]) + (lo - lj[i]));
+    return y;
+  };
+  if (role == 1) {
+    if (chunks > 0) fetch_rows(key, p.k.token, 0, kk);
+    __syncthreads();
+    for (int c = -1; c < chunks; ++c) {
+      if (c + 1 < chunks) {
+        char* const next = lds + ((c + 1) & 1) * kBuffer;
+        const ChunkGates& gate = gates[(c + 1) % 3];
+        lay_out(kk, next + kK);
+        float* const m = (float*)(next + kM);
+#pragma unroll
+        for (int tile = 0; tile < 3; ++tile) {       // (it, jt) = (0, 0), (1, 0), (1, 1)
+          const int it = tile > 0, jt = tile > 1;
+          f32x4 d = {0, 0, 0, 0};
+#pragma unroll
+          for (int k = 0; k < KS; ++k) d = mfma16(kk[jt][k], kk[it][k], d);
+          const f32x4 w = gamma(gate, it, jt);
+          const float beta = gate.beta[16 * it + row];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[i] = it == jt && 4 * g + i >= row ? 0.0f : beta * w[i] * d[i];
+          *(f32x4*)(m + (16 * it + row) * kMPitch + 16 * jt + 4 * g) = d;
+        }
+        if (c + 2 < chunks) fetch_rows(key, p.k.token, c + 2, kk);
+        wave_order();
+        // the inverses of the diagonal blocks, a column per lane: lanes 0 .. 15 of the first, 16 .. 31 of the second
+        float* const diagonal = m + (lane >> 4 & 1) * (16 * kMPitch + 16);
+        const float beta = gate.beta[lane & 31];
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float y = i == row ? 1.0f : 0.0f;
+#pragma unroll
+          for (int j = 0; j < i; j += 4) {
+            const f32x4 a = *(const f32x4*)(diagonal + i * kMPitch + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (j + e < i) y = fmaf(-a[e], x[j + e], y);
+          }
+          x[i] = y;
+        }
+        wave_order();
+        // the first with beta, the second as it is, until the block below the first is formed: -T22 A21 T11
+        if (lane < 32)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) diagonal[i * kMPitch + row] = lane < 16 ? x[i] * beta : x[i];
+        wave_order();
+        const f32x4 a21 = *(const f32x4*)(m + (16 + row) * kMPitch + 4 * g), t22 = *(const f32x4*)(m + (16 + row) * kMPitch + 16 + 4 * g);
+        f32x4 w = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w = __builtin_amdgcn_mfma_f32_16x16x4f32(a21[i], m[(4 * g + i) * kMPitch + row], w, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(t22[i], w[i], y, 0, 0, 0);
+        wave_order();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[(16 + 4 * g + i) * kMPitch + row] = -y[i];
+        if (lane >= 16 && lane < 32)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) diagonal[i * kMPitch + row] = x[i] * beta;
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  if (chunks > 0) {
+    fetch_rows(key, p.k.token, 0, kk);
+    fetch_rows(query, p.q.token, 0, qq);
+  }
+  __syncthreads();
+  for (int c = -1; c < chunks; ++c) {
+    if (c + 1 < chunks) {
+      char* const next = lds + ((c + 1) & 1) * kBuffer;
+      const ChunkGates& gate = gates[(c + 1) % 3];
+      lay_out(qq, next + kQ);
+#pragma unroll
+      for (int tile = 0; tile < 4; ++tile) {         // (it, jt) = (0, 0), (0, 1): nothing, (1, 0), (1, 1)
+        const int it = tile >> 1, jt = tile & 1;
+        f32x4 d = {0, 0, 0, 0};
+        if (tile != 1) {
+#pragma unroll
+          for (int k = 0; k < KS; ++k) d = mfma16(kk[jt][k], qq[it][k], d);
+          const f32x4 w = gamma(gate, it, jt);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[i] = it == jt && 4 * g + i > row ? 0.0f : w[i] * d[i];
+        }
+        char* const to = next + kP + (16 * it + row) * kPPitch + 16 * g + 8 * jt;
+        float rest[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rest[i] = d[i] - upper_half(d[i]);
+        *(u32x2*)to = u32x2{pack_upper(d[0], d[1]), pack_upper(d[2], d[3])};
+        *(u32x2*)(to + kChunk * kPPitch) = u32x2{pack_upper(rest[0], rest[1]), pack_upper(rest[2], rest[3])};
+      }
+      if (c + 2 < chunks) {
+        fetch_rows(key, p.k.token, c + 2, kk);
+        fetch_rows(query, p.q.token, c + 2, qq);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+namespace {
+DeltaGrid grid_of(const DeltaParams& p) {
+  const int columns = (p.value_dim + 15) / 16;
+  DeltaGrid grid;
+  // as many of the state's waves in a workgroup as leave a workgroup for every CU
+  grid.waves = std::min(kStateWaves, columns);
+  while (grid.waves > 1 && (int64_t)p.batch * p.heads * ((columns + grid.waves - 1) / grid.waves) < 256) --grid.waves;
+  grid.blocks = (columns + grid.waves - 1) / grid.waves;
+  grid.waves = (columns + grid.blocks - 1) / grid.blocks;
+  return grid;
+}
 template <class T>
-static const void* steps_of(const DeltaParams& p) {
+const void* steps_of(const DeltaParams& p) {
   return p.key_dim <= 64 ? (const void*)k_delta_steps<T, 4> : (const void*)k_delta_steps<T, 8>;
 }
+template <class T>
+const void* chunks_of(const DeltaParams& p) {
+  return p.key_dim <= 64 ? (const void*)k_delta_chunks<T, 64> : p.key_dim <= 96 ? (const void*)k_delta_chunks<T, 96> : (const void*)k_delta_chunks<T, 128>;
+}
+}  // namespace
+
+size_t delta_workspace(const DeltaParams&) { return 0; }
 
 hipError_t launch(const DeltaParams& p, hipStream_t stream) {
   DeltaParams params = p;
-  void* args[] = {&params};
+  DeltaGrid grid = grid_of(p);
+  void* args[] = {&params, &grid};
+  if (p.tokens > 8)
+    return launch_kernel(p.dtype == HS_F16 ? chunks_of<f16>(p) : chunks_of<bf16>(p), (int64_t)p.batch * p.heads * grid.blocks, 64 * (grid.waves + kOtherWaves),
+                         args, stream);
   const int64_t workgroups = (int64_t)p.batch * p.heads * ((p.value_dim + 63) / 64);
   return launch_kernel(p.dtype == HS_F16 ? steps_of<f16>(p) : steps_of<bf16>(p), workgroups, 256, args, stream);
 }
