@@ -8,12 +8,17 @@
 namespace hs {
 namespace {
 
+constexpr int kSlice = 16;      // hidden values with a power of two of their own
+
 struct ExpertParts {            // the workspace
   int32_t* chosen;              // [tokens][top]
   float* weights;               // [tokens][top]
-  float* hidden;                // [tokens][top][hidden]
+  void* hidden;                 // [tokens][top][hidden], in the inputs' type
+  int16_t* power;               // [tokens][top][hidden / 16]: what fp16 values were divided by, as a power of two
+  float* products;              // [tokens][top][channels]
   size_t bytes;
 };
+__host__ __device__ inline int slices_of(const ExpertParams& p) { return (p.hidden + kSlice - 1) / kSlice; }
 ExpertParts parts_of(const ExpertParams& p) {
   ExpertParts w;
   size_t at = 0;
@@ -25,7 +30,9 @@ ExpertParts parts_of(const ExpertParams& p) {
   const size_t pairs = (size_t)p.tokens * p.top;
   w.chosen = (int32_t*)take(pairs * 4);
   w.weights = (float*)take(pairs * 4);
-  w.hidden = (float*)take(pairs * p.hidden * 4);
+  w.hidden = take(pairs * p.hidden * 2);
+  w.power = (int16_t*)take(p.dtype == HS_F16 ? pairs * slices_of(p) * 2 : 0);
+  w.products = (float*)take(pairs * p.channels * 4);
   w.bytes = at;
   return w;
 }
@@ -37,13 +44,15 @@ __device__ __forceinline__ uint64_t rank_of(double x) {
   return bits >> 63 ? ~bits : bits | 1ull << 63;
 }
 
-// A wave per token: scores in 64 bits, lane l has experts l, l + 64, ..
+// A workgroup per token: scores in 64 bits, a quarter of the experts per wave; the first wave chooses, lane l with experts
+// l, l + 64, ..
 template <class T>
-__global__ __launch_bounds__(64) void k_expert_route(ExpertParams p, ExpertParts w) {
+__global__ __launch_bounds__(256) void k_expert_route(ExpertParams p, ExpertParts w) {
   typedef typename Vec<T>::x8 x8;
-  const int t = blockIdx.x, lane = threadIdx.x;
+  __shared__ double scores[HS_MAX_EXPERTS];
+  const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (p.mask && !p.mask[t]) {
-    if (lane < p.top) {
+    if ((int)threadIdx.x < p.top) {
       w.chosen[t * p.top + lane] = -1;
       w.weights[t * p.top + lane] = 0.0f;
       if (p.chosen) p.chosen[t * p.top + lane] = -1;
@@ -52,20 +61,32 @@ __global__ __launch_bounds__(64) void k_expert_route(ExpertParams p, ExpertParts
     return;
   }
   const T* const x = (const T*)p.x + t * p.x_stride;
-  double score[HS_MAX_EXPERTS / 64];
-  for (int e = 0; e < p.experts; ++e) {
-    const T* const r = (const T*)p.router + (int64_t)e * p.channels;
-    double sum = 0.0;
+  constexpr int kAtOnce = 4;
+  for (int e0 = wave; e0 < p.experts; e0 += 4 * kAtOnce) {
+    double sum[kAtOnce] = {};
     for (int c = 8 * lane; c < p.channels; c += 512) {
-      const x8 a = *(const x8*)(x + c), g = *(const x8*)(r + c);
+      const x8 a = *(const x8*)(x + c);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fma((double)(float)a[i], (double)(float)g[i], sum);
+      for (int n = 0; n < kAtOnce; ++n) {
+        const int e = min(e0 + 4 * n, p.experts - 1);
+        const x8 r = *(const x8*)((const T*)p.router + (int64_t)e * p.channels + c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[n] = fma((double)(float)a[i], (double)(float)r[i], sum[n]);
+      }
     }
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
 #pragma unroll
-    for (int i = 0; i < HS_MAX_EXPERTS / 64; ++i)
-      if (lane + 64 * i == e) score[i] = sum;
+    for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) sum[n] += __shfl_xor(sum[n], d);
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n)
+      if (lane == n && e0 + 4 * n < p.experts) scores[e0 + 4 * n] = sum[n];
   }
+  __syncthreads();
+  if (wave > 0) return;
+  double score[HS_MAX_EXPERTS / 64];
+#pragma unroll
+  for (int i = 0; i < HS_MAX_EXPERTS / 64; ++i) score[i] = lane + 64 * i < p.experts ? scores[lane + 64 * i] : 0.0;
   double best[HS_MAX_TOP];
   uint32_t taken = 0;
   double most = 0.0;
@@ -115,61 +136,236 @@ __global__ __launch_bounds__(64) void k_expert_route(ExpertParams p, ExpertParts
     }
 }
 
-template <class T>
-__device__ __forceinline__ float dot(const T* a, const T* b, int n, int lane) {
+// The pairs (token, place) that chose expert e, in their order: those numbered first .. first + most - 1 of them are left in
+// `list`; returns how many these are.  For a whole workgroup of 256.
+__device__ __forceinline__ int pairs_of(const ExpertParams& p, const int32_t* chosen, int e, int first, int most, int32_t* list, int* counts) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = p.tokens * p.top;
+  int seen = 0;
+  for (int at = 0; at < pairs && seen < first + most; at += 256) {
+    const int i = at + threadIdx.x;
+    const bool hit = i < pairs && chosen[i] == e;
+    const uint64_t hits = __ballot(hit);
+    if (lane == 0) counts[wave] = __popcll(hits);
+    __syncthreads();
+    int place = seen + __popcll(hits & ((1ull << lane) - 1));
+    for (int n = 0; n < 4; ++n) {
+      if (n < wave) place += counts[n];
+      seen += counts[n];
+    }
+    if (hit && place >= first && place < first + most) list[place - first] = i;
+    __syncthreads();
+  }
+  return min(max(seen - first, 0), most);
+}
+
+// Products of RT tiles of 16 weight rows with NT tiles of 16 vectors over steps first .. last - 1 of 64: a lane has 16 values side by
+// side of a row, so that four lanes read 128 bytes of it, and of a vector; the matrix pipe takes them in the same order.
+// Lane l has result [row 4 * (l / 16) + i][vector l % 16].  A step's loads are issued before the products of the one before.
+template <class T, int RT, int NT, bool POWERS>
+__device__ __forceinline__ void products(const T* const (&rows)[RT], const T* const (&vectors)[NT], const int16_t* const (&power)[NT],
+                                         const int (&row_power)[NT], int first, int last, int length, f32x4 (&acc)[RT][NT]) {
   typedef typename Vec<T>::x8 x8;
-  float sum = 0.0f;
-  for (int c = 8 * lane; c < n; c += 512) {
-    const x8 u = *(const x8*)(a + c), v = *(const x8*)(b + c);
+  const int g = (threadIdx.x & 63) >> 4;
+  struct Step {
+    x8 a[RT][2], b[NT][2];
+    int16_t power[NT];
+  };
+  auto load = [&](int step, Step& s) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fmaf((float)u[i], (float)v[i], sum);
+    for (int e = 0; e < 2; ++e) {
+      const int d0 = min(64 * step + 16 * g + 8 * e, length - 8);   // (what lies behind the row's end is left out below)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) s.a[r][e] = __builtin_bit_cast(x8, load16(rows[r] + d0));
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s.b[n][e] = __builtin_bit_cast(x8, load16(vectors[n] + d0));
+    }
+    if (POWERS)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s.power[n] = power[n][min(64 * step + 16 * g, length - 1) / kSlice];
+  };
+  auto multiply = [&](int step, Step& s) {
+    if (64 * step + 64 > length) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (64 * step + 16 * g + 8 * e >= length) {
+#pragma unroll
+          for (int r = 0; r < RT; ++r) s.a[r][e] = x8{};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) s.b[n][e] = x8{};
+        }
+    }
+    if (POWERS)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const T f = (T)ldexpf(1.0f, max(s.power[n] - row_power[n], -40));
+        s.b[n][0] *= f;
+        s.b[n][1] *= f;
+      }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[r][n] = mfma16(s.a[r][e], s.b[n][e], acc[r][n]);
+  };
+  Step even, odd;
+  if (first < last) load(first, even);
+  for (int step = first; step < last; step += 2) {
+    if (step + 1 < last) load(step + 1, odd);
+    multiply(step, even);
+    if (step + 1 >= last) break;
+    if (step + 2 < last) load(step + 2, even);
+    multiply(step + 1, odd);
   }
-  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-  return sum;
 }
 
-// A wave per token, chosen expert and value of the hidden layer.
-template <class T>
-__global__ __launch_bounds__(256) void k_expert_in(ExpertParams p, ExpertParts w) {
-  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, pair = id / p.hidden;
-  if (pair >= (int64_t)p.tokens * p.top) return;
-  const int f = id % p.hidden, e = w.chosen[pair], lane = threadIdx.x & 63;
-  if (e < 0) return;
-  const T* const x = (const T*)p.x + pair / p.top * p.x_stride;
-  const T* const rows = (const T*)p.w_in + ((int64_t)e * 2 * p.hidden + f) * p.channels;
-  const float gate = dot(x, rows, p.channels, lane), up = dot(x, rows + (int64_t)p.hidden * p.channels, p.channels, lane);
-  if (lane == 0) w.hidden[pair * p.hidden + f] = gate / (1.0f + expf(-gate)) * up;
+constexpr int kNoPower = -1000;   // of a slice of zeros
+
+// Hidden layer: a workgroup has an expert, 16 of its hidden values and up to 16 * NT of its tokens; its four waves take a quarter
+// of the channels each.
+template <class T, int NT>
+__global__ __launch_bounds__(256) void k_expert_in(ExpertParams p, ExpertParts w, int groups) {
+  __shared__ int32_t list[16 * NT];
+  __shared__ int counts[4];
+  __shared__ f32x4 partial[4][2][NT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
+  int id = xcd_number();
+  const int group = id % groups, slices = slices_of(p);
+  id /= groups;
+  const int slice = id % slices, e = id / slices;
+  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
+  if (n == 0) return;
+  const T* vectors[NT];                              // (a place without a token has the first's, and is left out below)
+  const int16_t* none[NT] = {};
+  int zero[NT] = {};
+#pragma unroll
+  for (int i = 0; i < NT; ++i) vectors[i] = (const T*)p.x + (int64_t)(list[16 * i + col < n ? 16 * i + col : 0] / p.top) * p.x_stride;
+  const T* const gate = (const T*)p.w_in + ((int64_t)e * 2 * p.hidden + min(16 * slice + col, p.hidden - 1)) * p.channels;
+  const T* const rows[2] = {gate, gate + (int64_t)p.hidden * p.channels};
+  const int steps = (p.channels + 63) / 64;
+  f32x4 acc[2][NT] = {};
+  products<T, 2, NT, false>(rows, vectors, none, zero, steps * wave / 4, steps * (wave + 1) / 4, p.channels, acc);
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) partial[wave][r][i][lane] = acc[r][i];
+  __syncthreads();
+  // thread t: hidden value t % 16 of token t / 16
+  const int u = threadIdx.x & 15, at = threadIdx.x >> 4, from = (u >> 2) * 16 + at;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    if (16 * i >= n) break;
+    float y[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+      y[r] = (partial[0][r][i][from][u & 3] + partial[1][r][i][from][u & 3]) + (partial[2][r][i][from][u & 3] + partial[3][r][i][from][u & 3]);
+    float h = y[0] / (1.0f + expf(-y[0])) * y[1];
+    const bool stored = 16 * i + at < n && 16 * slice + u < p.hidden;
+    const int64_t pair = list[min(16 * i + at, n - 1)];
+    if (__is_same(T, f16)) {
+      float most = stored ? fabsf(h) : 0.0f;
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+      const int power = most > 0.0f && most < INFINITY ? ilogbf(most) - 14 : most > 0.0f ? 0 : kNoPower;
+      if (power != kNoPower) h = ldexpf(h, -power);
+      if (stored && u == 0) w.power[pair * slices + slice] = power;
+    }
+    if (stored) ((T*)w.hidden)[pair * p.hidden + 16 * slice + u] = (T)h;
+  }
 }
 
-// A wave per token and channel.
+// What comes out of an expert: 16 channels per workgroup, a quarter of the hidden values per wave.
+template <class T, int NT>
+__global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts w, int groups) {
+  __shared__ int32_t list[16 * NT];
+  __shared__ int counts[4];
+  __shared__ f32x4 partial[4][NT][64];
+  __shared__ int powers[16 * NT];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
+  int id = xcd_number();
+  const int group = id % groups, blocks = (p.channels + 15) / 16, slices = slices_of(p);
+  id /= groups;
+  const int block = id % blocks, e = id / blocks;
+  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
+  if (n == 0) return;
+  constexpr bool kPowers = __is_same(T, f16);
+  if (kPowers) {
+    const int at = threadIdx.x >> 4;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      if (16 * i + at >= n) break;
+      const int16_t* const power = w.power + (int64_t)list[16 * i + at] * slices;
+      int most = kNoPower;
+      for (int s = threadIdx.x & 15; s < slices; s += 16) most = max(most, (int)power[s]);
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) most = max(most, __shfl_xor(most, d));
+      if ((threadIdx.x & 15) == 0) powers[16 * i + at] = most;
+    }
+    __syncthreads();
+  }
+  const T* vectors[NT];
+  const int16_t* power[NT];
+  int row_power[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int at = 16 * i + col < n ? 16 * i + col : 0;
+    const int64_t pair = list[at];
+    vectors[i] = (const T*)w.hidden + pair * p.hidden;
+    power[i] = w.power + pair * slices;
+    row_power[i] = kPowers ? powers[at] : 0;
+  }
+  const T* const rows[1] = {(const T*)p.w_out + ((int64_t)e * p.channels + min(16 * block + col, p.channels - 1)) * p.hidden};
+  const int steps = (p.hidden + 63) / 64;
+  f32x4 acc[1][NT] = {};
+  products<T, 1, NT, kPowers>(rows, vectors, power, row_power, steps * wave / 4, steps * (wave + 1) / 4, p.hidden, acc);
+#pragma unroll
+  for (int i = 0; i < NT; ++i) partial[wave][i][lane] = acc[0][i];
+  __syncthreads();
+  const int u = threadIdx.x & 15, at = threadIdx.x >> 4, from = (u >> 2) * 16 + at;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    if (16 * i + at >= n || 16 * block + u >= p.channels) break;
+    const int64_t pair = list[16 * i + at];
+    float y = (partial[0][i][from][u & 3] + partial[1][i][from][u & 3]) + (partial[2][i][from][u & 3] + partial[3][i][from][u & 3]);
+    if (kPowers) y = powers[16 * i + at] == kNoPower ? y : ldexpf(y, powers[16 * i + at]);
+    w.products[pair * p.channels + 16 * block + u] = w.weights[pair] * y;
+  }
+}
+
+// A token's experts in the order of their choice: 8 channels per thread.
 template <class T>
-__global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts w) {
-  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, t = id / p.channels;
+__global__ __launch_bounds__(256) void k_expert_sum(ExpertParams p, ExpertParts w) {
+  const int pieces = p.channels / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, t = id / pieces;
   if (t >= p.tokens) return;
-  const int c = id % p.channels, lane = threadIdx.x & 63;
-  float all = 0.0f;
-  for (int i = 0; i < p.top; ++i) {
-    const int e = w.chosen[t * p.top + i];
-    if (e < 0) continue;
-    const T* const row = (const T*)p.w_out + ((int64_t)e * p.channels + c) * p.hidden;
-    const float* const h = w.hidden + (t * p.top + i) * p.hidden;
-    float sum = 0.0f;
-    for (int f = lane; f < p.hidden; f += 64) sum = fmaf(h[f], (float)row[f], sum);
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    all = fmaf(w.weights[t * p.top + i], sum, all);
-  }
-  if (lane == 0) ((T*)p.out)[t * p.out_stride + c] = (T)all;
+  const int c = (int)(id % pieces) * 8;
+  float sum[8] = {};
+  if (!p.mask || p.mask[t])
+    for (int i = 0; i < p.top; ++i) {
+      const float* const from = w.products + (t * p.top + i) * p.channels + c;
+      const f32x4 a = *(const f32x4*)from, b = *(const f32x4*)(from + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += a[e], sum[4 + e] += b[e];
+    }
+  *(typename Vec<T>::x8*)((T*)p.out + t * p.out_stride + c) = round8<T>(sum);
 }
 
-template <class T>
+template <class T, int NT>
 hipError_t launch_of(const ExpertParams& p, hipStream_t stream) {
   ExpertParams params = p;
   ExpertParts parts = parts_of(p);
-  void* args[] = {&params, &parts};
-  hipError_t e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 64, args, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_in<T>, ((int64_t)p.tokens * p.top * p.hidden + 3) / 4, 256, args, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_out<T>, ((int64_t)p.tokens * p.channels + 3) / 4, 256, args, stream);
+  int groups = (p.tokens + 16 * NT - 1) / (16 * NT);
+  void* args[] = {&params, &parts, &groups};
+  hipError_t e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 256, args, stream);
+  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_in<T, NT>, (int64_t)p.experts * slices_of(p) * groups, 256, args, stream);
+  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_out<T, NT>, (int64_t)p.experts * ((p.channels + 15) / 16) * groups, 256, args, stream);
+  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_sum<T>, ((int64_t)p.tokens * (p.channels / 8) + 255) / 256, 256, args, stream);
   return e;
+}
+template <class T>
+hipError_t launch_of(const ExpertParams& p, hipStream_t stream) {
+  const int64_t each = (int64_t)p.tokens * p.top / p.experts;          // tokens of an expert, on average
+  return p.tokens <= 16 ? launch_of<T, 1>(p, stream) : each <= 32 ? launch_of<T, 2>(p, stream) : launch_of<T, 4>(p, stream);
 }
 }  // namespace
 
