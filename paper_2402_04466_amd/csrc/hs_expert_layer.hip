@@ -16,6 +16,8 @@ struct ExpertParts {            // the workspace
   void* hidden;                 // [tokens][top][hidden], in the inputs' type
   int16_t* power;               // [tokens][top][hidden / 16]: what fp16 values were divided by, as a power of two
   float* products;              // [tokens][top][channels]
+  int32_t* count;               // [experts]: pairs that chose it
+  int32_t* list;                // [experts][tokens]: these pairs, in their order
   size_t bytes;
 };
 __host__ __device__ inline int slices_of(const ExpertParams& p) { return (p.hidden + kSlice - 1) / kSlice; }
@@ -33,6 +35,8 @@ ExpertParts parts_of(const ExpertParams& p) {
   w.hidden = take(pairs * p.hidden * 2);
   w.power = (int16_t*)take(p.dtype == HS_F16 ? pairs * slices_of(p) * 2 : 0);
   w.products = (float*)take(pairs * p.channels * 4);
+  w.count = (int32_t*)take((size_t)p.experts * 4);
+  w.list = (int32_t*)take((size_t)p.experts * p.tokens * 4);
   w.bytes = at;
   return w;
 }
@@ -332,6 +336,183 @@ __global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts 
   }
 }
 
+// The pairs that chose each expert, a workgroup per expert: a thread looks at 16 pairs side by side.
+__global__ __launch_bounds__(256) void k_expert_lists(ExpertParams p, ExpertParts w) {
+  __shared__ int counts[4];
+  const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = p.tokens * p.top;
+  int seen = 0;
+  for (int at = 0; at < pairs; at += 4096) {
+    const int first = at + 16 * threadIdx.x;
+    uint32_t hits = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (first + i < pairs && w.chosen[first + i] == e) hits |= 1u << i;
+    int before = __popc(hits);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int other = __shfl_up(before, d);
+      if (lane >= d) before += other;
+    }
+    if (lane == 63) counts[wave] = before;
+    __syncthreads();
+    int place = seen + before - __popc(hits);
+    for (int n = 0; n < 4; ++n) {
+      if (n < wave) place += counts[n];
+      seen += counts[n];
+    }
+    for (; hits; hits &= hits - 1) w.list[(int64_t)e * p.tokens + place++] = first + __ffs(hits) - 1;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) w.count[e] = seen;
+}
+
+// Either product for many tokens of an expert: a workgroup has 128 hidden values (IN: 128 rows of each of the two weights) or channels
+// and up to 32 * NT of the expert's tokens, 32 rows per wave.  Weights go from memory into the registers that multiply them, as
+// no other wave needs them; the tokens' values, which all waves need, through LDS, 64 at a time.
+template <class T, bool IN, int NT>
+__global__ __launch_bounds__(256, 2) void k_expert_tiles(ExpertParams p, ExpertParts w, int groups) {
+  typedef typename Vec<T>::x8 x8;
+  typedef typename Vec<T>::x4 x4;
+  constexpr int RT = IN ? 2 : 1, kTile = 32 * NT * 128;
+  constexpr bool kPowers = __is_same(T, f16);
+  __shared__ __align__(16) char lds[2 * kTile];
+  __shared__ int powers[32 * NT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  const int rows = IN ? p.hidden : p.channels, length = IN ? p.channels : p.hidden, blocks = (rows + 127) / 128, slices = slices_of(p);
+  // the groups of the tokens behind the first, most often empty, come last
+  const int per_group = blocks * p.experts, group = blockIdx.x / per_group;
+  const int id = blockIdx.x % per_group, block = id % blocks, e = id / blocks;
+  const int n = min(w.count[e] - group * 32 * NT, 32 * NT);
+  if (n <= 0) return;
+  const int32_t* const list = w.list + (int64_t)e * p.tokens + group * 32 * NT;
+
+  // staging: this thread's 16 bytes of vectors r0 + 32 i
+  const int r0 = threadIdx.x >> 3, ch = threadIdx.x & 7;
+  const T* from[NT];
+  const int16_t* power[NT];
+  int row_power[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int64_t pair = list[min(r0 + 32 * i, n - 1)];
+    from[i] = IN ? (const T*)p.x + pair / p.top * p.x_stride : (const T*)w.hidden + pair * p.hidden;
+    power[i] = w.power + pair * slices;
+    row_power[i] = 0;
+    if (!IN && kPowers) {                            // the eight threads of a vector look for its largest power
+      int most = kNoPower;
+      for (int s = ch; s < slices; s += 8) most = max(most, (int)power[i][s]);
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) most = max(most, __shfl_xor(most, d));
+      row_power[i] = most;
+      if (ch == 0) powers[r0 + 32 * i] = most;
+    }
+  }
+  const int row = 128 * block + 32 * wave;
+  const int64_t first_row = (int64_t)e * (IN ? 2 * p.hidden : p.channels) + min(row + col, rows - 1);
+  const T* weights[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) weights[r] = (const T*)(IN ? p.w_in : p.w_out) + (first_row + (int64_t)r * p.hidden) * length + 8 * half;
+
+  struct Step {
+    x8 a[RT][4];
+    x8 b[NT];
+    int16_t power[NT];
+  };
+  auto load = [&](int step, Step& s) {
+    const int d0 = min(64 * step + 8 * ch, length - 8);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      s.b[i] = __builtin_bit_cast(x8, load16(from[i] + d0));
+      if (!IN && kPowers) s.power[i] = power[i][d0 / kSlice];
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s.a[r][k] = __builtin_bit_cast(x8, load16(weights[r] + min(64 * step + 16 * k, length - 8 - 8 * half)));
+  };
+  int koff[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) koff[k] = slot<8>(col, 2 * k + half);
+  f32x16 acc[RT][NT] = {};
+  const int steps = (length + 63) / 64;
+  auto multiply = [&](int step, Step& s, Step& next) {
+    char* const here = lds + (step & 1) * kTile;
+    const bool whole = 64 * step + 64 <= length;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      if (!whole && 64 * step + 8 * ch >= length) s.b[i] = x8{};
+      if (!IN && kPowers) s.b[i] *= (T)ldexpf(1.0f, max(s.power[i] - row_power[i], -40));
+      *(x8*)(here + slot<8>(r0 + 32 * i, ch)) = s.b[i];
+    }
+    if (step + 1 < steps) load(step + 1, next);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (!whole && 64 * step + 16 * k + 8 * half >= length)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) s.a[r][k] = x8{};
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const x8 b = *(const x8*)(here + koff[k] + i * 32 * 128);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[r][i] = mfma32(s.a[r][k], b, acc[r][i]);
+      }
+    }
+  };
+  Step even, odd;
+  load(0, even);
+  for (int step = 0; step < steps; step += 2) {
+    multiply(step, even, odd);
+    if (step + 1 < steps) multiply(step + 1, odd, even);
+  }
+
+  // lane l has vector l % 32 and rows 8 * (i / 4) + 4 * half + i % 4
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    if (32 * i >= n) break;
+    const bool live = 32 * i + col < n;
+    const int64_t pair = list[min(32 * i + col, n - 1)];
+    if (IN) {
+      f32x16 h;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) h[j] = acc[0][i][j] / (1.0f + expf(-acc[0][i][j])) * acc[RT - 1][i][j];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        int own = 0;
+        if (kPowers) {
+          float most = 0.0f, lower, upper;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (row + 16 * s + 8 * (j / 4) + 4 * half < rows) most = fmaxf(most, fabsf(h[8 * s + j]));
+          both_halves(most, lower, upper);
+          most = fmaxf(lower, upper);
+          own = most > 0.0f && most < INFINITY ? ilogbf(most) - 14 : most > 0.0f ? 0 : kNoPower;
+          if (live && half == 0 && row + 16 * s < rows) w.power[pair * slices + row / kSlice + s] = own;
+          if (own == kNoPower) own = 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) {
+          const int unit = row + 16 * s + 2 * j + 4 * half;
+          x4 y;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) y[d] = (T)(kPowers ? ldexpf(h[8 * s + j + d], -own) : h[8 * s + j + d]);
+          if (live && unit < rows) *(x4*)((T*)w.hidden + pair * p.hidden + unit) = y;
+        }
+      }
+    } else {
+      float f = w.weights[pair];
+      const int own = kPowers ? powers[min(32 * i + col, n - 1)] : 0;
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        const int channel = row + 2 * j + 4 * half;
+        f32x4 y;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) y[d] = f * (kPowers && own != kNoPower ? ldexpf(acc[0][i][j + d], own) : acc[0][i][j + d]);
+        if (live && channel < rows) *(f32x4*)(w.products + pair * p.channels + channel) = y;
+      }
+    }
+  }
+}
+
 // A token's experts in the order of their choice: 8 channels per thread.
 template <class T>
 __global__ __launch_bounds__(256) void k_expert_sum(ExpertParams p, ExpertParts w) {
@@ -351,21 +532,34 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertParams p, ExpertParts 
 }
 
 template <class T, int NT>
-hipError_t launch_of(const ExpertParams& p, hipStream_t stream) {
-  ExpertParams params = p;
-  ExpertParts parts = parts_of(p);
-  int groups = (p.tokens + 16 * NT - 1) / (16 * NT);
-  void* args[] = {&params, &parts, &groups};
-  hipError_t e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 256, args, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_in<T, NT>, (int64_t)p.experts * slices_of(p) * groups, 256, args, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_out<T, NT>, (int64_t)p.experts * ((p.channels + 15) / 16) * groups, 256, args, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_sum<T>, ((int64_t)p.tokens * (p.channels / 8) + 255) / 256, 256, args, stream);
+hipError_t launch_tiles(const ExpertParams& p, void** args, hipStream_t stream) {
+  int groups = (p.tokens + 32 * NT - 1) / (32 * NT);
+  void* all[] = {args[0], args[1], &groups};
+  hipError_t e = launch_kernel((const void*)k_expert_lists, p.experts, 256, args, stream);
+  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_tiles<T, true, NT>, (int64_t)p.experts * ((p.hidden + 127) / 128) * groups, 256, all, stream);
+  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_tiles<T, false, NT>, (int64_t)p.experts * ((p.channels + 127) / 128) * groups, 256, all, stream);
+  return e;
+}
+template <class T>
+hipError_t launch_few(const ExpertParams& p, void** args, hipStream_t stream) {
+  int groups = 1;
+  void* all[] = {args[0], args[1], &groups};
+  hipError_t e = launch_kernel((const void*)k_expert_in<T, 1>, (int64_t)p.experts * slices_of(p), 256, all, stream);
+  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_out<T, 1>, (int64_t)p.experts * ((p.channels + 15) / 16), 256, all, stream);
   return e;
 }
 template <class T>
 hipError_t launch_of(const ExpertParams& p, hipStream_t stream) {
+  ExpertParams params = p;
+  ExpertParts parts = parts_of(p);
+  void* args[] = {&params, &parts};
+  hipError_t e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 256, args, stream);
   const int64_t each = (int64_t)p.tokens * p.top / p.experts;          // tokens of an expert, on average
-  return p.tokens <= 16 ? launch_of<T, 1>(p, stream) : each <= 32 ? launch_of<T, 2>(p, stream) : launch_of<T, 4>(p, stream);
+  if (e == hipSuccess)
+    e = p.tokens <= 16 ? launch_few<T>(p, args, stream) : each <= 24 ? launch_tiles<T, 1>(p, args, stream)
+      : each <= 48 ? launch_tiles<T, 2>(p, args, stream) : launch_tiles<T, 4>(p, args, stream);
+  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_sum<T>, ((int64_t)p.tokens * (p.channels / 8) + 255) / 256, 256, args, stream);
+  return e;
 }
 }  // namespace
 
