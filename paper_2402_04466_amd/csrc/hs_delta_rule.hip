@@ -146,13 +146,6 @@ __device__ __forceinline__ void split8(const float* x, b8* part) {
   }
 }
 
-// The accesses of a wave to LDS before this come before those after it, whichever lane they are of.
-__device__ __forceinline__ void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 struct ChunkGates {                                  // of one chunk
   float upto_hi[kChunk], upto_lo[kChunk];            // L in two parts
   float since[kChunk], left[kChunk];                 // 2^L, 2^(L_end - L)

@@ -8,16 +8,24 @@
 namespace hs {
 namespace {
 
-constexpr int kSlice = 16;      // hidden values with a power of two of their own
+// The choice (k_expert_route), the hidden layer, what comes out of each expert, and the sum over a token's experts (k_expert_sum):
+// up to 64 tokens by strips of 16 weight rows (k_expert_in, k_expert_out), a frame's 16 with the choice and the hidden layer in one
+// launch (k_expert_frame); more by tiles of 128 rows (k_expert_tiles).
+// A product has a weight's rows as its first and tokens as its second operand, so that few tokens waste little of the matrix pipe, and
+// every weight that is needed is read once, straight from memory into the registers that multiply it.
+//
+// fp16: hidden values are kept divided by a power of two, one for each token and 16 of them, which lets them neither overflow nor lose
+// bits; the second product takes all of a token's divided by their largest.
+constexpr int kFewTokens = 64;
+constexpr int kSlice = 16;
+constexpr int kNoPower = -1000;                      // of a slice of zeros
 
 struct ExpertParts {            // the workspace
   int32_t* chosen;              // [tokens][top]
   float* weights;               // [tokens][top]
   void* hidden;                 // [tokens][top][hidden], in the inputs' type
-  int16_t* power;               // [tokens][top][hidden / 16]: what fp16 values were divided by, as a power of two
+  int16_t* power;               // [tokens][top][slices of hidden], fp16
   float* products;              // [tokens][top][channels]
-  int32_t* count;               // [experts]: pairs that chose it
-  int32_t* list;                // [experts][tokens]: these pairs, in their order
   size_t bytes;
 };
 __host__ __device__ inline int slices_of(const ExpertParams& p) { return (p.hidden + kSlice - 1) / kSlice; }
@@ -35,8 +43,6 @@ ExpertParts parts_of(const ExpertParams& p) {
   w.hidden = take(pairs * p.hidden * 2);
   w.power = (int16_t*)take(p.dtype == HS_F16 ? pairs * slices_of(p) * 2 : 0);
   w.products = (float*)take(pairs * p.channels * 4);
-  w.count = (int32_t*)take((size_t)p.experts * 4);
-  w.list = (int32_t*)take((size_t)p.experts * p.tokens * 4);
   w.bytes = at;
   return w;
 }
@@ -48,305 +54,306 @@ __device__ __forceinline__ uint64_t rank_of(double x) {
   return bits >> 63 ? ~bits : bits | 1ull << 63;
 }
 
-// A workgroup per token: scores in 64 bits, a quarter of the experts per wave; the first wave chooses, lane l with experts
-// l, l + 64, ..
+__device__ __forceinline__ double score_of(uint64_t rank) {
+  return rank == 0 ? __builtin_nan("") : __builtin_bit_cast(double, rank >> 63 ? rank & ~(1ull << 63) : ~rank);
+}
+
+// A token's choice by one wave, from the scores' ranks in LDS: an expert's place is the number of experts before it.  Left
+// there and, where a caller's arrays are given, with them; `best`: HS_MAX_TOP doubles in LDS of this wave's own.
+__device__ __forceinline__ void choose(const ExpertParams& p, const uint64_t* ranks, double* best, int32_t* chosen, float* weights, int32_t* user_chosen,
+                                       float* user_weights) {
+  const int lane = threadIdx.x & 63;
+  for (int e = lane; e < p.experts; e += 64) {
+    const uint64_t own = ranks[e];
+    int place = 0;
+    for (int j = 0; j < p.experts; ++j) {
+      const uint64_t other = ranks[j];
+      place += other > own || (other == own && j < e);
+    }
+    if (place < p.top) {
+      chosen[place] = e;
+      if (user_chosen) user_chosen[place] = e;
+      best[place] = score_of(own);
+    }
+  }
+  wave_order();
+  const double most = best[0];
+  double total = 0.0;
+  if (p.renormalise) {
+    if (lane < p.top) total = exp(best[lane] - most);
+  } else {
+    for (int e = lane; e < p.experts; e += 64) total += exp(score_of(ranks[e]) - most);
+  }
+  const int sharers = p.renormalise ? HS_MAX_TOP : 64;
+  for (int d = 1; d < sharers; d *= 2) total += __shfl_xor(total, d);
+  if (lane < p.top) {
+    const float weight = (float)(exp(best[lane] - most) / total);
+    weights[lane] = weight;
+    if (user_weights) user_weights[lane] = weight;
+  }
+}
+
+__device__ __forceinline__ void choose_none(const ExpertParams& p, int32_t* chosen, float* weights, int32_t* user_chosen, float* user_weights) {
+  const int lane = threadIdx.x & 63;
+  if (lane >= p.top) return;
+  chosen[lane] = -1;
+  weights[lane] = 0.0f;
+  if (user_chosen) user_chosen[lane] = -1;
+  if (user_weights) user_weights[lane] = 0.0f;
+}
+
+// A workgroup per token: scores in 64 bits.  A wave has a quarter of the experts, eight at a time, a lane 8 of every 512 channels;
+// the lanes' sums of the eight are joined together, half as many with every step.
 template <class T>
 __global__ __launch_bounds__(256) void k_expert_route(ExpertParams p, ExpertParts w) {
   typedef typename Vec<T>::x8 x8;
-  __shared__ double scores[HS_MAX_EXPERTS];
+  __shared__ uint64_t ranks[HS_MAX_EXPERTS];
+  __shared__ double best[HS_MAX_TOP];
   const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (p.mask && !p.mask[t]) {
-    if ((int)threadIdx.x < p.top) {
-      w.chosen[t * p.top + lane] = -1;
-      w.weights[t * p.top + lane] = 0.0f;
-      if (p.chosen) p.chosen[t * p.top + lane] = -1;
-      if (p.weights) p.weights[t * p.top + lane] = 0.0f;
-    }
-    return;
-  }
-  const T* const x = (const T*)p.x + t * p.x_stride;
-  constexpr int kAtOnce = 4;
-  for (int e0 = wave; e0 < p.experts; e0 += 4 * kAtOnce) {
-    double sum[kAtOnce] = {};
-    for (int c = 8 * lane; c < p.channels; c += 512) {
-      const x8 a = *(const x8*)(x + c);
+  int32_t* const chosen = w.chosen + t * p.top;
+  float* const weights = w.weights + t * p.top;
+  int32_t* const user_chosen = p.chosen ? p.chosen + t * p.top : nullptr;
+  float* const user_weights = p.weights ? p.weights + t * p.top : nullptr;
+  const bool here = !p.mask || p.mask[t];
+  if (here) {
+    const T* const x = (const T*)p.x + t * p.x_stride;
+    constexpr int kAtOnce = 8;
+    for (int e0 = kAtOnce * wave; e0 < p.experts; e0 += 4 * kAtOnce) {
+      double sum[kAtOnce] = {};
+      for (int c = 8 * lane; c < p.channels; c += 512) {
+        const x8 a = __builtin_bit_cast(x8, load16(x + c));
+        x8 r[kAtOnce];
 #pragma unroll
-      for (int n = 0; n < kAtOnce; ++n) {
-        const int e = min(e0 + 4 * n, p.experts - 1);
-        const x8 r = *(const x8*)((const T*)p.router + (int64_t)e * p.channels + c);
+        for (int n = 0; n < kAtOnce; ++n) r[n] = __builtin_bit_cast(x8, load16((const T*)p.router + (int64_t)min(e0 + n, p.experts - 1) * p.channels + c));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[n] = fma((double)(float)a[i], (double)(float)r[i], sum[n]);
+        for (int n = 0; n < kAtOnce; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[n] = fma((double)(float)a[i], (double)(float)r[n][i], sum[n]);
       }
+#pragma unroll
+      for (int half = kAtOnce / 2; half > 0; half /= 2) {     // lane bits 2, 1, 0: which of the eight a lane goes on with
+        const bool upper = lane & half;
+#pragma unroll
+        for (int n = 0; n < half; ++n) {
+          const double mine = upper ? sum[n + half] : sum[n], theirs = upper ? sum[n] : sum[n + half];
+          sum[n] = mine + __shfl_xor(theirs, half);
+        }
+      }
+#pragma unroll
+      for (int d = kAtOnce; d < 64; d *= 2) sum[0] += __shfl_xor(sum[0], d);
+      if (lane < kAtOnce && e0 + lane < p.experts) ranks[e0 + lane] = rank_of(sum[0]);
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-#pragma unroll
-      for (int n = 0; n < kAtOnce; ++n) sum[n] += __shfl_xor(sum[n], d);
-#pragma unroll
-    for (int n = 0; n < kAtOnce; ++n)
-      if (lane == n && e0 + 4 * n < p.experts) scores[e0 + 4 * n] = sum[n];
   }
   __syncthreads();
   if (wave > 0) return;
-  double score[HS_MAX_EXPERTS / 64];
-#pragma unroll
-  for (int i = 0; i < HS_MAX_EXPERTS / 64; ++i) score[i] = lane + 64 * i < p.experts ? scores[lane + 64 * i] : 0.0;
-  double best[HS_MAX_TOP];
-  uint32_t taken = 0;
-  double most = 0.0;
-  for (int n = 0; n < p.top; ++n) {
-    uint64_t rank = 0;
-    int index = INT32_MAX;
-    double value = 0.0;
-#pragma unroll
-    for (int i = 0; i < HS_MAX_EXPERTS / 64; ++i) {
-      if (lane + 64 * i >= p.experts || taken >> i & 1) continue;
-      const uint64_t r = rank_of(score[i]);
-      if (index == INT32_MAX || r > rank) rank = r, index = lane + 64 * i, value = score[i];
-    }
-    for (int d = 1; d < 64; d *= 2) {
-      const uint64_t r = __shfl_xor(rank, d);
-      const int other = __shfl_xor(index, d);
-      const double v = __shfl_xor(value, d);
-      if (other != INT32_MAX && (index == INT32_MAX || r > rank || (r == rank && other < index))) rank = r, index = other, value = v;
-    }
-    if ((index & 63) == lane) taken |= 1u << (index >> 6);
-    if (n == 0) most = value;
-    if (lane == n) {
-      w.chosen[t * p.top + n] = index;
-      if (p.chosen) p.chosen[t * p.top + n] = index;
-    }
-#pragma unroll
-    for (int i = 0; i < HS_MAX_TOP; ++i)
-      if (i == n) best[i] = value;
-  }
-  double total = 0.0;
-  if (p.renormalise) {
-#pragma unroll
-    for (int i = 0; i < HS_MAX_TOP; ++i)
-      if (i < p.top) total += exp(best[i] - most);
-  } else {
-#pragma unroll
-    for (int i = 0; i < HS_MAX_EXPERTS / 64; ++i)
-      if (lane + 64 * i < p.experts) total += exp(score[i] - most);
-    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
-  }
-#pragma unroll
-  for (int i = 0; i < HS_MAX_TOP; ++i)
-    if (i < p.top && lane == i) {
-      const float weight = (float)(exp(best[i] - most) / total);
-      w.weights[t * p.top + i] = weight;
-      if (p.weights) p.weights[t * p.top + i] = weight;
-    }
+  if (here) choose(p, ranks, best, chosen, weights, user_chosen, user_weights);
+  else choose_none(p, chosen, weights, user_chosen, user_weights);
 }
 
-// The pairs (token, place) that chose expert e, in their order: those numbered first .. first + most - 1 of them are left in
-// `list`; returns how many these are.  For a whole workgroup of 256.
-__device__ __forceinline__ int pairs_of(const ExpertParams& p, const int32_t* chosen, int e, int first, int most, int32_t* list, int* counts) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = p.tokens * p.top;
-  int seen = 0;
-  for (int at = 0; at < pairs && seen < first + most; at += 256) {
-    const int i = at + threadIdx.x;
-    const bool hit = i < pairs && chosen[i] == e;
-    const uint64_t hits = __ballot(hit);
-    if (lane == 0) counts[wave] = __popcll(hits);
-    __syncthreads();
-    int place = seen + __popcll(hits & ((1ull << lane) - 1));
-    for (int n = 0; n < 4; ++n) {
-      if (n < wave) place += counts[n];
-      seen += counts[n];
-    }
-    if (hit && place >= first && place < first + most) list[place - first] = i;
-    __syncthreads();
-  }
-  return min(max(seen - first, 0), most);
-}
-
-// Products of RT tiles of 16 weight rows with NT tiles of 16 vectors over steps first .. last - 1 of 64: a lane has 16 values side by
-// side of a row, so that four lanes read 128 bytes of it, and of a vector; the matrix pipe takes them in the same order.
-// Lane l has result [row 4 * (l / 16) + i][vector l % 16].  A step's loads are issued before the products of the one before.
-template <class T, int RT, int NT, bool POWERS>
-__device__ __forceinline__ void products(const T* const (&rows)[RT], const T* const (&vectors)[NT], const int16_t* const (&power)[NT],
-                                         const int (&row_power)[NT], int first, int last, int length, f32x4 (&acc)[RT][NT]) {
+// The same for up to 16 tokens and kFusedExperts experts, in a workgroup of 16 waves that goes on with the result, by matrix products in 64
+// bits: a wave has 16 experts and every 4th to 16th 32 channels, then a token.  The choice is left in `place` and `weights` in LDS;
+// `publish`: in memory as well.
+constexpr int kFusedExperts = 64;
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+struct RouteLds {
+  double part[16 * 16 * 16];                         // [share of the channels][token][expert]
+  uint64_t ranks[16][kFusedExperts];
+  double best[16][HS_MAX_TOP];
+  int32_t chosen[16][HS_MAX_TOP];
+  float weights[16][HS_MAX_TOP];
+  int8_t place[kFusedExperts][16];
+};
+template <class T>
+__device__ __forceinline__ void route_here(const ExpertParams& p, const ExpertParts& w, RouteLds& lds, bool publish) {
   typedef typename Vec<T>::x8 x8;
-  const int g = (threadIdx.x & 63) >> 4;
-  struct Step {
-    x8 a[RT][2], b[NT][2];
-    int16_t power[NT];
-  };
-  auto load = [&](int step, Step& s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
+  const int tiles = p.experts <= 16 ? 1 : p.experts <= 32 ? 2 : 4, shares = 16 / tiles, share = wave / tiles, e0 = 16 * (wave % tiles);
+  ((int32_t*)lds.place)[threadIdx.x & 255] = -1;
+  const T* const x = (const T*)p.x + min(row, p.tokens - 1) * p.x_stride;
+  const T* const r = (const T*)p.router + (int64_t)min(e0 + row, p.experts - 1) * p.channels;
+  f64x4 sum = {};
+  for (int c = 32 * share; c < p.channels; c += 32 * shares) {
+    const int c0 = min(c + 8 * g, p.channels - 8);
+    x8 a = __builtin_bit_cast(x8, load16(x + c0)), b = __builtin_bit_cast(x8, load16(r + c0));
+    if (c + 8 * g >= p.channels) a = b = x8{};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int d0 = min(64 * step + 16 * g + 8 * e, length - 8);   // (what lies behind the row's end is left out below)
+    for (int i = 0; i < 8; ++i) sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(float)a[i], (double)(float)b[i], sum, 0, 0, 0);
+  }
 #pragma unroll
-      for (int r = 0; r < RT; ++r) s.a[r][e] = __builtin_bit_cast(x8, load16(rows[r] + d0));
-#pragma unroll
-      for (int n = 0; n < NT; ++n) s.b[n][e] = __builtin_bit_cast(x8, load16(vectors[n] + d0));
+  for (int i = 0; i < 4; ++i) lds.part[(share * 16 + g + 4 * i) * 16 * tiles + e0 + row] = sum[i];   // (row g + 4 i of the result, in 64 bits)
+  __syncthreads();
+  const int t = wave;
+  if (t < p.tokens) {
+    int32_t* const user_chosen = publish && p.chosen ? p.chosen + t * p.top : nullptr;
+    float* const user_weights = publish && p.weights ? p.weights + t * p.top : nullptr;
+    if (p.mask && !p.mask[t]) {
+      choose_none(p, lds.chosen[t], lds.weights[t], user_chosen, user_weights);
+    } else {
+      if (lane < p.experts) {
+        double score = 0.0;
+        for (int n = 0; n < shares; ++n) score += lds.part[(n * 16 + t) * 16 * tiles + lane];
+        lds.ranks[t][lane] = rank_of(score);
+      }
+      wave_order();
+      choose(p, lds.ranks[t], lds.best[t], lds.chosen[t], lds.weights[t], user_chosen, user_weights);
+      wave_order();
+      if (lane < p.top) lds.place[lds.chosen[t][lane]][t] = lane;
     }
-    if (POWERS)
+    wave_order();
+    if (publish && lane < p.top) {
+      w.chosen[t * p.top + lane] = lds.chosen[t][lane];
+      w.weights[t * p.top + lane] = lds.weights[t][lane];
+    }
+  }
+  __syncthreads();
+}
+
+// ---- few tokens: strips of 16 weight rows
+
+// 64 values of each of RT * 16 weight rows and NT * 16 vectors: a lane has 16 values side by side of a row, so that four lanes read 128 bytes
+// of it, and of a vector; the matrix pipe takes them in the same order.  Lane l has result [row 4 * (l / 16) + i][vector l % 16].
+template <class T, int RT, int NT>
+struct Strip {
+  typedef typename Vec<T>::x8 x8;
+  x8 a[RT][2], b[NT][2];
+  static __device__ __forceinline__ int place(int step, int e, int length) {       // (what lies behind the row's end is left out below)
+    return min(64 * step + 16 * (int)((threadIdx.x & 63) >> 4) + 8 * e, length - 8);
+  }
+  __device__ __forceinline__ void load_rows(const T* const (&rows)[RT], int step, int length) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s.power[n] = power[n][min(64 * step + 16 * g, length - 1) / kSlice];
-  };
-  auto multiply = [&](int step, Step& s) {
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) a[r][e] = __builtin_bit_cast(x8, load16(rows[r] + place(step, e, length)));
+  }
+  __device__ __forceinline__ void load_vectors(const T* const (&vectors)[NT], int step, int length) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) b[n][e] = __builtin_bit_cast(x8, load16(vectors[n] + place(step, e, length)));
+  }
+  __device__ __forceinline__ void multiply(int step, int length, f32x4 (&acc)[RT][NT]) {
+    const int g = (threadIdx.x & 63) >> 4;
     if (64 * step + 64 > length) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         if (64 * step + 16 * g + 8 * e >= length) {
 #pragma unroll
-          for (int r = 0; r < RT; ++r) s.a[r][e] = x8{};
+          for (int r = 0; r < RT; ++r) a[r][e] = x8{};
 #pragma unroll
-          for (int n = 0; n < NT; ++n) s.b[n][e] = x8{};
+          for (int n = 0; n < NT; ++n) b[n][e] = x8{};
         }
     }
-    if (POWERS)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const T f = (T)ldexpf(1.0f, max(s.power[n] - row_power[n], -40));
-        s.b[n][0] *= f;
-        s.b[n][1] *= f;
-      }
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[r][n] = mfma16(s.a[r][e], s.b[n][e], acc[r][n]);
-  };
-  Step even, odd;
-  if (first < last) load(first, even);
-  for (int step = first; step < last; step += 2) {
-    if (step + 1 < last) load(step + 1, odd);
-    multiply(step, even);
-    if (step + 1 >= last) break;
-    if (step + 2 < last) load(step + 2, even);
-    multiply(step + 1, odd);
+        for (int n = 0; n < NT; ++n) acc[r][n] = mfma16(a[r][e], b[n][e], acc[r][n]);
   }
+};
+
+// The strips first .. last - 1 of a wave.  The first two strips' rows are on their way (begin) while the caller finds out which
+// vectors they are for (go on).
+template <class T, int RT, int NT>
+struct Strips {
+  Strip<T, RT, NT> even, odd;
+  int first, last, length;
+  __device__ __forceinline__ void begin(const T* const (&rows)[RT]) {
+    if (first < last) even.load_rows(rows, first, length);
+    if (first + 1 < last) odd.load_rows(rows, first + 1, length);
+  }
+  // `prepare`: what is to be done to a strip's vectors before they are multiplied
+  template <class F>
+  __device__ __forceinline__ void go_on(const T* const (&rows)[RT], const T* const (&vectors)[NT], f32x4 (&acc)[RT][NT], F&& prepare) {
+    if (first < last) even.load_vectors(vectors, first, length);
+    for (int step = first; step < last; step += 2) {
+      if (step + 1 < last) odd.load_vectors(vectors, step + 1, length);
+      prepare(step, even);
+      even.multiply(step, length, acc);
+      if (step + 1 >= last) break;
+      if (step + 2 < last) {
+        even.load_rows(rows, step + 2, length);
+        even.load_vectors(vectors, step + 2, length);
+      }
+      prepare(step + 1, odd);
+      odd.multiply(step + 1, length, acc);
+      if (step + 3 < last) odd.load_rows(rows, step + 3, length);
+    }
+  }
+};
+
+// The hidden value u of 16 from its gate and its other sum, for 16 threads side by side, which agree on the power of two that fp16 takes out.
+template <class T>
+__device__ __forceinline__ void store_hidden(const ExpertParams& p, const ExpertParts& w, int64_t pair, int slice, int u, bool there, float gate, float up) {
+  float h = gate / (1.0f + expf(-gate)) * up;
+  const bool stored = there && kSlice * slice + u < p.hidden;
+  if (__is_same(T, f16)) {
+    float most = stored ? fabsf(h) : 0.0f;
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    const int power = most > 0.0f && most < INFINITY ? ilogbf(most) - 14 : most > 0.0f ? 0 : kNoPower;
+    if (power != kNoPower) h = ldexpf(h, -power);
+    if (stored && u == 0) w.power[pair * slices_of(p) + slice] = power;
+  }
+  if (stored) ((T*)w.hidden)[pair * p.hidden + kSlice * slice + u] = (T)h;
 }
 
-constexpr int kNoPower = -1000;   // of a slice of zeros
-
-// Hidden layer: a workgroup has an expert, 16 of its hidden values and up to 16 * NT of its tokens; its four waves take a quarter
-// of the channels each.
-template <class T, int NT>
-__global__ __launch_bounds__(256) void k_expert_in(ExpertParams p, ExpertParts w, int groups) {
-  __shared__ int32_t list[16 * NT];
-  __shared__ int counts[4];
-  __shared__ f32x4 partial[4][2][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
-  int id = xcd_number();
-  const int group = id % groups, slices = slices_of(p);
-  id /= groups;
-  const int slice = id % slices, e = id / slices;
-  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
-  if (n == 0) return;
-  const T* vectors[NT];                              // (a place without a token has the first's, and is left out below)
-  const int16_t* none[NT] = {};
-  int zero[NT] = {};
-#pragma unroll
-  for (int i = 0; i < NT; ++i) vectors[i] = (const T*)p.x + (int64_t)(list[16 * i + col < n ? 16 * i + col : 0] / p.top) * p.x_stride;
-  const T* const gate = (const T*)p.w_in + ((int64_t)e * 2 * p.hidden + min(16 * slice + col, p.hidden - 1)) * p.channels;
+// A frame's tokens, up to 16: the choice and the hidden layer.  A workgroup has an expert and 64 of its hidden values, 16 for every four waves,
+// which take a quarter of the channels each; every workgroup works the choice out by itself, which costs less than a launch for it, and
+// each token has a column of the products, whether it chose the expert or not.
+// ahead: the first weights are asked for before it is known whether some token needs them.
+template <class T>
+__global__ __launch_bounds__(1024) void k_expert_frame(ExpertParams p, ExpertParts w, int ahead) {
+  __shared__ union {
+    RouteLds route;
+    f32x4 partial[16][2][64];
+  } lds;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, block = wave >> 2, quarter = wave & 3;
+  const int id = xcd_number(), groups = (slices_of(p) + 3) / 4, slice = id % groups * 4 + block, e = id / groups;
+  const T* const gate = (const T*)p.w_in + ((int64_t)e * 2 * p.hidden + min(kSlice * slice + col, p.hidden - 1)) * p.channels;
   const T* const rows[2] = {gate, gate + (int64_t)p.hidden * p.channels};
+  const T* const vectors[1] = {(const T*)p.x + min(col, p.tokens - 1) * p.x_stride};     // (columns without a token are left out below)
   const int steps = (p.channels + 63) / 64;
-  f32x4 acc[2][NT] = {};
-  products<T, 2, NT, false>(rows, vectors, none, zero, steps * wave / 4, steps * (wave + 1) / 4, p.channels, acc);
+  Strips<T, 2, 1> strips;
+  strips.first = steps * quarter / 4;
+  strips.last = steps * (quarter + 1) / 4;
+  strips.length = p.channels;
+  if (ahead) strips.begin(rows);
+  route_here<T>(p, w, lds.route, id == 0);
+  const int u = threadIdx.x & 15, at = threadIdx.x >> 4 & 15, from = (u >> 2) * 16 + at;     // thread t finishes value t % 16 of token t / 16 % 16
+  const int place = at < p.tokens ? lds.route.place[e][at] : -1;
+  if (!__syncthreads_or(place >= 0)) return;
+  if (!ahead) strips.begin(rows);
+  f32x4 acc[2][1] = {};
+  strips.go_on(rows, vectors, acc, [](int, Strip<T, 2, 1>&) {});
+  lds.partial[wave][0][lane] = acc[0][0];
+  lds.partial[wave][1][lane] = acc[1][0];
+  __syncthreads();
+  float y[2];
 #pragma unroll
   for (int r = 0; r < 2; ++r)
-#pragma unroll
-    for (int i = 0; i < NT; ++i) partial[wave][r][i][lane] = acc[r][i];
-  __syncthreads();
-  // thread t: hidden value t % 16 of token t / 16
-  const int u = threadIdx.x & 15, at = threadIdx.x >> 4, from = (u >> 2) * 16 + at;
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    if (16 * i >= n) break;
-    float y[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-      y[r] = (partial[0][r][i][from][u & 3] + partial[1][r][i][from][u & 3]) + (partial[2][r][i][from][u & 3] + partial[3][r][i][from][u & 3]);
-    float h = y[0] / (1.0f + expf(-y[0])) * y[1];
-    const bool stored = 16 * i + at < n && 16 * slice + u < p.hidden;
-    const int64_t pair = list[min(16 * i + at, n - 1)];
-    if (__is_same(T, f16)) {
-      float most = stored ? fabsf(h) : 0.0f;
-#pragma unroll
-      for (int d = 1; d < 16; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-      const int power = most > 0.0f && most < INFINITY ? ilogbf(most) - 14 : most > 0.0f ? 0 : kNoPower;
-      if (power != kNoPower) h = ldexpf(h, -power);
-      if (stored && u == 0) w.power[pair * slices + slice] = power;
-    }
-    if (stored) ((T*)w.hidden)[pair * p.hidden + 16 * slice + u] = (T)h;
-  }
+    y[r] = (lds.partial[4 * block][r][from][u & 3] + lds.partial[4 * block + 1][r][from][u & 3])
+         + (lds.partial[4 * block + 2][r][from][u & 3] + lds.partial[4 * block + 3][r][from][u & 3]);
+  store_hidden<T>(p, w, (int64_t)at * p.top + place, slice, u, place >= 0, y[0], y[1]);
 }
 
-// What comes out of an expert: 16 channels per workgroup, a quarter of the hidden values per wave.
-template <class T, int NT>
-__global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts w, int groups) {
-  __shared__ int32_t list[16 * NT];
-  __shared__ int counts[4];
-  __shared__ f32x4 partial[4][NT][64];
-  __shared__ int powers[16 * NT];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
-  int id = xcd_number();
-  const int group = id % groups, blocks = (p.channels + 15) / 16, slices = slices_of(p);
-  id /= groups;
-  const int block = id % blocks, e = id / blocks;
-  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
-  if (n == 0) return;
-  constexpr bool kPowers = __is_same(T, f16);
-  if (kPowers) {
-    const int at = threadIdx.x >> 4;
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      if (16 * i + at >= n) break;
-      const int16_t* const power = w.power + (int64_t)list[16 * i + at] * slices;
-      int most = kNoPower;
-      for (int s = threadIdx.x & 15; s < slices; s += 16) most = max(most, (int)power[s]);
-#pragma unroll
-      for (int d = 1; d < 16; d *= 2) most = max(most, __shfl_xor(most, d));
-      if ((threadIdx.x & 15) == 0) powers[16 * i + at] = most;
-    }
-    __syncthreads();
-  }
-  const T* vectors[NT];
-  const int16_t* power[NT];
-  int row_power[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int at = 16 * i + col < n ? 16 * i + col : 0;
-    const int64_t pair = list[at];
-    vectors[i] = (const T*)w.hidden + pair * p.hidden;
-    power[i] = w.power + pair * slices;
-    row_power[i] = kPowers ? powers[at] : 0;
-  }
-  const T* const rows[1] = {(const T*)p.w_out + ((int64_t)e * p.channels + min(16 * block + col, p.channels - 1)) * p.hidden};
-  const int steps = (p.hidden + 63) / 64;
-  f32x4 acc[1][NT] = {};
-  products<T, 1, NT, kPowers>(rows, vectors, power, row_power, steps * wave / 4, steps * (wave + 1) / 4, p.hidden, acc);
-#pragma unroll
-  for (int i = 0; i < NT; ++i) partial[wave][i][lane] = acc[0][i];
-  __syncthreads();
-  const int u = threadIdx.x & 15, at = threadIdx.x >> 4, from = (u >> 2) * 16 + at;
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    if (16 * i + at >= n || 16 * block + u >= p.channels) break;
-    const int64_t pair = list[16 * i + at];
-    float y = (partial[0][i][from][u & 3] + partial[1][i][from][u & 3]) + (partial[2][i][from][u & 3] + partial[3][i][from][u & 3]);
-    if (kPowers) y = powers[16 * i + at] == kNoPower ? y : ldexpf(y, powers[16 * i + at]);
-    w.products[pair * p.channels + 16 * block + u] = w.weights[pair] * y;
-  }
-}
-
-// The pairs that chose each expert, a workgroup per expert: a thread looks at 16 pairs side by side.
-__global__ __launch_bounds__(256) void k_expert_lists(ExpertParams p, ExpertParts w) {
-  __shared__ int counts[4];
-  const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = p.tokens * p.top;
+// The pairs (token, place) that chose expert e, in their order: those numbered first .. first + most - 1 of them are left in
+// `list`; returns how many these are.  For a whole workgroup of 256, a thread of which looks at 16 pairs side by side.
+__device__ __forceinline__ int pairs_of(const ExpertParams& p, const int32_t* chosen, int e, int first, int most, int32_t* list, int* counts) {
+  typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = p.tokens * p.top;
   int seen = 0;
   for (int at = 0; at < pairs; at += 4096) {
-    const int first = at + 16 * threadIdx.x;
+    const int own = at + 16 * threadIdx.x;
     uint32_t hits = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (first + i < pairs && w.chosen[first + i] == e) hits |= 1u << i;
+    for (int i = 0; i < 16; i += 4) {
+      // (the array's room is a multiple of 256 bytes: what lies behind its end is read, and not looked at)
+      const i32x4 c = own + i < pairs ? *(const i32x4*)(chosen + own + i) : i32x4{};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (own + i + j < pairs && c[j] == e) hits |= 1u << (i + j);
+    }
     int before = __popc(hits);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -360,11 +367,126 @@ __global__ __launch_bounds__(256) void k_expert_lists(ExpertParams p, ExpertPart
       if (n < wave) place += counts[n];
       seen += counts[n];
     }
-    for (; hits; hits &= hits - 1) w.list[(int64_t)e * p.tokens + place++] = first + __ffs(hits) - 1;
+    for (; hits; hits &= hits - 1, ++place)
+      if (place >= first && place < first + most) list[place - first] = own + __ffs(hits) - 1;
     __syncthreads();
   }
-  if (threadIdx.x == 0) w.count[e] = seen;
+  return min(max(seen - first, 0), most);
 }
+
+// Hidden layer: a workgroup has an expert, 16 of its hidden values and up to 16 * NT of its tokens; its four waves take a quarter of the
+// channels each.
+template <class T, int NT>
+__global__ __launch_bounds__(256) void k_expert_in(ExpertParams p, ExpertParts w, int ahead) {
+  __shared__ int32_t list[16 * NT];
+  __shared__ int counts[4];
+  __shared__ f32x4 partial[4][2][NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, slices = slices_of(p);
+  const int per_group = slices * p.experts, group = blockIdx.x / per_group, slice = blockIdx.x % per_group % slices, e = blockIdx.x % per_group / slices;
+  const T* const gate = (const T*)p.w_in + ((int64_t)e * 2 * p.hidden + min(kSlice * slice + col, p.hidden - 1)) * p.channels;
+  const T* const rows[2] = {gate, gate + (int64_t)p.hidden * p.channels};
+  const int steps = (p.channels + 63) / 64;
+  Strips<T, 2, NT> strips;
+  strips.first = steps * wave / 4;
+  strips.last = steps * (wave + 1) / 4;
+  strips.length = p.channels;
+  const bool early = ahead && group == 0;
+  if (early) strips.begin(rows);
+  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
+  if (n == 0) return;
+  if (!early) strips.begin(rows);
+  const T* vectors[NT];                              // (a place without a token has the first's, and is left out below)
+#pragma unroll
+  for (int i = 0; i < NT; ++i) vectors[i] = (const T*)p.x + (int64_t)(list[16 * i + col < n ? 16 * i + col : 0] / p.top) * p.x_stride;
+  f32x4 acc[2][NT] = {};
+  strips.go_on(rows, vectors, acc, [](int, Strip<T, 2, NT>&) {});
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) partial[wave][r][i][lane] = acc[r][i];
+  __syncthreads();
+  const int u = threadIdx.x & 15, at = threadIdx.x >> 4, from = (u >> 2) * 16 + at;   // thread t finishes value t % 16 of token t / 16
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    if (16 * i >= n) break;
+    float y[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+      y[r] = (partial[0][r][i][from][u & 3] + partial[1][r][i][from][u & 3]) + (partial[2][r][i][from][u & 3] + partial[3][r][i][from][u & 3]);
+    store_hidden<T>(p, w, list[min(16 * i + at, n - 1)], slice, u, 16 * i + at < n, y[0], y[1]);
+  }
+}
+
+// What comes out of an expert: 16 channels per workgroup, a quarter of the hidden values per wave.
+template <class T, int NT>
+__global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts w, int ahead) {
+  constexpr bool kPowers = __is_same(T, f16);
+  __shared__ int32_t list[16 * NT];
+  __shared__ int counts[4], powers[16 * NT];
+  __shared__ f32x4 partial[4][NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, slices = slices_of(p);
+  const int blocks = (p.channels + 15) / 16, per_group = blocks * p.experts;
+  const int group = blockIdx.x / per_group, block = blockIdx.x % per_group % blocks, e = blockIdx.x % per_group / blocks;
+  const T* const rows[1] = {(const T*)p.w_out + ((int64_t)e * p.channels + min(16 * block + col, p.channels - 1)) * p.hidden};
+  const int steps = (p.hidden + 63) / 64;
+  Strips<T, 1, NT> strips;
+  strips.first = steps * wave / 4;
+  strips.last = steps * (wave + 1) / 4;
+  strips.length = p.hidden;
+  const bool early = ahead && group == 0;
+  if (early) strips.begin(rows);
+  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
+  if (n == 0) return;
+  if (!early) strips.begin(rows);
+  const int u = threadIdx.x & 15, at = threadIdx.x >> 4, from = (u >> 2) * 16 + at;
+  if (kPowers) {                                     // a token's largest power, by 16 threads
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      if (16 * i + at >= n) break;
+      const int16_t* const power = w.power + (int64_t)list[16 * i + at] * slices;
+      int most = kNoPower;
+      for (int s = u; s < slices; s += 16) most = max(most, (int)power[s]);
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) most = max(most, __shfl_xor(most, d));
+      if (u == 0) powers[16 * i + at] = most;
+    }
+    __syncthreads();
+  }
+  const T* vectors[NT];
+  const int16_t* power[NT];
+  int row_power[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int place = 16 * i + col < n ? 16 * i + col : 0;
+    const int64_t pair = list[place];
+    vectors[i] = (const T*)w.hidden + pair * p.hidden;
+    power[i] = w.power + pair * slices;
+    row_power[i] = kPowers ? powers[place] : 0;
+  }
+  f32x4 acc[1][NT] = {};
+  strips.go_on(rows, vectors, acc, [&](int step, Strip<T, 1, NT>& strip) {
+    if (!kPowers) return;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const T f = (T)ldexpf(1.0f, max(power[i][min(4 * step + (lane >> 4), slices - 1)] - row_power[i], -40));
+      strip.b[i][0] *= f;
+      strip.b[i][1] *= f;
+    }
+  });
+#pragma unroll
+  for (int i = 0; i < NT; ++i) partial[wave][i][lane] = acc[0][i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    if (16 * i + at >= n || 16 * block + u >= p.channels) break;
+    const int64_t pair = list[16 * i + at];
+    float y = (partial[0][i][from][u & 3] + partial[1][i][from][u & 3]) + (partial[2][i][from][u & 3] + partial[3][i][from][u & 3]);
+    if (kPowers && powers[16 * i + at] != kNoPower) y = ldexpf(y, powers[16 * i + at]);
+    w.products[pair * p.channels + 16 * block + u] = w.weights[pair] * y;
+  }
+}
+
+// ---- more tokens: tiles of 128 weight rows
 
 // Either product for many tokens of an expert: a workgroup has 128 hidden values (IN: 128 rows of each of the two weights) or channels
 // and up to 32 * NT of the expert's tokens, 32 rows per wave.  Weights go from memory into the registers that multiply them, as
@@ -376,15 +498,15 @@ __global__ __launch_bounds__(256, 2) void k_expert_tiles(ExpertParams p, ExpertP
   constexpr int RT = IN ? 2 : 1, kTile = 32 * NT * 128;
   constexpr bool kPowers = __is_same(T, f16);
   __shared__ __align__(16) char lds[2 * kTile];
-  __shared__ int powers[32 * NT];
+  __shared__ int powers[32 * NT], counts[4];
+  __shared__ int32_t list[32 * NT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int rows = IN ? p.hidden : p.channels, length = IN ? p.channels : p.hidden, blocks = (rows + 127) / 128, slices = slices_of(p);
-  // the groups of the tokens behind the first, most often empty, come last
+  // The groups of the tokens behind the first, most of them empty, come last: dealt out among the others, those would leave CUs without work.
   const int per_group = blocks * p.experts, group = blockIdx.x / per_group;
   const int id = blockIdx.x % per_group, block = id % blocks, e = id / blocks;
-  const int n = min(w.count[e] - group * 32 * NT, 32 * NT);
-  if (n <= 0) return;
-  const int32_t* const list = w.list + (int64_t)e * p.tokens + group * 32 * NT;
+  const int n = pairs_of(p, w.chosen, e, group * 32 * NT, 32 * NT, list, counts);
+  if (n == 0) return;
 
   // staging: this thread's 16 bytes of vectors r0 + 32 i
   const int r0 = threadIdx.x >> 3, ch = threadIdx.x & 7;
@@ -452,6 +574,7 @@ __global__ __launch_bounds__(256, 2) void k_expert_tiles(ExpertParams p, ExpertP
         for (int r = 0; r < RT; ++r) s.a[r][k] = x8{};
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
+        if (32 * i >= n) break;
         const x8 b = *(const x8*)(here + koff[k] + i * 32 * 128);
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[r][i] = mfma32(s.a[r][k], b, acc[r][i]);
@@ -532,34 +655,34 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertParams p, ExpertParts 
 }
 
 template <class T, int NT>
+hipError_t launch_few(const ExpertParams& p, bool frame, void** args, hipStream_t stream) {
+  int ahead = (int64_t)p.tokens * p.top >= p.experts;
+  void* all[] = {args[0], args[1], &ahead};
+  const int64_t groups = (p.tokens + 16 * NT - 1) / (16 * NT);
+  const hipError_t e = frame ? launch_kernel((const void*)k_expert_frame<T>, (int64_t)p.experts * ((slices_of(p) + 3) / 4), 1024, all, stream)
+                             : launch_kernel((const void*)k_expert_in<T, NT>, p.experts * slices_of(p) * groups, 256, all, stream);
+  return e != hipSuccess ? e : launch_kernel((const void*)k_expert_out<T, NT>, p.experts * groups * ((p.channels + 15) / 16), 256, all, stream);
+}
+template <class T, int NT>
 hipError_t launch_tiles(const ExpertParams& p, void** args, hipStream_t stream) {
   int groups = (p.tokens + 32 * NT - 1) / (32 * NT);
   void* all[] = {args[0], args[1], &groups};
-  hipError_t e = launch_kernel((const void*)k_expert_lists, p.experts, 256, args, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_tiles<T, true, NT>, (int64_t)p.experts * ((p.hidden + 127) / 128) * groups, 256, all, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_tiles<T, false, NT>, (int64_t)p.experts * ((p.channels + 127) / 128) * groups, 256, all, stream);
-  return e;
-}
-template <class T>
-hipError_t launch_few(const ExpertParams& p, void** args, hipStream_t stream) {
-  int groups = 1;
-  void* all[] = {args[0], args[1], &groups};
-  hipError_t e = launch_kernel((const void*)k_expert_in<T, 1>, (int64_t)p.experts * slices_of(p), 256, all, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_out<T, 1>, (int64_t)p.experts * ((p.channels + 15) / 16), 256, all, stream);
-  return e;
+  const hipError_t e = launch_kernel((const void*)k_expert_tiles<T, true, NT>, (int64_t)p.experts * ((p.hidden + 127) / 128) * groups, 256, all, stream);
+  return e != hipSuccess ? e : launch_kernel((const void*)k_expert_tiles<T, false, NT>, (int64_t)p.experts * ((p.channels + 127) / 128) * groups, 256, all, stream);
 }
 template <class T>
 hipError_t launch_of(const ExpertParams& p, hipStream_t stream) {
   ExpertParams params = p;
   ExpertParts parts = parts_of(p);
   void* args[] = {&params, &parts};
-  hipError_t e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 256, args, stream);
+  const bool frame = p.tokens <= 16 && p.experts <= kFusedExperts && (p.experts + 15) / 16 * p.channels <= 2048;
+  hipError_t e = hipSuccess;
+  if (!frame) e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 256, args, stream);
+  if (e != hipSuccess) return e;
   const int64_t each = (int64_t)p.tokens * p.top / p.experts;          // tokens of an expert, on average
-  if (e == hipSuccess)
-    e = p.tokens <= 16 ? launch_few<T>(p, args, stream) : each <= 24 ? launch_tiles<T, 1>(p, args, stream)
-      : each <= 48 ? launch_tiles<T, 2>(p, args, stream) : launch_tiles<T, 4>(p, args, stream);
-  if (e == hipSuccess) e = launch_kernel((const void*)k_expert_sum<T>, ((int64_t)p.tokens * (p.channels / 8) + 255) / 256, 256, args, stream);
-  return e;
+  if (p.tokens <= kFewTokens) e = p.tokens <= 16 ? launch_few<T, 1>(p, frame, args, stream) : launch_few<T, 2>(p, false, args, stream);
+  else e = each <= 24 ? launch_tiles<T, 1>(p, args, stream) : each <= 48 ? launch_tiles<T, 2>(p, args, stream) : launch_tiles<T, 4>(p, args, stream);
+  return e != hipSuccess ? e : launch_kernel((const void*)k_expert_sum<T>, ((int64_t)p.tokens * (p.channels / 8) + 255) / 256, 256, args, stream);
 }
 }  // namespace
 

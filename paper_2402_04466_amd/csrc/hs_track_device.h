@@ -117,6 +117,13 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int batch, int 
   return __builtin_amdgcn_readfirstlane(lengths ? min(max(lengths[batch], 0), longest) : longest);
 }
 
+// The accesses of a wave to LDS before this come before those after it, whichever lane they are of.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ---- softmax by tiles of keys, of the attentions
 constexpr float kLog2e = 1.44269504088896340736f;
 // A row's maximum is only raised, and what it has summed only rescaled, when the scores have grown by
