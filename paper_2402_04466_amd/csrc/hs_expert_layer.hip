@@ -24,11 +24,12 @@ struct ExpertParts {            // the workspace
   int32_t* chosen;              // [tokens][top]
   float* weights;               // [tokens][top]
   void* hidden;                 // [tokens][top][hidden], in the inputs' type
-  int16_t* power;               // [tokens][top][slices of hidden], fp16
+  int16_t* power;               // [tokens][top][power_pitch()], fp16
   float* products;              // [tokens][top][channels]
   size_t bytes;
 };
 __host__ __device__ inline int slices_of(const ExpertParams& p) { return (p.hidden + kSlice - 1) / kSlice; }
+__host__ __device__ inline int power_pitch(const ExpertParams& p) { return (slices_of(p) + 7) / 8 * 8; }      // 16-byte pieces
 ExpertParts parts_of(const ExpertParams& p) {
   ExpertParts w;
   size_t at = 0;
@@ -41,7 +42,7 @@ ExpertParts parts_of(const ExpertParams& p) {
   w.chosen = (int32_t*)take(pairs * 4);
   w.weights = (float*)take(pairs * 4);
   w.hidden = take(pairs * p.hidden * 2);
-  w.power = (int16_t*)take(p.dtype == HS_F16 ? pairs * slices_of(p) * 2 : 0);
+  w.power = (int16_t*)take(p.dtype == HS_F16 ? pairs * power_pitch(p) * 2 : 0);
   w.products = (float*)take(pairs * p.channels * 4);
   w.bytes = at;
   return w;
@@ -58,48 +59,53 @@ __device__ __forceinline__ double score_of(uint64_t rank) {
   return rank == 0 ? __builtin_nan("") : __builtin_bit_cast(double, rank >> 63 ? rank & ~(1ull << 63) : ~rank);
 }
 
-// A token's choice by one wave, from the scores' ranks in LDS: an expert's place is the number of experts before it.  Left
-// there and, where a caller's arrays are given, with them; `best`: HS_MAX_TOP doubles in LDS of this wave's own.
-__device__ __forceinline__ void choose(const ExpertParams& p, const uint64_t* ranks, double* best, int32_t* chosen, float* weights, int32_t* user_chosen,
-                                       float* user_weights) {
+// A token's choice by one wave, from the scores' ranks in LDS: an expert's place is the number of experts before it.
+__device__ __forceinline__ void choose(const ExpertParams& p, const uint64_t* ranks, int32_t* chosen) {
   const int lane = threadIdx.x & 63;
-  for (int e = lane; e < p.experts; e += 64) {
-    const uint64_t own = ranks[e];
+  for (int e0 = 0; e0 < p.experts; e0 += 64) {
+    const int e = e0 + lane;
+    const uint64_t own = e < p.experts ? ranks[e] : 0;
     int place = 0;
-    for (int j = 0; j < p.experts; ++j) {
-      const uint64_t other = ranks[j];
-      place += other > own || (other == own && j < e);
+    for (int j0 = 0; j0 < p.experts; j0 += 64) {
+      const uint64_t theirs = j0 + lane < p.experts ? ranks[j0 + lane] : 0;
+      const int n = min(64, p.experts - j0);
+      for (int j = 0; j < n; ++j) {
+        const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(theirs >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)theirs, j);
+        place += other > own || (other == own && j0 + j < e);
+      }
     }
-    if (place < p.top) {
-      chosen[place] = e;
-      if (user_chosen) user_chosen[place] = e;
-      best[place] = score_of(own);
-    }
+    if (e < p.experts && place < p.top) chosen[place] = e;
   }
   wave_order();
-  const double most = best[0];
-  double total = 0.0;
-  if (p.renormalise) {
-    if (lane < p.top) total = exp(best[lane] - most);
-  } else {
-    for (int e = lane; e < p.experts; e += 64) total += exp(score_of(ranks[e]) - most);
+}
+
+// The chosen experts of token t, in LDS, and their weights to memory.
+__device__ __forceinline__ void publish(const ExpertParams& p, const ExpertParts& w, int t, const uint64_t* ranks, const int32_t* chosen) {
+  const int lane = threadIdx.x & 63;
+  const int e = chosen[lane < p.top ? lane : 0];
+  const double most = score_of(ranks[chosen[0]]), own = lane < p.top ? exp(score_of(ranks[e]) - most) : 0.0;
+  double total = own;
+  if (!p.renormalise) {
+    total = 0.0;
+    for (int i = lane; i < p.experts; i += 64) total += exp(score_of(ranks[i]) - most);
   }
   const int sharers = p.renormalise ? HS_MAX_TOP : 64;
   for (int d = 1; d < sharers; d *= 2) total += __shfl_xor(total, d);
-  if (lane < p.top) {
-    const float weight = (float)(exp(best[lane] - most) / total);
-    weights[lane] = weight;
-    if (user_weights) user_weights[lane] = weight;
-  }
+  if (lane >= p.top) return;
+  const float weight = (float)(own / total);
+  w.chosen[t * p.top + lane] = e;
+  w.weights[t * p.top + lane] = weight;
+  if (p.chosen) p.chosen[t * p.top + lane] = e;
+  if (p.weights) p.weights[t * p.top + lane] = weight;
 }
 
-__device__ __forceinline__ void choose_none(const ExpertParams& p, int32_t* chosen, float* weights, int32_t* user_chosen, float* user_weights) {
+__device__ __forceinline__ void publish_none(const ExpertParams& p, const ExpertParts& w, int t) {
   const int lane = threadIdx.x & 63;
   if (lane >= p.top) return;
-  chosen[lane] = -1;
-  weights[lane] = 0.0f;
-  if (user_chosen) user_chosen[lane] = -1;
-  if (user_weights) user_weights[lane] = 0.0f;
+  w.chosen[t * p.top + lane] = -1;
+  w.weights[t * p.top + lane] = 0.0f;
+  if (p.chosen) p.chosen[t * p.top + lane] = -1;
+  if (p.weights) p.weights[t * p.top + lane] = 0.0f;
 }
 
 // A workgroup per token: scores in 64 bits.  A wave has a quarter of the experts, eight at a time, a lane 8 of every 512 channels;
@@ -108,12 +114,8 @@ template <class T>
 __global__ __launch_bounds__(256) void k_expert_route(ExpertParams p, ExpertParts w) {
   typedef typename Vec<T>::x8 x8;
   __shared__ uint64_t ranks[HS_MAX_EXPERTS];
-  __shared__ double best[HS_MAX_TOP];
+  __shared__ int32_t chosen[HS_MAX_TOP];
   const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int32_t* const chosen = w.chosen + t * p.top;
-  float* const weights = w.weights + t * p.top;
-  int32_t* const user_chosen = p.chosen ? p.chosen + t * p.top : nullptr;
-  float* const user_weights = p.weights ? p.weights + t * p.top : nullptr;
   const bool here = !p.mask || p.mask[t];
   if (here) {
     const T* const x = (const T*)p.x + t * p.x_stride;
@@ -146,25 +148,26 @@ __global__ __launch_bounds__(256) void k_expert_route(ExpertParams p, ExpertPart
   }
   __syncthreads();
   if (wave > 0) return;
-  if (here) choose(p, ranks, best, chosen, weights, user_chosen, user_weights);
-  else choose_none(p, chosen, weights, user_chosen, user_weights);
+  if (here) {
+    choose(p, ranks, chosen);
+    publish(p, w, t, ranks, chosen);
+  } else {
+    publish_none(p, w, t);
+  }
 }
 
 // The same for up to 16 tokens and kFusedExperts experts, in a workgroup of 16 waves that goes on with the result, by matrix products in 64
-// bits: a wave has 16 experts and every 4th to 16th 32 channels, then a token.  The choice is left in `place` and `weights` in LDS;
-// `publish`: in memory as well.
+// bits: a wave has 16 experts and every 4th to 16th 32 channels, then a token.  The choice is left in LDS.
 constexpr int kFusedExperts = 64;
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 struct RouteLds {
   double part[16 * 16 * 16];                         // [share of the channels][token][expert]
   uint64_t ranks[16][kFusedExperts];
-  double best[16][HS_MAX_TOP];
   int32_t chosen[16][HS_MAX_TOP];
-  float weights[16][HS_MAX_TOP];
-  int8_t place[kFusedExperts][16];
+  int8_t place[kFusedExperts][16];                   // where in a token's choice the expert is, or -1
 };
 template <class T>
-__device__ __forceinline__ void route_here(const ExpertParams& p, const ExpertParts& w, RouteLds& lds, bool publish) {
+__device__ __forceinline__ void route_here(const ExpertParams& p, RouteLds& lds) {
   typedef typename Vec<T>::x8 x8;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
   const int tiles = p.experts <= 16 ? 1 : p.experts <= 32 ? 2 : 4, shares = 16 / tiles, share = wave / tiles, e0 = 16 * (wave % tiles);
@@ -183,27 +186,15 @@ __device__ __forceinline__ void route_here(const ExpertParams& p, const ExpertPa
   for (int i = 0; i < 4; ++i) lds.part[(share * 16 + g + 4 * i) * 16 * tiles + e0 + row] = sum[i];   // (row g + 4 i of the result, in 64 bits)
   __syncthreads();
   const int t = wave;
-  if (t < p.tokens) {
-    int32_t* const user_chosen = publish && p.chosen ? p.chosen + t * p.top : nullptr;
-    float* const user_weights = publish && p.weights ? p.weights + t * p.top : nullptr;
-    if (p.mask && !p.mask[t]) {
-      choose_none(p, lds.chosen[t], lds.weights[t], user_chosen, user_weights);
-    } else {
-      if (lane < p.experts) {
-        double score = 0.0;
-        for (int n = 0; n < shares; ++n) score += lds.part[(n * 16 + t) * 16 * tiles + lane];
-        lds.ranks[t][lane] = rank_of(score);
-      }
-      wave_order();
-      choose(p, lds.ranks[t], lds.best[t], lds.chosen[t], lds.weights[t], user_chosen, user_weights);
-      wave_order();
-      if (lane < p.top) lds.place[lds.chosen[t][lane]][t] = lane;
+  if (t < p.tokens && (!p.mask || p.mask[t])) {
+    if (lane < p.experts) {
+      double score = 0.0;
+      for (int n = 0; n < shares; ++n) score += lds.part[(n * 16 + t) * 16 * tiles + lane];
+      lds.ranks[t][lane] = rank_of(score);
     }
     wave_order();
-    if (publish && lane < p.top) {
-      w.chosen[t * p.top + lane] = lds.chosen[t][lane];
-      w.weights[t * p.top + lane] = lds.weights[t][lane];
-    }
+    choose(p, lds.ranks[t], lds.chosen[t]);
+    if (lane < p.top) lds.place[lds.chosen[t][lane]][t] = lane;
   }
   __syncthreads();
 }
@@ -282,6 +273,15 @@ struct Strips {
   }
 };
 
+__device__ __forceinline__ int most_of(const int16_t* power, int first, int slices) {      // of eight powers
+  const s16x8 eight = load16(power + first);
+  int most = kNoPower;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (first + i < slices) most = max(most, (int)eight[i]);
+  return most;
+}
+
 // The hidden value u of 16 from its gate and its other sum, for 16 threads side by side, which agree on the power of two that fp16 takes out.
 template <class T>
 __device__ __forceinline__ void store_hidden(const ExpertParams& p, const ExpertParts& w, int64_t pair, int slice, int u, bool there, float gate, float up) {
@@ -293,7 +293,7 @@ __device__ __forceinline__ void store_hidden(const ExpertParams& p, const Expert
     for (int d = 1; d < 16; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
     const int power = most > 0.0f && most < INFINITY ? ilogbf(most) - 14 : most > 0.0f ? 0 : kNoPower;
     if (power != kNoPower) h = ldexpf(h, -power);
-    if (stored && u == 0) w.power[pair * slices_of(p) + slice] = power;
+    if (stored && u == 0) w.power[pair * power_pitch(p) + slice] = power;
   }
   if (stored) ((T*)w.hidden)[pair * p.hidden + kSlice * slice + u] = (T)h;
 }
@@ -309,7 +309,8 @@ __global__ __launch_bounds__(1024) void k_expert_frame(ExpertParams p, ExpertPar
     f32x4 partial[16][2][64];
   } lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, block = wave >> 2, quarter = wave & 3;
-  const int id = xcd_number(), groups = (slices_of(p) + 3) / 4, slice = id % groups * 4 + block, e = id / groups;
+  const int id = xcd_number(), groups = (slices_of(p) + 3) / 4;
+  const int slice = id % groups * 4 + block, e = id / groups;
   const T* const gate = (const T*)p.w_in + ((int64_t)e * 2 * p.hidden + min(kSlice * slice + col, p.hidden - 1)) * p.channels;
   const T* const rows[2] = {gate, gate + (int64_t)p.hidden * p.channels};
   const T* const vectors[1] = {(const T*)p.x + min(col, p.tokens - 1) * p.x_stride};     // (columns without a token are left out below)
@@ -319,7 +320,15 @@ __global__ __launch_bounds__(1024) void k_expert_frame(ExpertParams p, ExpertPar
   strips.last = steps * (quarter + 1) / 4;
   strips.length = p.channels;
   if (ahead) strips.begin(rows);
-  route_here<T>(p, w, lds.route, id == 0);
+  route_here<T>(p, lds.route);
+  if (slice == block) {                              // an expert's first workgroup: that of one without a token, if there is any, leaves the choice in memory
+    const bool used = lane < p.experts && (*(const uint64_t*)lds.route.place[lane] & *(const uint64_t*)(lds.route.place[lane] + 8)) != ~0ull;
+    const uint64_t unused = ~__ballot(used) & (p.experts < 64 ? (1ull << p.experts) - 1 : ~0ull);
+    if (e == (unused ? __ffsll((unsigned long long)unused) - 1 : 0) && wave < p.tokens) {
+      if (!p.mask || p.mask[wave]) publish(p, w, wave, lds.route.ranks[wave], lds.route.chosen[wave]);
+      else publish_none(p, w, wave);
+    }
+  }
   const int u = threadIdx.x & 15, at = threadIdx.x >> 4 & 15, from = (u >> 2) * 16 + at;     // thread t finishes value t % 16 of token t / 16 % 16
   const int place = at < p.tokens ? lds.route.place[e][at] : -1;
   if (!__syncthreads_or(place >= 0)) return;
@@ -338,12 +347,12 @@ __global__ __launch_bounds__(1024) void k_expert_frame(ExpertParams p, ExpertPar
 }
 
 // The pairs (token, place) that chose expert e, in their order: those numbered first .. first + most - 1 of them are left in
-// `list`; returns how many these are.  For a whole workgroup of 256, a thread of which looks at 16 pairs side by side.
+// `list`; returns how many these are.  For a whole workgroup, a thread of which looks at 16 pairs side by side; `counts`: a place per wave.
 __device__ __forceinline__ int pairs_of(const ExpertParams& p, const int32_t* chosen, int e, int first, int most, int32_t* list, int* counts) {
   typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = p.tokens * p.top;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, pairs = p.tokens * p.top;
   int seen = 0;
-  for (int at = 0; at < pairs; at += 4096) {
+  for (int at = 0; at < pairs; at += 16 * blockDim.x) {
     const int own = at + 16 * threadIdx.x;
     uint32_t hits = 0;
 #pragma unroll
@@ -363,7 +372,7 @@ __device__ __forceinline__ int pairs_of(const ExpertParams& p, const int32_t* ch
     if (lane == 63) counts[wave] = before;
     __syncthreads();
     int place = seen + before - __popc(hits);
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < waves; ++n) {
       if (n < wave) place += counts[n];
       seen += counts[n];
     }
@@ -382,7 +391,7 @@ __global__ __launch_bounds__(256) void k_expert_in(ExpertParams p, ExpertParts w
   __shared__ int counts[4];
   __shared__ f32x4 partial[4][2][NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, slices = slices_of(p);
-  const int per_group = slices * p.experts, group = blockIdx.x / per_group, slice = blockIdx.x % per_group % slices, e = blockIdx.x % per_group / slices;
+  const int slice = blockIdx.x % slices, e = blockIdx.x / slices;
   const T* const gate = (const T*)p.w_in + ((int64_t)e * 2 * p.hidden + min(kSlice * slice + col, p.hidden - 1)) * p.channels;
   const T* const rows[2] = {gate, gate + (int64_t)p.hidden * p.channels};
   const int steps = (p.channels + 63) / 64;
@@ -390,9 +399,11 @@ __global__ __launch_bounds__(256) void k_expert_in(ExpertParams p, ExpertParts w
   strips.first = steps * wave / 4;
   strips.last = steps * (wave + 1) / 4;
   strips.length = p.channels;
-  const bool early = ahead && group == 0;
+  for (int begin = 0; begin < p.tokens; begin += 16 * NT) {
+  const bool early = ahead && begin == 0;
   if (early) strips.begin(rows);
-  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
+  __syncthreads();                                   // the list's and the parts' last readers are done
+  const int n = pairs_of(p, w.chosen, e, begin, 16 * NT, list, counts);
   if (n == 0) return;
   if (!early) strips.begin(rows);
   const T* vectors[NT];                              // (a place without a token has the first's, and is left out below)
@@ -415,6 +426,8 @@ __global__ __launch_bounds__(256) void k_expert_in(ExpertParams p, ExpertParts w
       y[r] = (partial[0][r][i][from][u & 3] + partial[1][r][i][from][u & 3]) + (partial[2][r][i][from][u & 3] + partial[3][r][i][from][u & 3]);
     store_hidden<T>(p, w, list[min(16 * i + at, n - 1)], slice, u, 16 * i + at < n, y[0], y[1]);
   }
+  if (n < 16 * NT) return;
+  }
 }
 
 // What comes out of an expert: 16 channels per workgroup, a quarter of the hidden values per wave.
@@ -425,17 +438,18 @@ __global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts 
   __shared__ int counts[4], powers[16 * NT];
   __shared__ f32x4 partial[4][NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, slices = slices_of(p);
-  const int blocks = (p.channels + 15) / 16, per_group = blocks * p.experts;
-  const int group = blockIdx.x / per_group, block = blockIdx.x % per_group % blocks, e = blockIdx.x % per_group / blocks;
+  const int blocks = (p.channels + 15) / 16, block = blockIdx.x % blocks, e = blockIdx.x / blocks;
   const T* const rows[1] = {(const T*)p.w_out + ((int64_t)e * p.channels + min(16 * block + col, p.channels - 1)) * p.hidden};
   const int steps = (p.hidden + 63) / 64;
   Strips<T, 1, NT> strips;
   strips.first = steps * wave / 4;
   strips.last = steps * (wave + 1) / 4;
   strips.length = p.hidden;
-  const bool early = ahead && group == 0;
+  for (int begin = 0; begin < p.tokens; begin += 16 * NT) {
+  const bool early = ahead && begin == 0;
   if (early) strips.begin(rows);
-  const int n = pairs_of(p, w.chosen, e, group * 16 * NT, 16 * NT, list, counts);
+  __syncthreads();                                   // the list's and the parts' last readers are done
+  const int n = pairs_of(p, w.chosen, e, begin, 16 * NT, list, counts);
   if (n == 0) return;
   if (!early) strips.begin(rows);
   const int u = threadIdx.x & 15, at = threadIdx.x >> 4, from = (u >> 2) * 16 + at;
@@ -443,9 +457,9 @@ __global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts 
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       if (16 * i + at >= n) break;
-      const int16_t* const power = w.power + (int64_t)list[16 * i + at] * slices;
+      const int16_t* const power = w.power + (int64_t)list[16 * i + at] * power_pitch(p);
       int most = kNoPower;
-      for (int s = u; s < slices; s += 16) most = max(most, (int)power[s]);
+      for (int s = 8 * u; s < slices; s += 128) most = max(most, most_of(power, s, slices));
 #pragma unroll
       for (int d = 1; d < 16; d *= 2) most = max(most, __shfl_xor(most, d));
       if (u == 0) powers[16 * i + at] = most;
@@ -460,7 +474,7 @@ __global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts 
     const int place = 16 * i + col < n ? 16 * i + col : 0;
     const int64_t pair = list[place];
     vectors[i] = (const T*)w.hidden + pair * p.hidden;
-    power[i] = w.power + pair * slices;
+    power[i] = w.power + pair * power_pitch(p);
     row_power[i] = kPowers ? powers[place] : 0;
   }
   f32x4 acc[1][NT] = {};
@@ -484,155 +498,180 @@ __global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts 
     if (kPowers && powers[16 * i + at] != kNoPower) y = ldexpf(y, powers[16 * i + at]);
     w.products[pair * p.channels + 16 * block + u] = w.weights[pair] * y;
   }
+  if (n < 16 * NT) return;
+  }
 }
 
-// ---- more tokens: tiles of 128 weight rows
+// ---- more tokens: tiles of 64 weight rows
 
-// Either product for many tokens of an expert: a workgroup has 128 hidden values (IN: 128 rows of each of the two weights) or channels
-// and up to 32 * NT of the expert's tokens, 32 rows per wave.  Weights go from memory into the registers that multiply them, as
-// no other wave needs them; the tokens' values, which all waves need, through LDS, 64 at a time.
-template <class T, bool IN, int NT>
-__global__ __launch_bounds__(256, 2) void k_expert_tiles(ExpertParams p, ExpertParts w, int groups) {
+// Either product for many tokens of an expert: a workgroup has 64 hidden values (IN: the rows of both weights) or channels and up to
+// 16 * NT of the expert's tokens, a wave 16 of the rows.  Weights go from memory into the registers that multiply them, as no
+// other wave needs them; the tokens' values, which all waves need, through LDS, 64 at a time.  Bound by the weights' way from
+// memory: AHEAD steps of loads are on their way.
+// (More tokens than that are taken in turn.)
+// ahead: the first weights are asked for before it is known whether some token needs them.
+template <class T, bool IN, int NT, int AHEAD>
+__global__ __launch_bounds__(256, 2) void k_expert_tiles(ExpertParams p, ExpertParts w, int ahead) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
-  constexpr int RT = IN ? 2 : 1, kTile = 32 * NT * 128;
+  constexpr int RT = IN ? 2 : 1, kVectors = 16 * NT, kTile = kVectors * 128, NB = (kVectors + 31) / 32;
   constexpr bool kPowers = __is_same(T, f16);
   __shared__ __align__(16) char lds[2 * kTile];
-  __shared__ int powers[32 * NT], counts[4];
-  __shared__ int32_t list[32 * NT];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int rows = IN ? p.hidden : p.channels, length = IN ? p.channels : p.hidden, blocks = (rows + 127) / 128, slices = slices_of(p);
-  // The groups of the tokens behind the first, most of them empty, come last: dealt out among the others, those would leave CUs without work.
-  const int per_group = blocks * p.experts, group = blockIdx.x / per_group;
-  const int id = blockIdx.x % per_group, block = id % blocks, e = id / blocks;
-  const int n = pairs_of(p, w.chosen, e, group * 32 * NT, 32 * NT, list, counts);
-  if (n == 0) return;
+  __shared__ int powers[kVectors], counts[4];
+  __shared__ int32_t list[kVectors];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+  const int rows = IN ? p.hidden : p.channels, length = IN ? p.channels : p.hidden, blocks = (rows + 63) / 64, slices = slices_of(p);
+  const int steps = (length + 63) / 64;
+  const int block = blockIdx.x % blocks, e = blockIdx.x / blocks;
 
-  // staging: this thread's 16 bytes of vectors r0 + 32 i
-  const int r0 = threadIdx.x >> 3, ch = threadIdx.x & 7;
-  const T* from[NT];
-  const int16_t* power[NT];
-  int row_power[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int64_t pair = list[min(r0 + 32 * i, n - 1)];
-    from[i] = IN ? (const T*)p.x + pair / p.top * p.x_stride : (const T*)w.hidden + pair * p.hidden;
-    power[i] = w.power + pair * slices;
-    row_power[i] = 0;
-    if (!IN && kPowers) {                            // the eight threads of a vector look for its largest power
-      int most = kNoPower;
-      for (int s = ch; s < slices; s += 8) most = max(most, (int)power[i][s]);
-#pragma unroll
-      for (int d = 1; d < 8; d *= 2) most = max(most, __shfl_xor(most, d));
-      row_power[i] = most;
-      if (ch == 0) powers[r0 + 32 * i] = most;
-    }
-  }
-  const int row = 128 * block + 32 * wave;
+  const int row = 64 * block + 16 * wave;
   const int64_t first_row = (int64_t)e * (IN ? 2 * p.hidden : p.channels) + min(row + col, rows - 1);
   const T* weights[RT];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) weights[r] = (const T*)(IN ? p.w_in : p.w_out) + (first_row + (int64_t)r * p.hidden) * length + 8 * half;
-
+  for (int r = 0; r < RT; ++r) weights[r] = (const T*)(IN ? p.w_in : p.w_out) + (first_row + (int64_t)r * p.hidden) * length;
   struct Step {
-    x8 a[RT][4];
-    x8 b[NT];
-    int16_t power[NT];
+    x8 a[RT][2];
+    x8 b[NB];
+    int16_t power[NB];
   };
-  auto load = [&](int step, Step& s) {
-    const int d0 = min(64 * step + 8 * ch, length - 8);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      s.b[i] = __builtin_bit_cast(x8, load16(from[i] + d0));
-      if (!IN && kPowers) s.power[i] = power[i][d0 / kSlice];
-    }
+  auto load_weights = [&](int step, Step& s) {       // a lane has 16 values side by side: four lanes read 128 bytes of a row
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) s.a[r][k] = __builtin_bit_cast(x8, load16(weights[r] + min(64 * step + 16 * k, length - 8 - 8 * half)));
+      for (int k = 0; k < 2; ++k) s.a[r][k] = __builtin_bit_cast(x8, load16(weights[r] + min(64 * step + 16 * g + 8 * k, length - 8)));
   };
-  int koff[4];
+  for (int begin = 0; begin < p.tokens; begin += kVectors) {
+  Step ring[AHEAD + 1];
+  const bool early = ahead && begin == 0;
+  if (early)
 #pragma unroll
-  for (int k = 0; k < 4; ++k) koff[k] = slot<8>(col, 2 * k + half);
-  f32x16 acc[RT][NT] = {};
-  const int steps = (length + 63) / 64;
-  auto multiply = [&](int step, Step& s, Step& next) {
+    for (int i = 0; i < AHEAD; ++i) load_weights(min(i, steps - 1), ring[i]);
+  __syncthreads();                                   // the list's and LDS's last readers are done
+  const int n = pairs_of(p, w.chosen, e, begin, kVectors, list, counts);
+  if (n == 0) return;
+  if (!early)
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load_weights(min(i, steps - 1), ring[i]);
+
+  // staging: this thread's 16 bytes of vectors r0 + 32 i
+  const int r0 = threadIdx.x >> 3, ch = threadIdx.x & 7;
+  const T* from[NB];
+  const int16_t* power[NB];
+  int row_power[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int64_t pair = list[min(r0 + 32 * i, n - 1)];
+    from[i] = IN ? (const T*)p.x + pair / p.top * p.x_stride : (const T*)w.hidden + pair * p.hidden;
+    power[i] = w.power + pair * power_pitch(p);
+    row_power[i] = 0;
+    if (!IN && kPowers) {                            // the eight threads of a vector look for its largest power
+      int most = kNoPower;
+      for (int s = 8 * ch; s < slices; s += 64) most = max(most, most_of(power[i], s, slices));
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) most = max(most, __shfl_xor(most, d));
+      row_power[i] = most;
+      if (ch == 0 && r0 + 32 * i < kVectors) powers[r0 + 32 * i] = most;
+    }
+  }
+  auto load_vectors = [&](int step, Step& s) {
+    const int d0 = min(64 * step + 8 * ch, length - 8);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      s.b[i] = __builtin_bit_cast(x8, load16(from[i] + d0));
+      if (!IN && kPowers) s.power[i] = power[i][d0 / kSlice];
+    }
+  };
+  int boff[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) boff[k] = slot<8>(col, 2 * g + k);
+  f32x4 acc[RT][NT] = {};
+  const int tiles = (n + 15) / 16;
+  auto multiply = [&](int step, Step& s) {
     char* const here = lds + (step & 1) * kTile;
     const bool whole = 64 * step + 64 <= length;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
+    for (int i = 0; i < NB; ++i) {
       if (!whole && 64 * step + 8 * ch >= length) s.b[i] = x8{};
       if (!IN && kPowers) s.b[i] *= (T)ldexpf(1.0f, max(s.power[i] - row_power[i], -40));
-      *(x8*)(here + slot<8>(r0 + 32 * i, ch)) = s.b[i];
+      if (kVectors % 32 == 0 || r0 + 32 * i < kVectors) *(x8*)(here + slot<8>(r0 + 32 * i, ch)) = s.b[i];
     }
-    if (step + 1 < steps) load(step + 1, next);
+    if (!whole)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (64 * step + 16 * g + 8 * k >= length)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) s.a[r][k] = x8{};
     __syncthreads();
+    // (Five tiles at a time, or all there are: a branch around each of them would have every one wait for its own reads.)
+    constexpr int kRun = NT % 5 ? NT : 5;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (!whole && 64 * step + 16 * k + 8 * half >= length)
+    for (int i0 = 0; i0 < NT; i0 += kRun) {
+      if (i0 >= tiles) break;
 #pragma unroll
-        for (int r = 0; r < RT; ++r) s.a[r][k] = x8{};
+      for (int i = i0; i < i0 + kRun; ++i)
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        if (32 * i >= n) break;
-        const x8 b = *(const x8*)(here + koff[k] + i * 32 * 128);
+        for (int k = 0; k < 2; ++k) {
+          const x8 b = *(const x8*)(here + boff[k] + i * 16 * 128);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) acc[r][i] = mfma32(s.a[r][k], b, acc[r][i]);
-      }
+          for (int r = 0; r < RT; ++r) acc[r][i] = mfma16(s.a[r][k], b, acc[r][i]);
+        }
     }
   };
-  Step even, odd;
-  load(0, even);
-  for (int step = 0; step < steps; step += 2) {
-    multiply(step, even, odd);
-    if (step + 1 < steps) multiply(step + 1, odd, even);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) load_vectors(min(i, steps - 1), ring[i]);
+  int step = 0;
+  // (Loads that a branch may leave out would be waited for where it ends: only the last steps have branches.)
+  for (; step + 2 * AHEAD < steps; step += AHEAD + 1)
+#pragma unroll
+    for (int i = 0; i <= AHEAD; ++i) {
+      Step& next = ring[(i + AHEAD) % (AHEAD + 1)];
+      load_weights(step + i + AHEAD, next);
+      load_vectors(step + i + AHEAD, next);
+      multiply(step + i, ring[i]);
+    }
+#pragma unroll
+  for (int i = 0; i < 2 * AHEAD; ++i) {
+    if (step + i >= steps) break;
+    if (step + i + AHEAD < steps) {
+      Step& next = ring[(i + AHEAD) % (AHEAD + 1)];
+      load_weights(step + i + AHEAD, next);
+      load_vectors(step + i + AHEAD, next);
+    }
+    multiply(step + i, ring[i % (AHEAD + 1)]);
   }
 
-  // lane l has vector l % 32 and rows 8 * (i / 4) + 4 * half + i % 4
+  // lane l has vector l % 16 and rows 4 * (l / 16) + i
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
-    if (32 * i >= n) break;
-    const bool live = 32 * i + col < n;
-    const int64_t pair = list[min(32 * i + col, n - 1)];
+    if (i >= tiles) continue;
+    const int place = 16 * i + col;
+    const bool live = place < n && row + 4 * g < rows;
+    const int64_t pair = list[min(place, n - 1)];
     if (IN) {
-      f32x16 h;
+      f32x4 h;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) h[j] = acc[0][i][j] / (1.0f + expf(-acc[0][i][j])) * acc[RT - 1][i][j];
+      for (int j = 0; j < 4; ++j) h[j] = acc[0][i][j] / (1.0f + expf(-acc[0][i][j])) * acc[RT - 1][i][j];
+      if (kPowers) {
+        float most = 0.0f;
+        if (row + 4 * g < rows) most = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
+        most = column_max(most);
+        const int own = most > 0.0f && most < INFINITY ? ilogbf(most) - 14 : most > 0.0f ? 0 : kNoPower;
+        if (live && g == 0) w.power[pair * power_pitch(p) + row / kSlice] = own;
+        if (own != kNoPower)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        int own = 0;
-        if (kPowers) {
-          float most = 0.0f, lower, upper;
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (row + 16 * s + 8 * (j / 4) + 4 * half < rows) most = fmaxf(most, fabsf(h[8 * s + j]));
-          both_halves(most, lower, upper);
-          most = fmaxf(lower, upper);
-          own = most > 0.0f && most < INFINITY ? ilogbf(most) - 14 : most > 0.0f ? 0 : kNoPower;
-          if (live && half == 0 && row + 16 * s < rows) w.power[pair * slices + row / kSlice + s] = own;
-          if (own == kNoPower) own = 0;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; j += 4) {
-          const int unit = row + 16 * s + 2 * j + 4 * half;
-          x4 y;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) y[d] = (T)(kPowers ? ldexpf(h[8 * s + j + d], -own) : h[8 * s + j + d]);
-          if (live && unit < rows) *(x4*)((T*)w.hidden + pair * p.hidden + unit) = y;
-        }
+          for (int j = 0; j < 4; ++j) h[j] = ldexpf(h[j], -own);
       }
+      if (live) *(x4*)((T*)w.hidden + pair * p.hidden + row + 4 * g) = round4<T>(h);
     } else {
-      float f = w.weights[pair];
-      const int own = kPowers ? powers[min(32 * i + col, n - 1)] : 0;
+      const float f = w.weights[pair];
+      const int own = kPowers ? powers[min(place, n - 1)] : 0;
+      f32x4 y;
 #pragma unroll
-      for (int j = 0; j < 16; j += 4) {
-        const int channel = row + 2 * j + 4 * half;
-        f32x4 y;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) y[d] = f * (kPowers && own != kNoPower ? ldexpf(acc[0][i][j + d], own) : acc[0][i][j + d]);
-        if (live && channel < rows) *(f32x4*)(w.products + pair * p.channels + channel) = y;
-      }
+      for (int j = 0; j < 4; ++j) y[j] = f * (kPowers && own != kNoPower ? ldexpf(acc[0][i][j], own) : acc[0][i][j]);
+      if (live) *(f32x4*)(w.products + pair * p.channels + row + 4 * g) = y;
     }
+  }
+  if (n < kVectors) return;
   }
 }
 
@@ -656,32 +695,28 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertParams p, ExpertParts 
 
 template <class T, int NT>
 hipError_t launch_few(const ExpertParams& p, bool frame, void** args, hipStream_t stream) {
-  int ahead = (int64_t)p.tokens * p.top >= p.experts;
-  void* all[] = {args[0], args[1], &ahead};
-  const int64_t groups = (p.tokens + 16 * NT - 1) / (16 * NT);
-  const hipError_t e = frame ? launch_kernel((const void*)k_expert_frame<T>, (int64_t)p.experts * ((slices_of(p) + 3) / 4), 1024, all, stream)
-                             : launch_kernel((const void*)k_expert_in<T, NT>, p.experts * slices_of(p) * groups, 256, all, stream);
-  return e != hipSuccess ? e : launch_kernel((const void*)k_expert_out<T, NT>, p.experts * groups * ((p.channels + 15) / 16), 256, all, stream);
+  const hipError_t e = frame ? launch_kernel((const void*)k_expert_frame<T>, (int64_t)p.experts * ((slices_of(p) + 3) / 4), 1024, args, stream)
+                             : launch_kernel((const void*)k_expert_in<T, NT>, (int64_t)p.experts * slices_of(p), 256, args, stream);
+  return e != hipSuccess ? e : launch_kernel((const void*)k_expert_out<T, NT>, (int64_t)p.experts * ((p.channels + 15) / 16), 256, args, stream);
 }
-template <class T, int NT>
+template <class T, int NT, int AHEAD_IN, int AHEAD_OUT>
 hipError_t launch_tiles(const ExpertParams& p, void** args, hipStream_t stream) {
-  int groups = (p.tokens + 32 * NT - 1) / (32 * NT);
-  void* all[] = {args[0], args[1], &groups};
-  const hipError_t e = launch_kernel((const void*)k_expert_tiles<T, true, NT>, (int64_t)p.experts * ((p.hidden + 127) / 128) * groups, 256, all, stream);
-  return e != hipSuccess ? e : launch_kernel((const void*)k_expert_tiles<T, false, NT>, (int64_t)p.experts * ((p.channels + 127) / 128) * groups, 256, all, stream);
+  const hipError_t e = launch_kernel((const void*)k_expert_tiles<T, true, NT, AHEAD_IN>, (int64_t)p.experts * ((p.hidden + 63) / 64), 256, args, stream);
+  return e != hipSuccess ? e : launch_kernel((const void*)k_expert_tiles<T, false, NT, AHEAD_OUT>, (int64_t)p.experts * ((p.channels + 63) / 64), 256, args, stream);
 }
 template <class T>
 hipError_t launch_of(const ExpertParams& p, hipStream_t stream) {
   ExpertParams params = p;
   ExpertParts parts = parts_of(p);
-  void* args[] = {&params, &parts};
+  int ahead = (int64_t)p.tokens * p.top >= p.experts;
+  void* args[] = {&params, &parts, &ahead};
   const bool frame = p.tokens <= 16 && p.experts <= kFusedExperts && (p.experts + 15) / 16 * p.channels <= 2048;
   hipError_t e = hipSuccess;
   if (!frame) e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 256, args, stream);
   if (e != hipSuccess) return e;
   const int64_t each = (int64_t)p.tokens * p.top / p.experts;          // tokens of an expert, on average
   if (p.tokens <= kFewTokens) e = p.tokens <= 16 ? launch_few<T, 1>(p, frame, args, stream) : launch_few<T, 2>(p, false, args, stream);
-  else e = each <= 24 ? launch_tiles<T, 1>(p, args, stream) : each <= 48 ? launch_tiles<T, 2>(p, args, stream) : launch_tiles<T, 4>(p, args, stream);
+  else e = each <= 20 ? launch_tiles<T, 2, 3, 4>(p, args, stream) : each <= 48 ? launch_tiles<T, 4, 3, 3>(p, args, stream) : launch_tiles<T, 10, 2, 2>(p, args, stream);
   return e != hipSuccess ? e : launch_kernel((const void*)k_expert_sum<T>, ((int64_t)p.tokens * (p.channels / 8) + 255) / 256, 256, args, stream);
 }
 }  // namespace
