@@ -15,7 +15,7 @@ __device__ __forceinline__ const float* gate_at(const hs_gates& g, int64_t batch
 // one sequence's and head's state in registers: 16 lanes side by side have 4 values of 16 bytes each, and thread group g of
 // 16 has ROWS rows from ROWS * g on.
 template <class T, int ROWS>
-__global__ __launch_bounds__(256) void k_delta_steps(DeltaParams p) {
+__global__ __launch_bounds__(256, ROWS > 4 ? 4 : 6) void k_delta_steps(DeltaParams p) {
   typedef typename Vec<T>::x4 x4;
   typedef T xr __attribute__((ext_vector_type(ROWS)));
   __shared__ f32x4 partial[2][2][4][16];
