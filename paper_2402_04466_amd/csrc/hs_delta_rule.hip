@@ -107,8 +107,8 @@ __global__ __launch_bounds__(256, ROWS > 4 ? 4 : 6) void k_delta_steps(DeltaPara
 //   (1 + A) U = diag(beta) (V - diag(2^L) K S),     A_ij = beta_i Gamma_ij k_i.k_j for j < i,
 // and  out = scale (diag(2^L) Q S + P U),           P_ij = Gamma_ij q_i.k_j for j <= i,
 //      S'  = 2^L_end S + K^T diag(2^(L_end - L)) U.
-// M = (1 + A)^-1 diag(beta) and P do not depend on the state: two waves form them for the chunk to come, a third lays its
-// values and gates out, while the state's waves work on this one.  A state wave has all rows of 16 of the state's columns in
+// M = (1 + A)^-1 diag(beta) and P do not depend on the state: while the state's waves work on a chunk, one wave forms P of the chunk
+// to come, one M from the A that another has left a chunk before, and one lays values and gates out.  A state wave has all rows of 16 of the state's columns in
 // registers, and needs nothing of the others: in the layout in which products leave their results (rows 4g .. 4g + 3
 // of a column in lane group g) pairs of 16 rows are operands of the next product, once its other operand is read in the order of rows
 // 4g .. 4g + 3, 16 + 4g .. 16 + 4g + 3.
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256, ROWS > 4 ? 4 : 6) void k_delta_steps(DeltaPara
 // Precision.  What enters the state is exact to 24 bits: the state and U go through the matrix pipe as three bf16 parts
 // (8 bits each, split by truncation, which is exact and cannot overflow), fp16 keys and queries as two, M in fp32.
 // Outputs, which are rounded to 16 bits, take two parts of each: 16 bits.
-constexpr int kChunk = 32, kStateWaves = 4, kOtherWaves = 3;
+constexpr int kChunk = 32, kStateWaves = 4, kOtherWaves = 4;
 constexpr int kMPitch = 36;                          // floats per row of M: 16 rows' same 16 bytes lie in different banks
 constexpr int kPPitch = 80;                          // bytes per row of P: as well
 
@@ -163,10 +163,10 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
   constexpr int NP = __is_same(T, f16) ? 2 : 1;      // bf16 parts of a key or query
   constexpr int CH = DK > 64 ? 16 : 8, KS = DK / 32, ST = DK / 16;
   constexpr int kTile = kChunk * CH * 16, kValues = kChunk * 8 * 16;
-  constexpr int kK = 0, kQ = NP * kTile, kV = 2 * NP * kTile, kM = kV + kValues, kP = kM + kChunk * kMPitch * 4;
-  constexpr int kBuffer = kP + 2 * kChunk * kPPitch;
+  constexpr int kK = 0, kQ = NP * kTile, kV = 2 * NP * kTile, kP = kV + kValues, kBuffer = kP + 2 * kChunk * kPPitch;
   __shared__ __align__(16) char lds[2 * kBuffer];
-  __shared__ ChunkGates gates[3];
+  __shared__ __align__(16) float ms[3][kChunk * kMPitch];      // A, then M
+  __shared__ ChunkGates gates[4];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = lane & 15, g = lane >> 4;
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
   const int block = id % grid.blocks, bh = id / grid.blocks, h = bh % p.heads, hk = h / p.group, b = bh / p.heads;
   const int n = length_of(p.lengths, b, p.tokens), chunks = (n + kChunk - 1) / kChunk;
   const int column0 = 16 * grid.waves * block;
-  // roles: the state's waves first, then M, P, and values and gates
+  // roles: the state's waves first, then A, M, P, and values and gates
   const int role = wave < grid.waves ? 0 : 1 + wave - grid.waves;
 
   if (role == 0) {
@@ -203,9 +203,10 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
 
     __syncthreads();
     __syncthreads();
+    __syncthreads();
     for (int c = 0; c < chunks; ++c) {
       const char* const here = lds + (c & 1) * kBuffer;
-      const ChunkGates& gate = gates[c % 3];
+      const ChunkGates& gate = gates[c % 4];
       f32x4 ks[2] = {}, qs[2] = {};                  // K S: tokens x columns; (Q S)^T: columns x tokens
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
@@ -214,25 +215,34 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         for (int i = 0; i < 4; ++i) x[i] = s[2 * k][i], x[4 + i] = s[2 * k + 1][i];
         b8 part[3];
         split8<3>(x, part);
+        b8 kk[2][NP], qq[2][NP];
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          b8 kk[NP], qq[NP];
+        for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int e = 0; e < NP; ++e) {
             const char* const at_k = here + kK + e * kTile + tt * kNext;
             const char* const at_q = here + kQ + e * kTile + tt * kNext;
-            kk[e] = join8<bf16>(*(const s16x4*)(at_k + koff[k][0]), *(const s16x4*)(at_k + koff[k][1]));
-            qq[e] = join8<bf16>(*(const s16x4*)(at_q + koff[k][0]), *(const s16x4*)(at_q + koff[k][1]));
+            kk[tt][e] = join8<bf16>(*(const s16x4*)(at_k + koff[k][0]), *(const s16x4*)(at_k + koff[k][1]));
+            qq[tt][e] = join8<bf16>(*(const s16x4*)(at_q + koff[k][0]), *(const s16x4*)(at_q + koff[k][1]));
           }
-          if (NP == 2) {
-            ks[tt] = mfma16(kk[NP - 1], part[1], ks[tt]);
-            ks[tt] = mfma16(kk[NP - 1], part[0], ks[tt]);
-            qs[tt] = mfma16(part[0], qq[NP - 1], qs[tt]);
+        // (products that add to the same sums are kept apart: one would wait for the other)
+        if (NP == 2) {
+#pragma unroll
+          for (int e = 1; e >= 0; --e) {
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) ks[tt] = mfma16(kk[tt][NP - 1], part[e], ks[tt]);
+            if (e == 0)
+#pragma unroll
+              for (int tt = 0; tt < 2; ++tt) qs[tt] = mfma16(part[0], qq[tt][NP - 1], qs[tt]);
           }
+        }
 #pragma unroll
-          for (int e = 2; e >= 0; --e) ks[tt] = mfma16(kk[0], part[e], ks[tt]);
+        for (int e = 2; e >= 0; --e) {
 #pragma unroll
-          for (int e = 1; e >= 0; --e) qs[tt] = mfma16(part[e], qq[0], qs[tt]);
+          for (int tt = 0; tt < 2; ++tt) ks[tt] = mfma16(kk[tt][0], part[e], ks[tt]);
+          if (e < 2)
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) qs[tt] = mfma16(part[e], qq[tt][0], qs[tt]);
         }
       }
       f32x4 x[2], u[2] = {};
@@ -244,7 +254,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[tt][i] = (float)v[i] - since[i] * ks[tt][i];
       }
-      const float* const m = (const float*)(here + kM) + row * kMPitch + 4 * g;
+      const float* const m = ms[c % 3] + row * kMPitch + 4 * g;
       const f32x4 m00 = *(const f32x4*)m, m10 = *(const f32x4*)(m + 16 * kMPitch), m11 = *(const f32x4*)(m + 16 * kMPitch + 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -253,6 +263,55 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) u[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m11[i], x[1][i], u[1], 0, 0, 0);
+
+      // Outputs and the state's new part are formed in one run with the above, so that their products fill the others' waits; what is
+      // not finite is found out before they are kept.
+      float y[8];
+      b8 part[3];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = u[0][i], y[4 + i] = u[1][i];
+      split8<2>(y, part);
+      f32x4 o[2] = {}, fresh[ST] = {};
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const char* const at_p = here + kP + (16 * tt + row) * kPPitch + 16 * g;
+        const b8 hi = __builtin_bit_cast(b8, *(const s16x8*)at_p), lo = __builtin_bit_cast(b8, *(const s16x8*)(at_p + kChunk * kPPitch));
+        o[tt] = mfma16(part[1], hi, o[tt]);
+        o[tt] = mfma16(part[0], lo, o[tt]);
+        o[tt] = mfma16(part[0], hi, o[tt]);
+        const float since = gate.since[16 * tt + row];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[tt][i] = p.scale * fmaf(since, qs[tt][i], o[tt][i]);
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const f32x4 left = *(const f32x4*)(gate.left + 16 * tt + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[4 * tt + i] *= left[i];
+      }
+      split8<3>(y, part);
+      const float whole = gate.since[kChunk - 1];
+#pragma unroll
+      for (int t0 = 0; t0 < ST; t0 += 2) {
+        b8 kk[2][NP];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < NP; ++e) {
+            const char* const at_k = here + kK + e * kTile + toff[t0 + t];
+            kk[t][e] = join8<bf16>(read_transposed(at_k), read_transposed(at_k + kNext));
+          }
+        if (NP == 2) {
+#pragma unroll
+          for (int e = 1; e >= 0; --e)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) fresh[t0 + t] = mfma16(kk[t][NP - 1], part[e], fresh[t0 + t]);
+        }
+#pragma unroll
+        for (int e = 2; e >= 0; --e)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) fresh[t0 + t] = mfma16(kk[t][0], part[e], fresh[t0 + t]);
+      }
 
       // Something is not finite: the recurrence says where it goes, token by token.
       float most = 0.0f;
@@ -298,51 +357,15 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         continue;
       }
 
-      float y[8];
-      b8 part[3];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = u[0][i], y[4 + i] = u[1][i];
-      split8<2>(y, part);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        f32x4 o = {0, 0, 0, 0};
-        const char* const at_p = here + kP + (16 * tt + row) * kPPitch + 16 * g;
-        const b8 hi = __builtin_bit_cast(b8, *(const s16x8*)at_p), lo = __builtin_bit_cast(b8, *(const s16x8*)(at_p + kChunk * kPPitch));
-        o = mfma16(part[1], hi, o);
-        o = mfma16(part[0], lo, o);
-        o = mfma16(part[0], hi, o);
         const int token = c * kChunk + 16 * tt + row;
-        const float since = gate.since[16 * tt + row];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = p.scale * fmaf(since, qs[tt][i], o[i]);
-        if (token < n && stored) *(x4*)(out + (int64_t)token * p.out.token + 4 * g) = round4<T>(o);
+        if (token < n && stored) *(x4*)(out + (int64_t)token * p.out.token + 4 * g) = round4<T>(o[tt]);
       }
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const f32x4 left = *(const f32x4*)(gate.left + 16 * tt + 4 * g);
+      for (int t = 0; t < ST; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[4 * tt + i] *= left[i];
-      }
-      split8<3>(y, part);
-      const float whole = gate.since[kChunk - 1];
-#pragma unroll
-      for (int t = 0; t < ST; ++t) {
-        f32x4 fresh = {0, 0, 0, 0};
-        b8 kk[NP];
-#pragma unroll
-        for (int e = 0; e < NP; ++e) {
-          const char* const at_k = here + kK + e * kTile + toff[t];
-          kk[e] = join8<bf16>(read_transposed(at_k), read_transposed(at_k + kNext));
-        }
-        if (NP == 2) {
-          fresh = mfma16(kk[NP - 1], part[1], fresh);
-          fresh = mfma16(kk[NP - 1], part[0], fresh);
-        }
-#pragma unroll
-        for (int e = 2; e >= 0; --e) fresh = mfma16(kk[0], part[e], fresh);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][i] = fmaf(whole, s[t][i], fresh[i]);
-      }
+        for (int i = 0; i < 4; ++i) s[t][i] = fmaf(whole, s[t][i], fresh[t][i]);
       __syncthreads();
     }
 #pragma unroll
@@ -357,7 +380,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
     return;
   }
 
-  if (role == 3) {   // values of chunk c + 1, gates of chunk c + 2
+  if (role == 4) {   // values of chunk c + 1, gates of chunk c + 3
     const T* const v = at<T>(p.v, b, 0, h) + column0;
     const float* const log_decay = gate_at(p.log_decay, b, h);
     const float* const beta = gate_at(p.beta, b, h);
@@ -382,9 +405,9 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
       }
     };
     fetch_gates(0);
-    for (int c = -2; c < chunks; ++c) {
-      if (c + 2 < chunks) {
-        ChunkGates& gate = gates[(c + 2) % 3];
+    for (int c = -3; c < chunks; ++c) {
+      if (c + 3 < chunks) {
+        ChunkGates& gate = gates[(c + 3) % 4];
         // A decay of zero is 2^-10000 here: nothing of it is left in 32 bits, and no infinity enters the sums.
         double upto = (double)l * 1.4426950408889634074;
         if (upto < -1e4) upto = -1e4;
@@ -398,25 +421,25 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         if (lane < 32) {
           gate.upto_hi[lane] = hi;
           gate.upto_lo[lane] = (float)(upto - (double)hi);
-          gate.since[lane] = exp2f(hi);
-          gate.left[lane] = exp2f((float)(end - upto));
+          gate.since[lane] = __builtin_amdgcn_exp2f(hi);
+          gate.left[lane] = __builtin_amdgcn_exp2f((float)(end - upto));
           gate.beta[lane] = be;
           gate.decay[lane] = expf(l);
         }
-        fetch_gates(c + 3);
+        fetch_gates(c + 4);
       }
       if (c + 1 >= 0 && c + 1 < chunks) {
         char* const next = lds + ((c + 1) & 1) * kBuffer + kV;
 #pragma unroll
         for (int e = 0; e < 4; ++e) *(s16x8*)(next + slot<8>(e * 8 + (lane >> 3), lane & 7)) = reg[e];
       }
-      if (c + 2 < chunks) fetch_values(c + 2);
+      if (c + 2 >= 0 && c + 2 < chunks) fetch_values(c + 2);
       __syncthreads();
     }
     return;
   }
 
-  // M (role 1) and P (role 2) of chunk c + 1, and its keys, or queries, in LDS
+  // A of chunk c + 2 (role 1); M of chunk c + 1, and its keys in LDS (role 2); P of chunk c + 1, and its queries in LDS (role 3)
   const T* const key = at<T>(p.k, b, 0, hk);
   const T* const query = at<T>(p.q, b, 0, hk);
   x8 kk[2][KS], qq[2][KS];
@@ -457,18 +480,16 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
     const f32x4 hj = *(const f32x4*)(gate.upto_hi + 16 * jt + 4 * g), lj = *(const f32x4*)(gate.upto_lo + 16 * jt + 4 * g);
     f32x4 y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = exp2f((hi - hj[i]) + (lo - lj[i]));
+    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_exp2f((hi - hj[i]) + (lo - lj[i]));
     return y;
   };
   if (role == 1) {
     if (chunks > 0) fetch_rows(key, p.k.token, 0, kk);
     __syncthreads();
-    for (int c = -1; c < chunks; ++c) {
-      if (c + 1 < chunks) {
-        char* const next = lds + ((c + 1) & 1) * kBuffer;
-        const ChunkGates& gate = gates[(c + 1) % 3];
-        lay_out(kk, next + kK);
-        float* const m = (float*)(next + kM);
+    for (int c = -2; c < chunks; ++c) {
+      if (c + 2 < chunks) {
+        const ChunkGates& gate = gates[(c + 2) % 4];
+        float* const m = ms[(c + 2) % 3];
 #pragma unroll
         for (int tile = 0; tile < 3; ++tile) {       // (it, jt) = (0, 0), (1, 0), (1, 1)
           const int it = tile > 0, jt = tile > 1;
@@ -481,8 +502,20 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
           for (int i = 0; i < 4; ++i) d[i] = it == jt && 4 * g + i >= row ? 0.0f : beta * w[i] * d[i];
           *(f32x4*)(m + (16 * it + row) * kMPitch + 16 * jt + 4 * g) = d;
         }
-        if (c + 2 < chunks) fetch_rows(key, p.k.token, c + 2, kk);
-        wave_order();
+        if (c + 3 < chunks) fetch_rows(key, p.k.token, c + 3, kk);
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  if (role == 2) {
+    if (chunks > 0) fetch_rows(key, p.k.token, 0, kk);
+    __syncthreads();
+    __syncthreads();
+    for (int c = -1; c < chunks; ++c) {
+      if (c + 1 < chunks) {
+        const ChunkGates& gate = gates[(c + 1) % 4];
+        float* const m = ms[(c + 1) % 3];
         // the inverses of the diagonal blocks, a column per lane: lanes 0 .. 15 of the first, 16 .. 31 of the second
         float* const diagonal = m + (lane >> 4 & 1) * (16 * kMPitch + 16);
         const float beta = gate.beta[lane & 31];
@@ -509,6 +542,8 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         f32x4 w = {0, 0, 0, 0}, y = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) w = __builtin_amdgcn_mfma_f32_16x16x4f32(a21[i], m[(4 * g + i) * kMPitch + row], w, 0, 0, 0);
+        lay_out(kk, lds + ((c + 1) & 1) * kBuffer + kK);
+        if (c + 2 < chunks) fetch_rows(key, p.k.token, c + 2, kk);
 #pragma unroll
         for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(t22[i], w[i], y, 0, 0, 0);
         wave_order();
@@ -527,10 +562,11 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
     fetch_rows(query, p.q.token, 0, qq);
   }
   __syncthreads();
+  __syncthreads();
   for (int c = -1; c < chunks; ++c) {
     if (c + 1 < chunks) {
       char* const next = lds + ((c + 1) & 1) * kBuffer;
-      const ChunkGates& gate = gates[(c + 1) % 3];
+      const ChunkGates& gate = gates[(c + 1) % 4];
       lay_out(qq, next + kQ);
 #pragma unroll
       for (int tile = 0; tile < 4; ++tile) {         // (it, jt) = (0, 0), (0, 1): nothing, (1, 0), (1, 1)
