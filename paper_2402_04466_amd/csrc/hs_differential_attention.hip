@@ -12,11 +12,10 @@ namespace hs {
 // share keys), S^T = K Q^T leaves each row's scores in one lane pair, and O^T += V^T P^T takes them, rounded to 16 bits
 // once, from the lanes that have them.
 //
-// Many rows (MAPS = 2): QW waves have other rows and share the tiles; a wave forms both maps of its rows, so that each value
+// Many rows (k_differential): eight waves have other rows and share the tiles; a wave forms both maps of its rows, so that each value
 // that it reads from LDS is used twice: with a map per wave LDS would be busy as long as the matrix pipe.
-// Few rows (MAPS = 1): the waves of a workgroup have the same rows; four take the keys in turn for the first map, four for
-// the second (half the registers, and twice the loads in flight), and are joined in LDS.  Where that leaves the device
-// idle the keys are cut further, over `splits` workgroups, which k_differential_join puts together.
+// Few rows (k_differential_few): the waves of a workgroup have the same rows and take the keys in turn.
+// Where either leaves the device idle the keys are cut further, over `splits` workgroups, which k_differential_join puts together.
 struct DifferentialGrid {
   int row_tiles, splits;
 };
@@ -42,24 +41,18 @@ __device__ __forceinline__ V difference(V a, float fa, V b, float fb) {
   return a * fa - b * fb;
 }
 
-template <class T, int DP, int VP, int MAPS, int QW, int KW, int BN>
-__global__ __launch_bounds__(64 * QW * KW * (3 - MAPS), 2) void k_differential(DifferentialParams p, DifferentialGrid grid) {
+template <class T, int DP, int VP>
+__global__ __launch_bounds__(512, 2) void k_differential(DifferentialParams p, DifferentialGrid grid) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
-  constexpr int WAVES = QW * KW * (3 - MAPS);
+  constexpr int MAPS = 2, QW = 8, BN = 64;
   constexpr int CK = DP > 64 ? 16 : 8, CV = VP > 64 ? 16 : 8, KS = DP / 16, DT = VP / 32, NB = BN / 32;   // CK, CV: 16-byte pieces per row in LDS
   constexpr int NT = 64 * QW;                       // threads that fill a tile together
   constexpr int NK = BN * CK / NT, NV = BN * CV / NT;   // 16-byte loads per thread for one map's keys, and for values
   constexpr int kKeys = BN * CK * 16, kTile = MAPS * kKeys + BN * CV * 16;   // bytes
-  constexpr int kBuffers = QW > 1 ? 2 : 1;          // a wave alone needs no second buffer: its accesses are in order
-  constexpr int PT = VP + 4;                        // floats per row of a wave's part: reads and writes spread over the banks
-  constexpr int kTiles = WAVES / QW * kBuffers * kTile, kParts = MAPS == 1 ? WAVES * 32 * (PT + 2) * 4 : 0;
-  constexpr int kLds = kTiles > kParts ? kTiles : kParts;
-  __shared__ __align__(16) char lds[kLds];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int qw = MAPS == 2 ? wave : 0, kw = MAPS == 2 ? 0 : wave >> 1, map = MAPS == 2 ? 0 : wave & 1;
+  __shared__ __align__(16) char lds[2 * kTile];
+  const int lane = threadIdx.x & 63, qw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row_in_wave = lane & 31, half = lane >> 5;
-  char* const tiles = lds + (MAPS == 2 ? 0 : wave * kTile);
 
   // the workgroups of one batch and key head read the same keys: on the same XCD
   int id = xcd_number();
@@ -73,7 +66,7 @@ __global__ __launch_bounds__(64 * QW * KW * (3 - MAPS), 2) void k_differential(D
   const uint32_t token = live ? row / group : 0;
   const int head = hk * p.group + (live ? (int)(row - token * group) : 0);
 
-  // the keys of this workgroup: tiles first .. last - 1, of which group kw takes every KW-th
+  // the keys of this workgroup: tiles first .. last - 1
   const int n = length_of(p.lengths, b, p.k_tokens);
   const int all_tiles = (int)(((int64_t)n + BN - 1) / BN);
   const int first = (int)((int64_t)all_tiles * split / grid.splits), last = (int)((int64_t)all_tiles * (split + 1) / grid.splits);
@@ -83,7 +76,7 @@ __global__ __launch_bounds__(64 * QW * KW * (3 - MAPS), 2) void k_differential(D
   x8 q[MAPS][KS];
 #pragma unroll
   for (int a = 0; a < MAPS; ++a) {
-    const T* const src = at<T>(p.q, b, token, 2 * head + a + map);
+    const T* const src = at<T>(p.q, b, token, 2 * head + a);
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       q[a][k] = x8{};
@@ -102,7 +95,7 @@ __global__ __launch_bounds__(64 * QW * KW * (3 - MAPS), 2) void k_differential(D
   // tile's loads are the same instructions.
   const int tg = threadIdx.x % NT, kr = tg / CK, kc = tg % CK, vr = tg / CV, vc = tg % CV;
   const bool in_k = 8 * kc < p.dim, in_v = 8 * vc < p.value_dim;
-  const T* const ksrc = at<T>(p.k, b, 0, 2 * hk + map) + 8 * kc;
+  const T* const ksrc = at<T>(p.k, b, 0, 2 * hk) + 8 * kc;
   const T* const vsrc = at<T>(p.v, b, 0, hk) + 8 * vc;
   const uint8_t* const mask = p.mask ? p.mask + b * p.mask_batch : nullptr;
   s16x8 kreg[MAPS][NK] = {}, vreg[NV] = {};
@@ -157,21 +150,17 @@ __global__ __launch_bounds__(64 * QW * KW * (3 - MAPS), 2) void k_differential(D
       voff[d][s] = MAPS * kKeys + slot<CV>(r, cc) + (lane & 1) * 8;
     }
 
-  const int rounds = (last - first + KW - 1) / KW;
-  if (first + kw < last) fetch(first + kw);
-  for (int i = 0; i < rounds; ++i) {
-    const int tile = first + kw + i * KW;
-    char* const here = tiles + (kBuffers == 2 ? (i & 1) * kTile : 0);
-    uint64_t visible = 0;
-    if (tile < last) visible = store(tile, here);
-    if (QW > 1) __syncthreads();
-    if (tile + KW < last) fetch(tile + KW);
+  if (first < last) fetch(first);
+  for (int tile = first; tile < last; ++tile) {
+    char* const here = lds + ((tile - first) & 1) * kTile;
+    const uint64_t visible = store(tile, here);
+    __syncthreads();
+    if (tile + 1 < last) fetch(tile + 1);
     if (!visible) continue;
-
 #pragma unroll 1
     for (int kb = 0; kb < NB; ++kb) {
       const uint32_t bits = (uint32_t)(visible >> (32 * kb));
-      if (BN > 32 && !bits) continue;
+      if (!bits) continue;
       x8 w[MAPS][2];                                 // the maps' weights: 16 keys each
 #pragma unroll
       for (int a = 0; a < MAPS; ++a) {
@@ -230,131 +219,248 @@ __global__ __launch_bounds__(64 * QW * KW * (3 - MAPS), 2) void k_differential(D
     l[a] = lower + upper;
   }
 
-  if (MAPS == 1) {   // the waves' parts of the same rows
-    float* const part_o = (float*)lds;
-    float* const part_ml = part_o + WAVES * 32 * PT;
-    __syncthreads();
-    if (live) {
+  if (grid.splits > 1) {
+    if (!live) return;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      float* const part = p.parts + (((split * (int64_t)(p.batch * kv_heads) + bh) * rows + row) * 2 + a) * (p.value_dim + 4);
       if (half == 0) {
-        part_ml[2 * (wave * 32 + row_in_wave)] = m[0];
-        part_ml[2 * (wave * 32 + row_in_wave) + 1] = l[0];
+        part[0] = m[a];
+        part[1] = l[a];
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4)
-          *(f32x4*)(part_o + (wave * 32 + row_in_wave) * PT + 32 * d + 2 * e + 4 * half) = f32x4{o[0][d][e], o[0][d][e + 1], o[0][d][e + 2], o[0][d][e + 3]};
-    }
-    __syncthreads();
-    // thread t: row t / 16, values 4 * (t % 16 + 16 * i)
-    const int r = threadIdx.x / 16;
-    const uint32_t at_row = row_tile * 32 + r;
-    if (at_row >= rows) return;
-    constexpr int NI = (VP + 63) / 64;
-    f32x4 sum[2][NI] = {};
-    float mm[2], ll[2];
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      mm[a] = -INFINITY;
-      ll[a] = 0.0f;
-#pragma unroll
-      for (int g = 0; g < KW; ++g) mm[a] = fmaxf(mm[a], part_ml[2 * ((2 * g + a) * 32 + r)]);
-#pragma unroll
-      for (int g = 0; g < KW; ++g) {
-        const int at_part = (2 * g + a) * 32 + r;
-        const float mg = part_ml[2 * at_part], f = mg == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mg - mm[a]) * c);
-        ll[a] = fmaf(part_ml[2 * at_part + 1], f, ll[a]);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int d0 = 4 * (threadIdx.x % 16) + 64 * i;
-          if (d0 < VP) sum[a][i] += f * *(const f32x4*)(part_o + at_part * PT + d0);
+        for (int e = 0; e < 16; e += 4) {
+          const int d0 = 32 * d + 2 * e + 4 * half;
+          if (d0 < p.value_dim) *(f32x4*)(part + 4 + d0) = f32x4{o[a][d][e], o[a][d][e + 1], o[a][d][e + 2], o[a][d][e + 3]};
         }
-      }
-    }
-    const uint32_t tok = at_row / group;
-    const int hh = hk * p.group + (int)(at_row - tok * group);
-    if (grid.splits > 1) {
-#pragma unroll
-      for (int a = 0; a < 2; ++a) {
-        float* const part = p.parts + (((split * (int64_t)(p.batch * kv_heads) + bh) * rows + at_row) * 2 + a) * (p.value_dim + 4);
-        if (threadIdx.x % 16 == 0) {
-          part[0] = mm[a];
-          part[1] = ll[a];
-        }
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int d0 = 4 * (threadIdx.x % 16) + 64 * i;
-          if (d0 < p.value_dim) *(f32x4*)(part + 4 + d0) = sum[a][i];
-        }
-      }
-      return;
-    }
-    const float f0 = inverse_sum(ll[0]), f1 = p.lambda[hh] * inverse_sum(ll[1]);
-    float squares = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      sum[0][i] = difference(sum[0][i], f0, sum[1][i], f1);
-      if (4 * (threadIdx.x % 16) + 64 * i < p.value_dim)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) squares = fmaf(sum[0][i][e], sum[0][i][e], squares);
-    }
-    const float factor = row_factor(p, sum16(squares), ll[0] != 0.0f || ll[1] != 0.0f);
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int d0 = 4 * (threadIdx.x % 16) + 64 * i;
-      if (d0 >= p.value_dim) break;
-      x4 y;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = (T)(sum[0][i][e] * factor * (p.weight ? p.weight[d0 + e] : 1.0f));
-      *(x4*)(at_out<T>(p.out, b, tok, hh) + d0) = y;
     }
     return;
   }
-  if constexpr (MAPS == 2) {
-    if (grid.splits > 1) {
-      if (!live) return;
+  const float f0 = inverse_sum(l[0]), f1 = p.lambda[head] * inverse_sum(l[1]);
+  float squares = 0.0f;                            // (values behind the last are zero)
 #pragma unroll
-      for (int a = 0; a < 2; ++a) {
-        float* const part = p.parts + (((split * (int64_t)(p.batch * kv_heads) + bh) * rows + row) * 2 + a) * (p.value_dim + 4);
-        if (half == 0) {
-          part[0] = m[a];
-          part[1] = l[a];
-        }
+  for (int d = 0; d < DT; ++d) {
+    o[0][d] = difference(o[0][d], f0, o[1][d], f1);
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+    for (int e = 0; e < 16; ++e) squares = fmaf(o[0][d][e], o[0][d][e], squares);
+  }
+  float lower, upper;
+  both_halves(squares, lower, upper);
+  const float factor = row_factor(p, lower + upper, l[0] != 0.0f || l[1] != 0.0f);
+  if (!live) return;
+  T* const dst = at_out<T>(p.out, b, token, head);
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const int d0 = 32 * d + 2 * e + 4 * half;
-            if (d0 < p.value_dim) *(f32x4*)(part + 4 + d0) = f32x4{o[a][d][e], o[a][d][e + 1], o[a][d][e + 2], o[a][d][e + 3]};
-          }
-      }
-      return;
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const int d0 = 32 * d + 2 * e + 4 * half;
+      if (d0 >= p.value_dim) continue;
+      x4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = (T)(o[0][d][e + i] * factor * (p.weight ? p.weight[d0 + i] : 1.0f));
+      *(x4*)(dst + d0) = y;
     }
-    const float f0 = inverse_sum(l[0]), f1 = p.lambda[head] * inverse_sum(l[1]);
-    float squares = 0.0f;                            // (values behind the last are zero)
+}
+
+// Few rows: 16 to a workgroup, whose eight waves take tiles of 32 keys in turn and are joined in LDS.  A wave forms both maps, on
+// products of 16 x 16, whose results (keys 4g .. 4g + 3 of a row in lane group g, two tiles of 16 keys side by side) are
+// operands of the next product.  Keys go from memory into the registers that multiply them; values, which are needed
+// transposed, through LDS of the wave's own.
+constexpr int kFewWaves = 8;
+template <class T, int DP, int VP>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void k_differential_few(DifferentialParams p, DifferentialGrid grid) {
+  typedef typename Vec<T>::x8 x8;
+  typedef typename Vec<T>::x4 x4;
+  constexpr int CV = VP > 64 ? 16 : 8, KS = DP / 32, DT = VP / 16, NV = 32 * CV / 64, kTile = 32 * CV * 16;
+  constexpr int PT = VP + 4;                        // floats per row of a wave's part: reads and writes spread over the banks
+  constexpr int kParts = kFewWaves * 2 * 16 * (PT + 2) * 4, kTiles = kFewWaves * kTile;
+  __shared__ __align__(16) char lds[kParts > kTiles ? kParts : kTiles];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+  char* const here = lds + wave * kTile;
+
+  int id = xcd_number();                            // the workgroups of one batch and key head read the same keys: on the same XCD
+  const int row_tile = id % grid.row_tiles;
+  id /= grid.row_tiles;
+  const int split = id % grid.splits;
+  const int bh = id / grid.splits, kv_heads = p.q_heads / p.group, hk = bh % kv_heads, b = bh / kv_heads;
+  const uint32_t rows = (uint32_t)p.q_tokens * p.group, group = p.group;   // below 2^30
+  const uint32_t row = row_tile * 16 + col;
+  const bool live = row < rows;
+  const uint32_t token = live ? row / group : 0;
+  const int head = hk * p.group + (live ? (int)(row - token * group) : 0);
+  const int n = length_of(p.lengths, b, p.k_tokens), all_tiles = (int)(((int64_t)n + 31) / 32);
+  const int first = (int)((int64_t)all_tiles * split / grid.splits), last = (int)((int64_t)all_tiles * (split + 1) / grid.splits);
+
+  const float c = positive_scale(p.scale) * kLog2e;
+  // a lane has DP / 4 dimensions side by side of a query, as of a key
+  x8 q[2][KS];
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    const T* const src = at<T>(p.q, b, token, 2 * head + a);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      q[a][k] = x8{};
+      const int d0 = (DP / 4) * g + 8 * k;
+      if (live && d0 < p.dim) q[a][k] = *(const x8*)(src + d0);
+      if (p.scale < 0.0f) q[a][k] = -q[a][k];
+      if (p.scale == 0.0f) q[a][k] = x8{};
+    }
+  }
+  f32x4 o[2][DT] = {};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
+
+  const int vr = lane / CV, vc = lane % CV;
+  const bool in_v = 8 * vc < p.value_dim;
+  const T* const ksrc = at<T>(p.k, b, 0, 2 * hk);
+  const T* const vsrc = at<T>(p.v, b, 0, hk) + (in_v ? 8 * vc : 0);
+  const uint8_t* const mask = p.mask ? p.mask + b * p.mask_batch : nullptr;
+  x8 key[2][2][KS];                                 // [keys][map]
+  s16x8 vreg[NV];
+  uint8_t seen = 0;
+  auto fetch = [&](int tile) {                      // (what lies behind the last key, or behind a head's dimensions, is read as what is there)
+    const int64_t j0 = (int64_t)tile * 32, end = (int64_t)n - 1;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const T* const from = ksrc + std::min(j0 + 16 * t + col, end) * p.k.token;
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) key[t][a][k] = __builtin_bit_cast(x8, load16(from + a * p.k.head + std::min((DP / 4) * g + 8 * k, p.dim - 8)));
+    }
+#pragma unroll
+    for (int e = 0; e < NV; ++e) vreg[e] = load16(vsrc + std::min(j0 + vr + e * (64 / CV), end) * p.v.token);
+    if (mask) seen = mask[std::min(j0 + (lane & 31), end)];
+  };
+  int voff[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) voff[d] = slot<CV>(4 * g + (col >> 2), 2 * d + (col >> 1 & 1)) + (col & 1) * 8;
+
+  if (first + wave < last) fetch(first + wave);
+  for (int tile = first + wave; tile < last; tile += kFewWaves) {
+    uint32_t visible = ~0u;
+    const int64_t left = n - (int64_t)tile * 32;
+    if (left < 32) visible = (1u << left) - 1;
+    if (mask) visible &= (uint32_t)__ballot(seen != 0);
+#pragma unroll
+    for (int e = 0; e < NV; ++e) {
+      const int r = vr + e * (64 / CV);
+      if (!(visible >> r & 1) || !in_v) vreg[e] = s16x8{};       // hidden values as zeros, whatever they hold
+      *(s16x8*)(here + slot<CV>(r, vc)) = vreg[e];
+    }
+    f32x4 s[2][2];                                  // [map][keys]
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[a][t] = f32x4{};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const bool there = (DP / 4) * g + 8 * k < p.dim;
+          s[a][t] = mfma16(there ? key[t][a][k] : x8{}, q[a][k], s[a][t]);
+        }
+      }
+    if (tile + kFewWaves < last) fetch(tile + kFewWaves);
+    if (!visible) continue;
+    wave_order();
+    x8 w[2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      if (visible != ~0u) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(visible >> (16 * t + 4 * g + i) & 1)) s[a][t][i] = -INFINITY;
+      }
+      float top = s[a][0][0];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, s[a][0][i]), s[a][1][i]);
+      top = column_max(top);
+      if (__any((top - m[a]) * c > kSlack)) {
+        const float raised = fmaxf(m[a], top), keep = m[a] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m[a] - raised) * c);
+        l[a] *= keep;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[a][d] *= keep;
+        m[a] = raised;
+      }
+      const float mc = m[a] == -INFINITY ? 0.0f : fmaf(m[a], c, -kRaise<T>);
+      float w8[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w8[i] = __builtin_amdgcn_exp2f(fmaf(s[a][i / 4][i % 4], c, -mc));
+      l[a] += ((w8[0] + w8[1]) + (w8[2] + w8[3])) + ((w8[4] + w8[5]) + (w8[6] + w8[7]));
+      w[a] = round8<T>(w8);
+    }
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      o[0][d] = difference(o[0][d], f0, o[1][d], f1);
+      const x8 v = join8<T>(read_transposed(here + voff[d]), read_transposed(here + voff[d] + 16 * CV * 16));
 #pragma unroll
-      for (int e = 0; e < 16; ++e) squares = fmaf(o[0][d][e], o[0][d][e], squares);
+      for (int a = 0; a < 2; ++a) o[a][d] = mfma16(v, w[a], o[a][d]);
     }
-    float lower, upper;
-    both_halves(squares, lower, upper);
-    const float factor = row_factor(p, lower + upper, l[0] != 0.0f || l[1] != 0.0f);
-    if (!live) return;
-    T* const dst = at_out<T>(p.out, b, token, head);
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int d0 = 32 * d + 2 * e + 4 * half;
-        if (d0 >= p.value_dim) continue;
-        x4 y;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = (T)(o[0][d][e + i] * factor * (p.weight ? p.weight[d0 + i] : 1.0f));
-        *(x4*)(dst + d0) = y;
-      }
+    wave_order();
   }
+
+  // the waves' parts: lane l has values 16 d + 4 g + i of row l % 16
+  float* const part_o = (float*)lds;
+  float* const part_ml = part_o + kFewWaves * 2 * 16 * PT;
+  __syncthreads();
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    l[a] += __shfl_xor(l[a], 16);
+    l[a] += __shfl_xor(l[a], 32);
+    const int at_part = (wave * 2 + a) * 16 + col;
+    if (g == 0) {
+      part_ml[2 * at_part] = m[a];
+      part_ml[2 * at_part + 1] = l[a];
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *(f32x4*)(part_o + at_part * PT + 16 * d + 4 * g) = o[a][d];
+  }
+  __syncthreads();
+  // thread t: row t / 32, values 4 * (t % 32) .. + 3
+  const int r = threadIdx.x / 32, d0 = 4 * (threadIdx.x % 32);
+  const uint32_t at_row = row_tile * 16 + r;
+  if (at_row >= rows) return;
+  f32x4 sum[2] = {};
+  float mm[2], ll[2];
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    mm[a] = -INFINITY;
+    ll[a] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) mm[a] = fmaxf(mm[a], part_ml[2 * ((2 * w + a) * 16 + r)]);
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      const int at_part = (2 * w + a) * 16 + r;
+      const float mw = part_ml[2 * at_part], f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mw - mm[a]) * c);
+      ll[a] = fmaf(part_ml[2 * at_part + 1], f, ll[a]);
+      if (d0 < VP) sum[a] += f * *(const f32x4*)(part_o + at_part * PT + d0);
+    }
+  }
+  const uint32_t tok = at_row / group;
+  const int hh = hk * p.group + (int)(at_row - tok * group);
+  if (grid.splits > 1) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      float* const part = p.parts + (((split * (int64_t)(p.batch * kv_heads) + bh) * rows + at_row) * 2 + a) * (p.value_dim + 4);
+      if (d0 == 0) {
+        part[0] = mm[a];
+        part[1] = ll[a];
+      }
+      if (d0 < p.value_dim) *(f32x4*)(part + 4 + d0) = sum[a];
+    }
+    return;
+  }
+  f32x4 y = difference(sum[0], inverse_sum(ll[0]), sum[1], p.lambda[hh] * inverse_sum(ll[1]));
+  float squares = d0 < p.value_dim ? fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3]))) : 0.0f;
+  squares = sum16(squares);
+  squares += __shfl_xor(squares, 16);
+  const float factor = row_factor(p, squares, ll[0] != 0.0f || ll[1] != 0.0f);
+  if (d0 >= p.value_dim) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] *= factor * (p.weight ? p.weight[d0 + e] : 1.0f);
+  *(x4*)(at_out<T>(p.out, b, tok, hh) + d0) = round4<T>(y);
 }
 
 // The splits' parts of a row, for each map a maximum, a sum and a weighted sum of values: a wave per row.  Lane s has what weighs
@@ -390,9 +496,12 @@ __global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p,
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
     f32x4 sum = {0, 0, 0, 0};
+    const int at_value = d0 < p.value_dim ? d0 : 0;
+#pragma unroll 4
     for (int s = 0; s < splits; s += 2) {
-      const float w = __shfl(f, s + half);          // (of a part that is not there, or saw no key: 0)
-      if (d0 < p.value_dim && w != 0.0f) sum += w * *(const f32x4*)(parts + (s + half) * all * 2 * pitch + 4 + d0);
+      const int part = std::min(s + half, splits - 1);
+      const float w = s + half < splits ? __shfl(f, part) : 0.0f;          // (of a part that saw no key: 0, and so are its sums)
+      sum += w * *(const f32x4*)(parts + part * all * 2 * pitch + 4 + at_value);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], 32);
@@ -405,7 +514,7 @@ __global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p,
     }
     saw = saw || l != 0.0f;
   }
-  float squares = half ? 0.0f : fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3])));
+  float squares = half || d0 >= p.value_dim ? 0.0f : fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3])));
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) squares += __shfl_xor(squares, d);
   const float factor = row_factor(p, squares, saw);
@@ -417,7 +526,7 @@ __global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p,
 
 namespace {
 struct DifferentialPlan {
-  bool wide;                    // eight waves with 32 rows each and the same keys, else eight with the same rows
+  bool wide;                    // eight waves with 32 rows each and the same keys, else eight with the same 16 rows
   DifferentialGrid grid;
   int64_t workgroups;
 };
@@ -429,13 +538,14 @@ DifferentialPlan plan_of(const DifferentialParams& p) {
     return (int)std::max<int64_t>(1, std::min<int64_t>({room / std::max<int64_t>(base, 1), parts, kMostParts}));
   };
   const int cut = at_most(256, wide, keys64 / 8);
-  const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, few = bh * ((rows + 31) / 32);
+  const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, few = bh * ((rows + 15) / 16);
   plan.wide = wide >= 256 || (2 * rows >= wide_tiles * 256 && wide * cut >= 192);
-  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? wide_tiles : (rows + 31) / 32, INT32_MAX);
+  plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? wide_tiles : (rows + 15) / 16, INT32_MAX);
   plan.grid.splits = wide >= 256 ? 1 : cut;
   if (!plan.wide) {
-    const int splits = at_most(512, few, tiles / 8);
-    const bool apart = (tiles + 4 * splits - 1) / (4 * splits) + 3 < (few + 255) / 256 * ((tiles + 3) / 4);
+    // the second launch, which joins the parts, costs as much as some rounds of tiles
+    const int splits = at_most(256, few, tiles / 16);
+    const bool apart = (tiles + 8 * splits - 1) / (8 * splits) + 5 < (few + 255) / 256 * ((tiles + 7) / 8);
     plan.grid.splits = apart ? splits : 1;
   }
   plan.workgroups = bh * plan.grid.row_tiles * plan.grid.splits;
@@ -443,7 +553,7 @@ DifferentialPlan plan_of(const DifferentialParams& p) {
 }
 template <class T, int DP, int VP>
 const void* kernel_of(const DifferentialPlan& plan) {
-  return plan.wide ? (const void*)k_differential<T, DP, VP, 2, 8, 1, 64> : (const void*)k_differential<T, DP, VP, 1, 1, 4, 32>;
+  return plan.wide ? (const void*)k_differential<T, DP, VP> : (const void*)k_differential_few<T, DP, VP>;
 }
 template <class T>
 const void* kernel_of(const DifferentialParams& p, const DifferentialPlan& plan) {
