@@ -41,11 +41,13 @@ __device__ __forceinline__ V difference(V a, float fa, V b, float fb) {
   return a * fa - b * fb;
 }
 
+// Heads and values of more than 64 need more registers than two waves of a SIMD have.
+__host__ __device__ constexpr int wide_waves(int dim, int value_dim) { return dim > 64 && value_dim > 64 ? 4 : 8; }
 template <class T, int DP, int VP>
-__global__ __launch_bounds__(512, 2) void k_differential(DifferentialParams p, DifferentialGrid grid) {
+__global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) void k_differential(DifferentialParams p, DifferentialGrid grid) {
   typedef typename Vec<T>::x8 x8;
   typedef typename Vec<T>::x4 x4;
-  constexpr int MAPS = 2, QW = 8, BN = 64;
+  constexpr int MAPS = 2, QW = wide_waves(DP, VP), BN = 64;
   constexpr int CK = DP > 64 ? 16 : 8, CV = VP > 64 ? 16 : 8, KS = DP / 16, DT = VP / 32, NB = BN / 32;   // CK, CV: 16-byte pieces per row in LDS
   constexpr int NT = 64 * QW;                       // threads that fill a tile together
   constexpr int NK = BN * CK / NT, NV = BN * CV / NT;   // 16-byte loads per thread for one map's keys, and for values
@@ -139,16 +141,13 @@ __global__ __launch_bounds__(512, 2) void k_differential(DifferentialParams p, D
     for (int e = 0; e < NV; ++e) *(s16x8*)(at_tile + MAPS * kKeys + slot<CV>(vr + e * (NT / CV), vc)) = vreg[e];
     return visible;
   };
-  int koff[KS], voff[DT][2];
+  // Chunk c of a row lies at c ^ swizzle: where chunks 4 d + .. lie is where chunk 0 + .. does but for the bits of 4 d.
+  int koff[KS], voff[2];
 #pragma unroll
   for (int k = 0; k < KS; ++k) koff[k] = slot<CK>(row_in_wave, 2 * k + half);
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int r = 8 * s + 4 * half + (lane >> 2 & 3), cc = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-      voff[d][s] = MAPS * kKeys + slot<CV>(r, cc) + (lane & 1) * 8;
-    }
+  for (int s = 0; s < 2; ++s)
+    voff[s] = slot<CV>(8 * s + 4 * half + (lane >> 2 & 3), 2 * (lane >> 4 & 1) + (lane >> 1 & 1)) + (lane & 1) * 8;
 
   if (first < last) fetch(first);
   for (int tile = first; tile < last; ++tile) {
@@ -205,8 +204,8 @@ __global__ __launch_bounds__(512, 2) void k_differential(DifferentialParams p, D
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const char* const at_v = here + (32 * kb + 16 * j) * CV * 16;
-          const x8 v = join8<T>(read_transposed(at_v + voff[d][0]), read_transposed(at_v + voff[d][1]));
+          const char* const at_v = here + MAPS * kKeys + (32 * kb + 16 * j) * CV * 16;
+          const x8 v = join8<T>(read_transposed(at_v + (voff[0] ^ 64 * d)), read_transposed(at_v + (voff[1] ^ 64 * d)));
 #pragma unroll
           for (int a = 0; a < MAPS; ++a) o[a][d] = mfma32(v, w[a][j], o[a][d]);
         }
@@ -533,13 +532,14 @@ struct DifferentialPlan {
 DifferentialPlan plan_of(const DifferentialParams& p) {
   const int64_t bh = (int64_t)p.batch * (p.q_heads / p.group), rows = (int64_t)p.q_tokens * p.group;
   DifferentialPlan plan;
-  const int64_t wide_tiles = (rows + 255) / 256, wide = bh * wide_tiles, keys64 = ((int64_t)p.k_tokens + 63) / 64;
+  const int tile = 32 * wide_waves(p.dim, p.value_dim);
+  const int64_t wide_tiles = (rows + tile - 1) / tile, wide = bh * wide_tiles, keys64 = ((int64_t)p.k_tokens + 63) / 64;
   auto at_most = [](int64_t room, int64_t base, int64_t parts) {
     return (int)std::max<int64_t>(1, std::min<int64_t>({room / std::max<int64_t>(base, 1), parts, kMostParts}));
   };
   const int cut = at_most(256, wide, keys64 / 8);
   const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, few = bh * ((rows + 15) / 16);
-  plan.wide = wide >= 256 || (2 * rows >= wide_tiles * 256 && wide * cut >= 192);
+  plan.wide = wide >= 256 || (2 * rows >= wide_tiles * tile && wide * cut >= 192);
   plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? wide_tiles : (rows + 15) / 16, INT32_MAX);
   plan.grid.splits = wide >= 256 ? 1 : cut;
   if (!plan.wide) {
@@ -570,9 +570,10 @@ size_t differential_workspace(const DifferentialParams& p) {
 hipError_t launch(const DifferentialParams& p, hipStream_t stream) {
   DifferentialParams params = p;
   DifferentialPlan plan = plan_of(p);
+  const unsigned threads = 64 * (plan.wide ? wide_waves(p.dim, p.value_dim) : kFewWaves);
   void* args[] = {&params, &plan.grid};
   const bool half = p.dtype == HS_F16;
-  hipError_t e = launch_kernel(half ? kernel_of<f16>(p, plan) : kernel_of<bf16>(p, plan), plan.workgroups, 512, args, stream);
+  hipError_t e = launch_kernel(half ? kernel_of<f16>(p, plan) : kernel_of<bf16>(p, plan), plan.workgroups, threads, args, stream);
   if (e != hipSuccess || plan.grid.splits == 1) return e;
   void* join_args[] = {&params, &plan.grid.splits};
   return launch_kernel(half ? (const void*)k_differential_join<f16> : (const void*)k_differential_join<bf16>,
