@@ -163,8 +163,9 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
   constexpr int NP = __is_same(T, f16) ? 2 : 1;      // bf16 parts of a key or query
   constexpr int CH = DK > 64 ? 16 : 8, KS = DK / 32, ST = DK / 16;
   constexpr int kTile = kChunk * CH * 16, kValues = kChunk * 8 * 16;
-  constexpr int kK = 0, kQ = NP * kTile, kV = 2 * NP * kTile, kP = kV + kValues, kBuffer = kP + 2 * kChunk * kPPitch;
+  constexpr int kQ = 0, kV = NP * kTile, kP = kV + kValues, kBuffer = kP + 2 * kChunk * kPPitch;
   __shared__ __align__(16) char lds[2 * kBuffer];
+  __shared__ __align__(16) char keys[3][NP * kTile];
   __shared__ __align__(16) float ms[3][kChunk * kMPitch];      // A, then M
   __shared__ ChunkGates gates[4];
 
@@ -206,6 +207,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
     __syncthreads();
     for (int c = 0; c < chunks; ++c) {
       const char* const here = lds + (c & 1) * kBuffer;
+      const char* const k_here = keys[c % 3];
       const ChunkGates& gate = gates[c % 4];
       f32x4 ks[2] = {}, qs[2] = {};                  // K S: tokens x columns; (Q S)^T: columns x tokens
 #pragma unroll
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int e = 0; e < NP; ++e) {
-            const char* const at_k = here + kK + e * kTile + tt * kNext;
+            const char* const at_k = k_here + e * kTile + tt * kNext;
             const char* const at_q = here + kQ + e * kTile + tt * kNext;
             kk[tt][e] = join8<bf16>(*(const s16x4*)(at_k + koff[k][0]), *(const s16x4*)(at_k + koff[k][1]));
             qq[tt][e] = join8<bf16>(*(const s16x4*)(at_q + koff[k][0]), *(const s16x4*)(at_q + koff[k][1]));
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < NP; ++e) {
-            const char* const at_k = here + kK + e * kTile + toff[t0 + t];
+            const char* const at_k = k_here + e * kTile + toff[t0 + t];
             kk[t][e] = join8<bf16>(read_transposed(at_k), read_transposed(at_k + kNext));
           }
         if (NP == 2) {
@@ -324,17 +326,17 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         for (int j = 0; j < here_n; ++j) {
           const float decay = gate.decay[j], beta = gate.beta[j];
           float kt[ST][4], a = 0.0f, e = 0.0f;
-          auto value = [&](int tile, int t, int i) {
+          auto value = [&](const char* tile, int t, int i) {
             const int at_value = slot<CH>(j, 2 * t + (g >> 1)) + (g & 1) * 8 + 2 * i;
-            float y = (float)*(const bf16*)(here + tile + at_value);
-            if (NP == 2) y += (float)*(const bf16*)(here + tile + kTile + at_value);
+            float y = (float)*(const bf16*)(tile + at_value);
+            if (NP == 2) y += (float)*(const bf16*)(tile + kTile + at_value);
             return y;
           };
 #pragma unroll
           for (int t = 0; t < ST; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              kt[t][i] = value(kK, t, i);
+              kt[t][i] = value(k_here, t, i);
               if (16 * t + 4 * g + i < p.key_dim) a = fmaf(kt[t][i], s[t][i], a);
             }
           a += __shfl_xor(a, 16);
@@ -347,7 +349,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
             for (int i = 0; i < 4; ++i) {
               if (16 * t + 4 * g + i >= p.key_dim) continue;
               s[t][i] = fmaf(kt[t][i], uj, decay * s[t][i]);
-              e = fmaf(value(kQ, t, i), s[t][i], e);
+              e = fmaf(value(here + kQ, t, i), s[t][i], e);
             }
           e += __shfl_xor(e, 16);
           e += __shfl_xor(e, 32);
@@ -439,21 +441,33 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
     return;
   }
 
-  // A of chunk c + 2 (role 1); M of chunk c + 1, and its keys in LDS (role 2); P of chunk c + 1, and its queries in LDS (role 3)
+  // A of chunk c + 2, and its keys in LDS (role 1); M of chunk c + 1 (role 2); P of chunk c + 1, and its queries in LDS (role 3)
   const T* const key = at<T>(p.k, b, 0, hk);
   const T* const query = at<T>(p.q, b, 0, hk);
   x8 kk[2][KS], qq[2][KS];
+  // Whether a lane's last 8 dimensions are there; the others are where key_dim is more than 32 * (KS - 1), as most often it is.
+  const bool in_dim = 32 * (KS - 1) + 8 * g < p.key_dim, others = p.key_dim > 32 * (KS - 1);
   auto fetch_rows = [&](const T* from, int64_t stride, int c, x8 (&to)[2][KS]) {
+    const T* const first = from + ((int64_t)c * kChunk + row) * stride + 8 * g;
+    const T* const at_row[2] = {first, first + 16 * stride};
+    if (others && c * kChunk + kChunk <= n) {        // (the same for the whole workgroup)
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const int64_t t = (int64_t)c * kChunk + 16 * tt + row;
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int k = 0; k < KS - 1; ++k) to[tt][k] = __builtin_bit_cast(x8, load16(at_row[tt] + 32 * k));
+      to[0][KS - 1] = to[1][KS - 1] = x8{};
+      if (in_dim)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) to[tt][KS - 1] = __builtin_bit_cast(x8, load16(at_row[tt] + 32 * (KS - 1)));
+      return;
+    }
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const int d0 = 32 * k + 8 * g;
         to[tt][k] = x8{};
-        if (t < n && d0 < p.key_dim) to[tt][k] = __builtin_bit_cast(x8, load16(from + t * stride + d0));
+        if (c * kChunk + 16 * tt + row < n && 32 * k + 8 * g < p.key_dim) to[tt][k] = __builtin_bit_cast(x8, load16(at_row[tt] + 32 * k));
       }
-    }
   };
   auto lay_out = [&](const x8 (&from)[2][KS], char* to) {
 #pragma unroll
@@ -490,6 +504,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
       if (c + 2 < chunks) {
         const ChunkGates& gate = gates[(c + 2) % 4];
         float* const m = ms[(c + 2) % 3];
+        lay_out(kk, keys[(c + 2) % 3]);
 #pragma unroll
         for (int tile = 0; tile < 3; ++tile) {       // (it, jt) = (0, 0), (1, 0), (1, 1)
           const int it = tile > 0, jt = tile > 1;
@@ -509,7 +524,6 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
     return;
   }
   if (role == 2) {
-    if (chunks > 0) fetch_rows(key, p.k.token, 0, kk);
     __syncthreads();
     __syncthreads();
     for (int c = -1; c < chunks; ++c) {
@@ -542,8 +556,6 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         f32x4 w = {0, 0, 0, 0}, y = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) w = __builtin_amdgcn_mfma_f32_16x16x4f32(a21[i], m[(4 * g + i) * kMPitch + row], w, 0, 0, 0);
-        lay_out(kk, lds + ((c + 1) & 1) * kBuffer + kK);
-        if (c + 2 < chunks) fetch_rows(key, p.k.token, c + 2, kk);
 #pragma unroll
         for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(t22[i], w[i], y, 0, 0, 0);
         wave_order();

@@ -257,6 +257,10 @@ hs_status check(const char* fn, const hs_delta_rule_desc* d) {   // all but the 
   HS_TRY(check_dim(fn, "key_dim", d->key_dim));
   HS_TRY(check_dim(fn, "value_dim", d->value_dim));
   if (!std::isfinite(d->scale)) { set_error("%s: scale must be finite", fn); return HS_E_INVAL; }
+  if (d->tokens > INT32_MAX - 1024) {
+    set_error("%s: too many tokens for one call (%d)", fn, d->tokens);
+    return HS_E_INVAL;
+  }
   if ((int64_t)d->batch * d->heads > INT32_MAX) {
     set_error("%s: too many heads of sequences for one call (%d x %d)", fn, d->batch, d->heads);
     return HS_E_INVAL;

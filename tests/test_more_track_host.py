@@ -169,6 +169,7 @@ def test_workspaces(name):
 
 def test_counts_beyond_one_call_are_refused():
     far = heads(batch=1 << 40, token=1 << 20, head=64)
+    refused("hs_delta_rule", delta(tokens=(1 << 31) - 1023, out=far), "too many tokens")
     refused("hs_delta_rule", delta(batch=1 << 20, heads=1 << 14, qk_heads=1, out=far), "too many heads")
     refused("hs_differential_attention", differential(batch=1 << 20, q_heads=1 << 13, kv_heads=1, out=far), "too many heads")
     refused("hs_differential_attention", differential(q_tokens=1 << 30, kv_heads=4, out=far), "too many tokens")
