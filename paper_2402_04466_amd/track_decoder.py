@@ -81,34 +81,53 @@ class TrackDecoder:
             mask = mask.contiguous()
         h, d, stream = self.heads, self.head_dim, torch.cuda.current_stream().cuda_stream
 
-        def tracks(y):                              # [s, f, t, ...] as [s * t, f, ...], without a copy
-            return y.flatten(0, 1).transpose(0, 1) if s == 1 else y.transpose(1, 2).flatten(0, 1)
         positions = self.frame + torch.arange(f, device=self.device)
-        qkv = tracks((x @ self.w_qkv).view(s, f, t, 3, h, d))
+        qkv = self._tracks((x @ self.w_qkv).view(s, f, t, 3, h, d))
         q, k, v = qkv[:, :, 0], qkv[:, :, 1], qkv[:, :, 2]
         self._norm_rotate(stream, q, k, self.w_norm[0], self.w_norm[1], positions)
         mixed = torch.empty(s, f, t, h, d, dtype=self.dtype, device=self.device)
-        desc = api.make_retention_desc(
-            dtype=DTYPES[self.dtype], batch=s * t, tokens=f, q_heads=h, kv_heads=h, key_dim=d, value_dim=d,
-            scale=d ** -0.5, decay=self.decay, q=heads_of(q), k=heads_of(k), v=heads_of(v), out=heads_of(tracks(mixed)),
-            d_state_in=self.state.data_ptr(), d_state_out=self.state.data_ptr())
-        work = self._workspace(desc, api.hs_query_retention_workspace(desc))
-        api.hs_retention(self.ctx, desc, stream)
+        work = self._mix(stream, x, qkv, self._tracks(mixed))
         x = x + mixed.flatten(-2) @ self.w_o
 
         q = (x @ self.w_q2).view(s * f, t, h, d)
         self._norm_rotate(stream, q, None, self.w_norm[2], None, None)
         kv = (maps @ self.w_kv).view(s * f, cells, 2, h, d)
         looked = torch.empty(s * f, t, h, d, dtype=self.dtype, device=self.device)
-        desc = api.make_cross_attention_desc(
-            dtype=DTYPES[self.dtype], batch=s * f, q_tokens=t, k_tokens=cells, q_heads=h, kv_heads=h, head_dim=d,
-            scale=d ** -0.5, q=heads_of(q), k=heads_of(kv[:, :, 0]), v=heads_of(kv[:, :, 1]), out=heads_of(looked),
-            d_mask=0 if mask is None else mask.data_ptr(), mask_batch_stride=cells)
-        work2 = self._workspace(desc, api.hs_query_cross_attention_workspace(desc))
-        api.hs_cross_attention(self.ctx, desc, stream)
+        work2 = self._look(stream, q, kv, looked, mask)
         self.frame += f
         del work, work2                             # (torch reuses them on this stream only)
-        return x + looked.view(s, f, t, c) @ self.w_o2
+        return self._end(stream, x + looked.view(s, f, t, c) @ self.w_o2)
+
+    def _tracks(self, y):
+        """[streams, frames, tools, ...] as [streams * tools, frames, ...], without a copy."""
+        return y.flatten(0, 1).transpose(0, 1) if self.streams == 1 else y.transpose(1, 2).flatten(0, 1)
+
+    def _mix(self, stream, x, qkv, out):
+        """The tracks' tokens (x: what they were projected from), behind norm and rotation, into `out`."""
+        h, d = self.heads, self.head_dim
+        q, k, v = qkv[:, :, 0], qkv[:, :, 1], qkv[:, :, 2]
+        desc = api.make_retention_desc(
+            dtype=DTYPES[self.dtype], batch=q.shape[0], tokens=q.shape[1], q_heads=h, kv_heads=h, key_dim=d, value_dim=d,
+            scale=d ** -0.5, decay=self.decay, q=heads_of(q), k=heads_of(k), v=heads_of(v), out=heads_of(out),
+            d_state_in=self.state.data_ptr(), d_state_out=self.state.data_ptr())
+        work = self._workspace(desc, api.hs_query_retention_workspace(desc))
+        api.hs_retention(self.ctx, desc, stream)
+        return work
+
+    def _look(self, stream, q, kv, out, mask):
+        """Queries on keys and values of the cells, into `out`."""
+        n, t, h, d = q.shape
+        cells = kv.shape[1]
+        desc = api.make_cross_attention_desc(
+            dtype=DTYPES[self.dtype], batch=n, q_tokens=t, k_tokens=cells, q_heads=h, kv_heads=h, head_dim=d,
+            scale=d ** -0.5, q=heads_of(q), k=heads_of(kv[:, :, 0]), v=heads_of(kv[:, :, 1]), out=heads_of(out),
+            d_mask=0 if mask is None else mask.data_ptr(), mask_batch_stride=cells)
+        work = self._workspace(desc, api.hs_query_cross_attention_workspace(desc))
+        api.hs_cross_attention(self.ctx, desc, stream)
+        return work
+
+    def _end(self, stream, x):
+        return x
 
     def live(self, cells: int) -> "LiveTracks":
         return LiveTracks(self, cells)
@@ -139,8 +158,8 @@ class LiveTracks:
         return self.out
 
 
-def main() -> None:
-    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+def run_example(decoder, doc: str) -> None:
+    ap = argparse.ArgumentParser(description=doc.splitlines()[0])
     ap.add_argument("--streams", type=int, default=16)
     ap.add_argument("--frames", type=int, default=600)
     ap.add_argument("--cells", type=int, default=405)
@@ -154,16 +173,20 @@ def main() -> None:
         call()
         torch.cuda.synchronize()
         print(f"{what}: {(time.perf_counter() - t0) / per * 1e6:.1f} us per frame")
-    clip = TrackDecoder(ctx, streams=1)
+    clip = decoder(ctx, streams=1)
     x = torch.randn(1, args.frames, clip.tools, clip.channels, dtype=clip.dtype, device=clip.device)
     maps = torch.randn(1, args.frames, args.cells, clip.channels, dtype=clip.dtype, device=clip.device)
     timed(f"a clip of {args.frames} frames in one call", args.frames, lambda: clip.forward(x, maps))
-    live = TrackDecoder(ctx, streams=args.streams).live(args.cells)
+    live = decoder(ctx, streams=args.streams).live(args.cells)
     live.x.normal_()
     live.maps.normal_()
     timed(f"{args.streams} live streams", args.frames, lambda: [live.step() for _ in range(args.frames)])
     torch.cuda.synchronize()
     api.hs_shutdown(ctx)
+
+
+def main() -> None:
+    run_example(TrackDecoder, __doc__)
 
 
 if __name__ == "__main__":

@@ -184,3 +184,14 @@ def test_gates_are_views_of_float32_tensors():
     for bad in (t.half(), t[0]):
         with pytest.raises(ValueError):
             gates_of(bad)
+
+
+def test_the_expert_decoders_keys_have_length_one_and_its_state_is_the_track_decoders():
+    import torch
+    from paper_2402_04466_amd.track_expert_decoder import ExpertTrackDecoder
+    dec = ExpertTrackDecoder(0, streams=2, heads=2, experts=3, hidden=8, device="cpu")
+    assert torch.equal(dec.w_norm[1], torch.full((64,), 0.125)) and dec.state.shape == (16, 2, 64, 64)
+    with pytest.raises(ValueError, match="even"):
+        ExpertTrackDecoder(0, streams=1, heads=3, device="cpu")
+    with pytest.raises(ValueError, match="one stream"):
+        dec.forward(torch.zeros(2, 2, 8, 128, dtype=torch.float16), torch.zeros(2, 2, 5, 128, dtype=torch.float16))
