@@ -634,9 +634,12 @@ hipError_t launch(const DeltaParams& p, hipStream_t stream) {
   DeltaParams params = p;
   DeltaGrid grid = grid_of(p);
   void* args[] = {&params, &grid};
-  if (p.tokens > 8)
-    return launch_kernel(p.dtype == HS_F16 ? chunks_of<f16>(p) : chunks_of<bf16>(p), (int64_t)p.batch * p.heads * grid.blocks, 64 * (grid.waves + kOtherWaves),
-                         args, stream);
+  // A chunk costs what it costs however few its tokens are, a token by itself more the fuller the device is.  Token by token and in chunks:
+  // 12 and 8.5 us for 12 tokens of 8 tracks (8 heads of 64 x 64), 28 and 25 for 16 of 40 (8 of 96 x 80), 22 and 25 for 12; 166 and 161 for 24
+  // of 128 (16 of 128 x 128), 124 and 149 for 16.
+  const int64_t chunked = (int64_t)p.batch * p.heads * grid.blocks;
+  if (p.tokens > (chunked <= 256 ? 8 : chunked <= 1024 ? 13 : 22))
+    return launch_kernel(p.dtype == HS_F16 ? chunks_of<f16>(p) : chunks_of<bf16>(p), chunked, 64 * (grid.waves + kOtherWaves), args, stream);
   const int64_t workgroups = (int64_t)p.batch * p.heads * ((p.value_dim + 63) / 64);
   return launch_kernel(p.dtype == HS_F16 ? steps_of<f16>(p) : steps_of<bf16>(p), workgroups, 256, args, stream);
 }

@@ -161,12 +161,16 @@ __global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) vo
       const uint32_t bits = (uint32_t)(visible >> (32 * kb));
       if (!bits) continue;
       x8 w[MAPS][2];                                 // the maps' weights: 16 keys each
+      // both maps' scores before either's softmax: those of the second are formed while the first's weights are (1120 us and 932 at 2040 rows of 8
+      // heads on 8160 keys, 8 times)
+      f32x16 scores[MAPS] = {};
+#pragma unroll
+      for (int a = 0; a < MAPS; ++a)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) scores[a] = mfma32(*(const x8*)(here + a * kKeys + kb * 32 * CK * 16 + koff[k]), q[a][k], scores[a]);
 #pragma unroll
       for (int a = 0; a < MAPS; ++a) {
-        const char* const at_k = here + a * kKeys + kb * 32 * CK * 16;
-        f32x16 s = {};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) s = mfma32(*(const x8*)(at_k + koff[k]), q[a][k], s);
+        f32x16& s = scores[a];
         if (bits != ~0u) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)

@@ -293,3 +293,15 @@ def test_offsets_beyond_32_bits(hs, ctx, gen):
     end = torch.empty_like(state)
     delta_call(hs, ctx, q, k, view, out, log_decay, beta, state, end, 0.125)
     check(out, end, reference(q, k, v, log_decay, beta, state, 0.125), t, "far")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("b, n, h, dk, dv", [(70, 12, 8, 40, 24), (70, 14, 8, 40, 24), (300, 22, 8, 16, 16), (300, 23, 8, 16, 16), (1, 9, 1, 8, 128),
+                                             (2, 40, 2, 32, 48), (2, 40, 2, 24, 80)])
+def test_both_forms_next_to_the_number_of_tokens_that_parts_them(hs, ctx, gen, dtype, b, n, h, dk, dv):
+    t = TYPES[dtype]
+    q, k, v, log_decay, beta, state = inputs(gen, b, n, h, h, dk, dv, t)
+    lens = torch.randint(0, n + 1, (b,), generator=gen, device=DEV, dtype=torch.int32)
+    out, end = torch.full((b, n, h, dv), 7.0, dtype=t, device=DEV), torch.full_like(state, 7.0)
+    delta_call(hs, ctx, q, k, v, out, log_decay, beta, state, end, 0.25, lens)
+    check(out, end, reference(q, k, v, log_decay, beta, state, 0.25, lens), t, "next to it")

@@ -245,3 +245,18 @@ def test_offsets_beyond_32_bits(hs, ctx, gen):
     differential_call(hs, ctx, q, kk, vv, out, lam, 0.125)
     want, bound = reference(q, k, v, lam, 0.125, torch.ones(2, nk, dtype=torch.bool, device=DEV), True, 1e-5, None)
     close(out, want, bound, "far")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("d, dv", [(64, 128), (128, 128), (104, 72), (40, 64)])
+@pytest.mark.parametrize("b, nq, nk, hq, hk", [(33, 250, 130, 8, 8), (4, 1000, 1100, 4, 2), (2, 129, 2100, 2, 2), (64, 130, 40, 4, 4)])
+def test_many_rows(hs, ctx, gen, dtype, d, dv, b, nq, nk, hq, hk):
+    """Row tiles enough for the device, and fewer whose keys are cut into parts, the last tiles with rows and keys missing."""
+    t = TYPES[dtype]
+    q, k, v, lam, weight = inputs(gen, b, nq, nk, hq, hk, d, dv, t)
+    seen, lengths, mask = visible(gen, b, nk, True, True)
+    want, bound = reference(q, k, v, lam, d ** -0.5, seen, False, 0.0, None)
+    k[~seen], v[~seen] = float("nan"), float("inf")
+    out = torch.full((b, nq, hq, dv), 7.0, dtype=t, device=DEV)
+    differential_call(hs, ctx, q, k, v, out, lam, d ** -0.5, norm=False, lengths=lengths, mask=mask)
+    close(out, want, bound, "outputs")

@@ -220,3 +220,27 @@ def test_weights_beyond_32_bits(hs, ctx, gen):
     for i in used:
         w_in[i], w_out[i] = normal(gen, 2 * f, ch, dtype=t) * ch ** -0.5, normal(gen, ch, f, dtype=t) * f ** -0.5
     check(hs, ctx, x, router, w_in, w_out, 2)
+
+
+@pytest.mark.parametrize("n, e, top", [(200, 64, 1), (300, 40, 4), (70, 3, 2), (1024, 256, 1)])
+def test_many_tokens_on_an_expert_that_few_are_expected_on(hs, ctx, gen, n, e, top):
+    """All tokens pick the same experts, so that theirs are taken in turn, in every form that the average number asks for."""
+    x, router, w_in, w_out = inputs(gen, n, 64, 72, e, torch.bfloat16)
+    x[:, 0] = 8.0
+    router[:, 0] = 0
+    router[1, 0] = 4.0
+    check(hs, ctx, x, router, w_in, w_out, top)
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own(hs, ctx, gen):
+    sets = [inputs(gen, n, 128, 136, 8, torch.float16) for n in (12, 200)]
+    want = [torch.empty_like(s[0]) for s in sets]
+    keep = [expert_call(hs, ctx, *s, out, 2) for s, out in zip(sets, want)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in sets], [torch.empty_like(s[0]) for s in sets]
+    for _ in range(5):
+        for st, s, out in zip(streams, sets, got):
+            with torch.cuda.stream(st):
+                keep.append(expert_call(hs, ctx, *s, out, 2))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
