@@ -476,7 +476,9 @@ hs_status hs_partition_copy(hs_app* app, void* d_dst, const void* d_src, size_t 
 /* What a decoder with one token per tool and frame is made of, next to the network: a track's
  * tokens carry a state from frame to frame (hs_retention, the counterpart of the ConvLSTM's state
  * per stream) and look at the cells of the frame's feature map (hs_cross_attention); queries and
- * keys of both are normalised and rotated by the frame's number (hs_norm_rotate).
+ * keys of both are normalised and rotated by the frame's number (hs_norm_rotate).  In the place of the first a state that gives up what
+ * it holds for a key (hs_delta_rule), in the place of the second the difference of two looks (hs_differential_attention); behind
+ * either, networks of which each token passes through a few (hs_expert_layer).
  *
  * Every call enqueues its kernels on the caller's HIP stream (hip_stream: a hipStream_t of the
  * context's device, NULL: the default stream) and returns; nothing is allocated, copied to the
@@ -494,7 +496,7 @@ hs_status hs_partition_copy(hs_app* app, void* d_dst, const void* d_src, size_t 
  * must not overlap, and but for the cases named below no output overlaps an input.  Offsets are
  * 64-bit.  Sums, norms, softmax statistics and states are fp32; every output is rounded once.
  * What goes through the matrix pipe on the way is 16 bits wide, each term off by half a step of the
- * inputs' type at most: softmax weights and, in a retention of more than 8 tokens, the weights that
+ * inputs' type at most: softmax weights, an expert's hidden values and, in a retention of more than 8 tokens, the weights that
  * tokens have for each other and the state that queries are multiplied by.  In fp16 these keep all
  * their bits down to 2^-28 of the largest of their row (a token and head, or a column of the state;
  * softmax weights down to 2^-21); what is smaller is off by 2^-32 of the largest. */
@@ -601,12 +603,12 @@ hs_status hs_cross_attention(hs_ctx* ctx, const hs_cross_attention_desc* desc, v
  * a clip or one frame of every live stream.  There is a state for each of `heads` value heads; head h has the query and
  * key of head h / (heads / qk_heads).  Keys are used as they are: of length 1 (hs_norm_rotate with a weight of
  * 1 / sqrt(key_dim)) and beta in [0, 1] the state stays bounded; with longer ones it grows as the formula has it.
- * The state and what enters it are fp32 or, where they go through the matrix pipe, carry 24 bits; queries are multiplied by
- * as much.  A clip cut into calls carries the same state up to the order of these sums.
- * Columns of the state (value dimensions) are apart: what is not finite in a value stays in its column, of the
- * outputs and the state, from its token on; in a key, a gate or a column of the state, every value from there on
- * is infinite or NaN that would be by the formula (which of the two is open); in a query, that token's outputs.  Finite
- * results do not change.  Calls of more than 8 tokens go over the affected parts of a sequence token by token. */
+ * The state and what enters it are fp32 or, where they go through the matrix pipe in calls of several tokens, carry 24 bits of each
+ * value; outputs take 16 bits of each before their own rounding.  A clip cut into calls carries the same state up to the order of these sums.
+ * Columns of the state (value dimensions) are apart.  Where a token or the state holds an infinity or NaN, those outputs and values of
+ * the state are infinite or NaN that are so by the formula (which of the two is open): of a value its own column, of a key or a gate all
+ * of the head's, each from that token on, of the state that column, of a query that token's outputs.  What the formula leaves finite
+ * stays as exact as it is without; such parts of a longer call are gone over token by token, some microseconds each. */
 typedef struct {
   const float* d;               /* DEVICE, 4-byte aligned: first value of batch 0, token 0, head 0 */
   int64_t batch, token, head;   /* strides in elements: any                                        */
@@ -618,7 +620,7 @@ typedef struct {
   int key_dim, value_dim;
   float scale;
   hs_heads q, k, v, out;
-  hs_gates log_decay;           /* natural logarithm of g, at most 0 in use (minus infinity: g = 0); d NULL: g = 1 */
+  hs_gates log_decay;           /* natural logarithm of g, at most 0 in use; minus infinity: g = 0; d NULL: g = 1 */
   hs_gates beta;                /* d NULL: 1                                                       */
   const int32_t* d_lengths;     /* DEVICE [batch] or NULL                                          */
   const float* d_state_in;      /* DEVICE [batch][heads][key_dim][value_dim], NULL: zeros; may be state_out */
@@ -666,8 +668,8 @@ hs_status hs_differential_attention(hs_ctx* ctx, const hs_differential_attention
  *   p_i = exp(s[e_i]) / sum of exp(s) over all experts, or over the chosen ones      (renormalise != 0)
  *   out = sum of p_i * W_out[e_i] (silu(W_gate[e_i] x) * (W_up[e_i] x)),   silu(a) = a / (1 + exp(-a))
  * Scores are compared as summed in 64 bits.  The products' sums are fp32, what the second product takes is rounded to the
- * inputs' type once (in fp16 with a power of two out of each token's row, so that it keeps its bits down to 2^-28 of the
- * row's largest).  Tokens with mask 0 pass through none, whatever they hold: out zero, chosen -1, weights 0.  A
+ * inputs' type once (in fp16 with a power of two out of each token's hidden values, so that they keep their bits down to 2^-28 of the
+ * largest of an expert's).  Tokens with mask 0 pass through none, whatever they hold: out zero, chosen -1, weights 0.  A
  * token that is not finite changes no other token's output.  A score of NaN ranks last. */
 typedef struct {
   int dtype;                    /* hs_dtype of x, out and the weights                              */

@@ -16,6 +16,10 @@ namespace hs {
 // that it reads from LDS is used twice: with a map per wave LDS would be busy as long as the matrix pipe.
 // Few rows (k_differential_few): the waves of a workgroup have the same rows and take the keys in turn.
 // Where either leaves the device idle the keys are cut further, over `splits` workgroups, which k_differential_join puts together.
+//
+// Many rows are bound by exponentials and products in turns (2040 rows of 8 heads of 64 on 8160 keys, values of 128, 8 times: 820 to 930 us,
+// 0.88 to 1.0 PFLOP/s; vector pipe 56 %, matrix pipe 42 % busy), few by their keys' and values' way from memory and the
+// chain of loads, products and join (8 on up to 6480 keys, 48 heads: 26 us, 3.1 TB/s, and 6 for the join; 8 on 405, 4 heads: 10 us).
 struct DifferentialGrid {
   int row_tiles, splits;
 };
