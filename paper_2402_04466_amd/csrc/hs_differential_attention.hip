@@ -511,7 +511,8 @@ __global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p,
 #pragma unroll 4
     for (int s = 0; s < splits; s += 2) {
       const int part = std::min(s + half, splits - 1);
-      const float w = s + half < splits ? __shfl(f, part) : 0.0f;          // (of a part that saw no key: 0, and so are its sums)
+      const float theirs = __shfl(f, part);                                // (from every lane: one that a branch leaves out gives zero)
+      const float w = s + half < splits ? theirs : 0.0f;                   // (of a part that saw no key: 0, and so are its sums)
       sum += w * *(const f32x4*)(parts + part * all * 2 * pitch + 4 + at_value);
     }
 #pragma unroll

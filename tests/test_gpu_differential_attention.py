@@ -260,3 +260,32 @@ def test_many_rows(hs, ctx, gen, dtype, d, dv, b, nq, nk, hq, hk):
     out = torch.full((b, nq, hq, dv), 7.0, dtype=t, device=DEV)
     differential_call(hs, ctx, q, k, v, out, lam, d ** -0.5, norm=False, lengths=lengths, mask=mask)
     close(out, want, bound, "outputs")
+
+
+def parts_of(work, b, nq, hq, dv):
+    """Into how many parts a call cut its keys, by the workspace that they take."""
+    return work.numel() / (b * hq * nq * 2 * (dv + 4) * 4)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("nq, hq, nk, dv, parts", [
+    (8, 4, 16400, 64, 32), (8, 4, 17010, 128, 33), (8, 4, 18360, 64, 35), (8, 4, 24300, 24, 47), (8, 5, 26400, 128, 51),
+    (8, 4, 32640, 64, 63), (8, 4, 33000, 128, 64), (256, 5, 20000, 128, 39), (256, 5, 20000, 64, 39)])
+def test_keys_cut_into_many_parts(hs, ctx, gen, dtype, norm, nq, hq, nk, dv, parts):
+    """Even and odd counts of parts on either side of half a wave.  The last sixty-fourth of the values is large and of one sign, so
+    that a last part that is left out, or added twice, is far beyond the bound."""
+    t = TYPES[dtype]
+    q, k, v, lam, weight = inputs(gen, 1, nq, nk, hq, hq, 64, dv, t)
+    v[:, -(nk // 64):] = v[:, -(nk // 64):].abs() * 16
+    for masked in (False, True):
+        mask = (torch.rand(1, nk, generator=gen, device=DEV) < 0.7).to(torch.uint8) if masked else None
+        lengths = torch.tensor([nk - 3], dtype=torch.int32, device=DEV) if masked else None
+        seen = torch.ones(1, nk, dtype=torch.bool, device=DEV)
+        if masked:
+            seen = (mask != 0) & (torch.arange(nk, device=DEV) < nk - 3)
+        want, bound = reference(q, k, v, lam, 0.125, seen, norm, 1e-5, weight)
+        out = torch.full((1, nq, hq, dv), 7.0, dtype=t, device=DEV)
+        work = differential_call(hs, ctx, q, k, v, out, lam, 0.125, norm=norm, weight=weight, lengths=lengths, mask=mask)
+        assert parts_of(work, 1, nq, hq, dv) == parts
+        close(out, want, bound, "outputs")
