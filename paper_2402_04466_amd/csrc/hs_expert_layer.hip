@@ -285,6 +285,14 @@ __device__ __forceinline__ int most_of(const int16_t* power, int first, int slic
   return most;
 }
 
+// Hidden values times 2^power, power <= 0, by two factors: fp16 has no 2^-25, and values times it that are normal ones keep their bits.
+template <class T>
+__device__ __forceinline__ void lower(typename Vec<T>::x8& values, int power) {
+  const int whole = max(power, -40), half = whole / 2;               // (2^-40 of 2^15 rounds to zero)
+  values *= (T)ldexpf(1.0f, half);
+  values *= (T)ldexpf(1.0f, whole - half);
+}
+
 // The hidden value u of 16 from its gate and its other sum, for 16 threads side by side, which agree on the power of two that fp16 takes out.
 template <class T>
 __device__ __forceinline__ void store_hidden(const ExpertParams& p, const ExpertParts& w, int64_t pair, int slice, int u, bool there, float gate, float up) {
@@ -485,9 +493,9 @@ __global__ __launch_bounds__(256) void k_expert_out(ExpertParams p, ExpertParts 
     if (!kPowers) return;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const T f = (T)ldexpf(1.0f, max(power[i][min(4 * step + (lane >> 4), slices - 1)] - row_power[i], -40));
-      strip.b[i][0] *= f;
-      strip.b[i][1] *= f;
+      const int down = power[i][min(4 * step + (lane >> 4), slices - 1)] - row_power[i];
+      lower<T>(strip.b[i][0], down);
+      lower<T>(strip.b[i][1], down);
     }
   });
 #pragma unroll
@@ -595,7 +603,7 @@ __global__ __launch_bounds__(256, 2) void k_expert_tiles(ExpertParams p, ExpertP
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       if (!whole && 64 * step + 8 * ch >= length) s.b[i] = x8{};
-      if (!IN && kPowers) s.b[i] *= (T)ldexpf(1.0f, max(s.power[i] - row_power[i], -40));
+      if (!IN && kPowers) lower<T>(s.b[i], s.power[i] - row_power[i]);
       if (kVectors % 32 == 0 || r0 + 32 * i < kVectors) *(x8*)(here + slot<8>(r0 + 32 * i, ch)) = s.b[i];
     }
     if (!whole)

@@ -244,3 +244,21 @@ def test_two_calls_at_once_with_workspaces_of_their_own(hs, ctx, gen):
                 keep.append(expert_call(hs, ctx, *s, out, 2))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("apart", [10, 20, 23, 24, 25, 26, 27, 28, 32])
+@pytest.mark.parametrize("n, e, top", [(8, 4, 2), (8, 70, 2), (40, 6, 3), (100, 16, 2), (100, 6, 2), (300, 4, 2)])
+def test_hidden_values_far_below_others_of_their_token(hs, ctx, gen, apart, n, e, top):
+    """Sixteen hidden values side by side are 2^apart and more above a token's others, which alone reach the outputs: their output
+    weights are positive as they are, so that what is lost of them adds up.  In every form that the number of tokens asks for."""
+    ch, f = 64, 40
+    x, router, w_in, w_out = inputs(gen, n, ch, f, e, torch.float16)
+    gate, up = w_in[:, :f].float(), w_in[:, f:].float()
+    up[:, 16:] = gate[:, 16:]                                # silu(a) a > 0; of a = 2^-6 and less about a^2 / 2
+    up[:, :16] *= 2.0 ** 12
+    gate[:, 16:] *= 2.0 ** -6
+    up[:, 16:] *= 2.0 ** (12 - apart + 7)
+    w_in = torch.cat((gate, up), 1).to(torch.float16)
+    w_out = w_out.float().abs() * 2.0 ** min(14, apart - 11)      # outputs of about one
+    w_out[:, :, :16] = 0
+    check(hs, ctx, x, router, w_in, w_out.to(torch.float16), top, what=f"2^{apart}")
