@@ -639,7 +639,8 @@ hs_status hs_delta_rule(hs_ctx* ctx, const hs_delta_rule_desc* desc, void* hip_s
  *   out = y / sqrt(mean(y^2) + eps) * weight                                          (norm != 0)
  * q has 2 * q_heads heads, q_0 and q_1 of head h being heads 2h and 2h + 1, k has 2 * kv_heads likewise, v has kv_heads
  * and out q_heads heads; head h has the keys and values of head h / (q_heads / kv_heads).  Visible keys as in
- * hs_cross_attention (lengths, mask; hidden keys and values are not used whatever they hold); a token that sees no key gets zeros.
+ * hs_cross_attention (lengths, mask; hidden keys and values are not used whatever they hold); a token that sees no key gets zeros,
+ * one whose visible scores are all minus infinity, in either map, NaN.  Scores are fp32: products beyond that are infinite.
  * The difference is formed and normalised in fp32. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k, v, out                                        */

@@ -36,7 +36,8 @@ __device__ __forceinline__ float sum16(float x) {
   return x + moved<0x140>(x);              // 15 - lane
 }
 
-__device__ __forceinline__ float inverse_sum(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
+// A map's sum is zero where no key is seen, which m = -INFINITY says, or where all scores are, which leaves 0 / 0.
+__device__ __forceinline__ float inverse_sum(float m, float l) { return m == -INFINITY ? 0.0f : 1.0f / l; }
 // What a row's values are multiplied by: its norm's inverse, 0 for a row that saw nothing.
 __device__ __forceinline__ float row_factor(const DifferentialParams& p, float squares, bool saw) {
   return !saw ? 0.0f : p.norm ? rsqrtf(squares / (float)p.value_dim + p.eps) : 1.0f;
@@ -184,9 +185,9 @@ __global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) vo
           for (int e = 0; e < 16; ++e)
             if (!(bits >> (4 * half) >> (8 * (e / 4) + e % 4) & 1)) s[e] = -INFINITY;
         }
-        float top = s[0];
+        float top = kLowest;                           // (some key is seen)
 #pragma unroll
-        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
         float lo, hi;
         both_halves(top, lo, hi);
         top = fmaxf(lo, hi);
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) vo
           for (int d = 0; d < DT; ++d) o[a][d] *= keep;
           m[a] = raised;
         }
-        const float mc = m[a] == -INFINITY ? 0.0f : fmaf(m[a], c, -kRaise<T>);
+        const float mc = exponent_of<T>(m[a], c);
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -mc));
         float part[4];
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) vo
     }
     return;
   }
-  const float f0 = inverse_sum(l[0]), f1 = p.lambda[head] * inverse_sum(l[1]);
+  const float f0 = inverse_sum(m[0], l[0]), f1 = p.lambda[head] * inverse_sum(m[1], l[1]);
   float squares = 0.0f;                            // (values behind the last are zero)
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) vo
   }
   float lower, upper;
   both_halves(squares, lower, upper);
-  const float factor = row_factor(p, lower + upper, l[0] != 0.0f || l[1] != 0.0f);
+  const float factor = row_factor(p, lower + upper, m[0] != -INFINITY);
   if (!live) return;
   T* const dst = at_out<T>(p.out, b, token, head);
 #pragma unroll
@@ -385,7 +386,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_differential_few(Differen
           for (int i = 0; i < 4; ++i)
             if (!(visible >> (16 * t + 4 * g + i) & 1)) s[a][t][i] = -INFINITY;
       }
-      float top = s[a][0][0];
+      float top = kLowest;                             // (some key is seen)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, s[a][0][i]), s[a][1][i]);
       top = column_max(top);
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_differential_few(Differen
         for (int d = 0; d < DT; ++d) o[a][d] *= keep;
         m[a] = raised;
       }
-      const float mc = m[a] == -INFINITY ? 0.0f : fmaf(m[a], c, -kRaise<T>);
+      const float mc = exponent_of<T>(m[a], c);
       float w8[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) w8[i] = __builtin_amdgcn_exp2f(fmaf(s[a][i / 4][i % 4], c, -mc));
@@ -463,11 +464,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_differential_few(Differen
     }
     return;
   }
-  f32x4 y = difference(sum[0], inverse_sum(ll[0]), sum[1], p.lambda[hh] * inverse_sum(ll[1]));
+  f32x4 y = difference(sum[0], inverse_sum(mm[0], ll[0]), sum[1], p.lambda[hh] * inverse_sum(mm[1], ll[1]));
   float squares = d0 < p.value_dim ? fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3]))) : 0.0f;
   squares = sum16(squares);
   squares += __shfl_xor(squares, 16);
-  const float factor = row_factor(p, squares, ll[0] != 0.0f || ll[1] != 0.0f);
+  const float factor = row_factor(p, squares, mm[0] != -INFINITY);
   if (d0 >= p.value_dim) return;
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] *= factor * (p.weight ? p.weight[d0 + e] : 1.0f);
@@ -517,14 +518,14 @@ __global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p,
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], 32);
-    const float inv = inverse_sum(l);
+    const float inv = inverse_sum(top, l);
     if (a == 0) {
       y = sum;
       first = inv;
     } else {
       y = difference(y, first, sum, p.lambda[head] * inv);
     }
-    saw = saw || l != 0.0f;
+    saw = top != -INFINITY;                        // (of both maps alike)
   }
   float squares = half || d0 >= p.value_dim ? 0.0f : fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3])));
 #pragma unroll

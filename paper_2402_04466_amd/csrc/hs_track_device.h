@@ -132,7 +132,13 @@ constexpr float kSlack = 8.0f;
 // fp16 weights are formed 2^7 times as large, below 2^15 then: those of up to 2^-21 of the largest keep all their bits, and
 // what is lost of the others stays below 2^-32 of it.
 template <class T> constexpr float kRaise = __is_same(T, f16) ? 7.0f : 0.0f;
+// A row's maximum is at least this once it has seen a key, so that one whose scores are all minus infinity is told from one that sees none.
+constexpr float kLowest = -3.402823466e38f;
 constexpr float kLn2 = 0.69314718055994530942f;
+
+// What is taken off scores times c: a maximum's, and a number where that is beyond fp32.
+template <class T>
+__device__ __forceinline__ float exponent_of(float m, float c) { return m == -INFINITY ? 0.0f : fmaxf(fmaf(m, c, -kRaise<T>), kLowest); }
 
 __device__ __forceinline__ float positive_scale(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale); }
 

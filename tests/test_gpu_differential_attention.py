@@ -289,3 +289,43 @@ def test_keys_cut_into_many_parts(hs, ctx, gen, dtype, norm, nq, hq, nk, dv, par
         work = differential_call(hs, ctx, q, k, v, out, lam, 0.125, norm=norm, weight=weight, lengths=lengths, mask=mask)
         assert parts_of(work, 1, nq, hq, dv) == parts
         close(out, want, bound, "outputs")
+
+
+# One key at a time per wave, keys cut into parts, row tiles, row tiles whose keys are cut.
+FORMS = [(2, 3, 500, 4), (1, 8, 6480, 2), (33, 250, 130, 8), (1, 256, 20000, 5)]
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("b, nq, nk, h", FORMS)
+def test_rows_whose_scores_are_all_minus_infinity_are_nan(hs, ctx, gen, norm, b, nq, nk, h):
+    """A visible key is seen whatever its score: 0 / 0, in either map, of infinite queries and of scores beyond fp32."""
+    t = torch.bfloat16
+    q, k, v, lam, weight = inputs(gen, b, nq, nk, h, h, 64, 64, t)
+    k[..., 0] = k[..., 0].abs() + 4
+    clean, out = (torch.empty(b, nq, h, 64, dtype=t, device=DEV) for _ in range(2))
+    differential_call(hs, ctx, q, k, v, clean, lam, 0.125, norm=norm, weight=weight)
+    q[-1, 0, 0] = torch.tensor([-math.inf] + [0.0] * 63, dtype=t, device=DEV)
+    q[-1, 2, 2 * h - 1, 0] = -3e38
+    q[0, 1, 2:4, 0] = -math.inf
+    differential_call(hs, ctx, q, k, v, out, lam, 0.125, norm=norm, weight=weight)
+    bad = torch.zeros(b, nq, h, dtype=torch.bool, device=DEV)
+    bad[-1, 0, 0], bad[-1, 2, h - 1], bad[0, 1, 1] = True, True, True
+    assert torch.isnan(out[bad]).all()
+    assert torch.equal(out[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("last", [True, False])
+@pytest.mark.parametrize("b, nq, nk, h", FORMS)
+def test_keys_of_minus_infinity_among_others_weigh_nothing(hs, ctx, gen, b, nq, nk, h, last):
+    """The first or last nine tenths of the keys, whole tiles and parts of them, have scores below fp32's range: as if they were hidden."""
+    t = torch.bfloat16
+    q, k, v, lam, _ = inputs(gen, b, nq, nk, h, h, 64, 64, t)
+    q[..., 0], k[..., 0] = 0.0, 0.0
+    none = torch.arange(nk, device=DEV) >= nk // 10 if last else torch.arange(nk, device=DEV) < nk - nk // 10
+    seen = (~none).expand(b, nk)
+    want, bound = reference(q, k, v, lam, 0.125, seen, False, 0.0, None)
+    q[..., 0] = -3e38
+    k[:, none, :, 0] = 4.0
+    out = torch.empty(b, nq, h, 64, dtype=t, device=DEV)
+    differential_call(hs, ctx, q, k, v, out, lam, 0.125, norm=False)
+    close(out, want, bound, "outputs")
