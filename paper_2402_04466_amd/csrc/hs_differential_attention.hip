@@ -38,9 +38,9 @@ __device__ __forceinline__ float sum16(float x) {
 
 // A map's sum is zero where no key is seen, which m = -INFINITY says, or where all scores are, which leaves 0 / 0.
 __device__ __forceinline__ float inverse_sum(float m, float l) { return m == -INFINITY ? 0.0f : 1.0f / l; }
-// What a row's values are multiplied by: its norm's inverse, 0 for a row that saw nothing.
-__device__ __forceinline__ float row_factor(const DifferentialParams& p, float squares, bool saw) {
-  return !saw ? 0.0f : p.norm ? rsqrtf(squares / (float)p.value_dim + p.eps) : 1.0f;
+// What a row's values are multiplied by: its norm's inverse.
+__device__ __forceinline__ float row_factor(const DifferentialParams& p, float squares) {
+  return p.norm ? rsqrtf(squares / (float)p.value_dim + p.eps) : 1.0f;
 }
 
 // a fa - b fb with both products rounded, so that equal maps leave nothing.
@@ -260,7 +260,8 @@ __global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) vo
   }
   float lower, upper;
   both_halves(squares, lower, upper);
-  const float factor = row_factor(p, lower + upper, m[0] != -INFINITY);
+  const float factor = row_factor(p, lower + upper);
+  const bool saw = m[0] != -INFINITY;              // (both maps alike; else zeros, whatever lambda and the weights are)
   if (!live) return;
   T* const dst = at_out<T>(p.out, b, token, head);
 #pragma unroll
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(64 * wide_waves(DP, VP), wide_waves(DP, VP) / 4) vo
       if (d0 >= p.value_dim) continue;
       x4 y;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = (T)(o[0][d][e + i] * factor * (p.weight ? p.weight[d0 + i] : 1.0f));
+      for (int i = 0; i < 4; ++i) y[i] = (T)(saw ? o[0][d][e + i] * factor * (p.weight ? p.weight[d0 + i] : 1.0f) : 0.0f);
       *(x4*)(dst + d0) = y;
     }
 }
@@ -468,10 +469,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_differential_few(Differen
   float squares = d0 < p.value_dim ? fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3]))) : 0.0f;
   squares = sum16(squares);
   squares += __shfl_xor(squares, 16);
-  const float factor = row_factor(p, squares, mm[0] != -INFINITY);
+  const float factor = row_factor(p, squares);
   if (d0 >= p.value_dim) return;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] *= factor * (p.weight ? p.weight[d0 + e] : 1.0f);
+  for (int e = 0; e < 4; ++e) y[e] = mm[0] != -INFINITY ? y[e] * factor * (p.weight ? p.weight[d0 + e] : 1.0f) : 0.0f;
   *(x4*)(at_out<T>(p.out, b, tok, hh) + d0) = round4<T>(y);
 }
 
@@ -530,10 +531,10 @@ __global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p,
   float squares = half || d0 >= p.value_dim ? 0.0f : fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3])));
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) squares += __shfl_xor(squares, d);
-  const float factor = row_factor(p, squares, saw);
+  const float factor = row_factor(p, squares);
   if (half || d0 >= p.value_dim) return;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] *= factor * (p.weight ? p.weight[d0 + e] : 1.0f);
+  for (int e = 0; e < 4; ++e) y[e] = saw ? y[e] * factor * (p.weight ? p.weight[d0 + e] : 1.0f) : 0.0f;
   *(x4*)(at_out<T>(p.out, b, token, head) + d0) = round4<T>(y);
 }
 

@@ -329,3 +329,16 @@ def test_keys_of_minus_infinity_among_others_weigh_nothing(hs, ctx, gen, b, nq, 
     out = torch.empty(b, nq, h, 64, dtype=t, device=DEV)
     differential_call(hs, ctx, q, k, v, out, lam, 0.125, norm=False)
     close(out, want, bound, "outputs")
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("b, nq, nk, h", FORMS)
+def test_rows_that_see_nothing_are_zero_whatever_lambda_and_weight(hs, ctx, gen, norm, bad, b, nq, nk, h):
+    q, k, v, lam, weight = inputs(gen, b, nq, nk, h, h, 64, 64, torch.float16)
+    lam[0], weight[5] = bad, bad
+    mask = torch.zeros(nk, dtype=torch.uint8, device=DEV).expand(b, nk)
+    for seen in (dict(mask=mask), dict(lengths=torch.zeros(b, dtype=torch.int32, device=DEV))):
+        out = torch.full((b, nq, h, 64), 7.0, dtype=q.dtype, device=DEV)
+        differential_call(hs, ctx, q, k, v, out, lam, 0.125, norm=norm, weight=weight, **seen)
+        assert not out.any()                                 # (a NaN counts as any)
