@@ -26,6 +26,11 @@ class ExpertTrackDecoder(TrackDecoder):
                  hidden: int = 1024, dtype: torch.dtype = torch.float16, seed: int = 0, device: str = "cuda:0"):
         if heads % 2:
             raise ValueError("heads must be even: two of them are compared")
+        for name, value, step, most in (("head_dim", head_dim, 16, 64), ("heads * head_dim", heads * head_dim, 16, api.HS_MAX_CHANNELS),
+                                        ("hidden", hidden, 8, api.HS_MAX_CHANNELS), ("experts", experts, 1, api.HS_MAX_EXPERTS),
+                                        ("top", top, 1, min(api.HS_MAX_TOP, experts))):
+            if not step <= value <= most or value % step:          # (values are twice as wide as head_dim, and 128 the most)
+                raise ValueError(f"{name} must be a multiple of {step} in {step}..{most}, got {value}")
         super().__init__(ctx, streams=streams, tools=tools, heads=heads, head_dim=head_dim, dtype=dtype, seed=seed, device=device)
         c, self.top, self.hidden = self.channels, top, hidden
         g = torch.Generator().manual_seed(seed + 1)

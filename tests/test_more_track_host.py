@@ -195,3 +195,21 @@ def test_the_expert_decoders_keys_have_length_one_and_its_state_is_the_track_dec
         ExpertTrackDecoder(0, streams=1, heads=3, device="cpu")
     with pytest.raises(ValueError, match="one stream"):
         dec.forward(torch.zeros(2, 2, 8, 128, dtype=torch.float16), torch.zeros(2, 2, 5, 128, dtype=torch.float16))
+
+
+@pytest.mark.parametrize("bad, name", [
+    (dict(head_dim=128), "head_dim"), (dict(head_dim=72), "head_dim"), (dict(head_dim=24), "head_dim"), (dict(head_dim=0), "head_dim"),
+    (dict(heads=258), "heads"), (dict(heads=0), "heads"), (dict(hidden=12), "hidden"), (dict(hidden=0), "hidden"),
+    (dict(hidden=16392), "hidden"), (dict(experts=257), "experts"), (dict(experts=0), "experts"), (dict(top=0), "top"),
+    (dict(top=9), "top"), (dict(experts=2, top=3), "top")])
+def test_the_expert_decoder_refuses_what_its_operators_do(bad, name):
+    """When it is made, not at the first frame."""
+    from paper_2402_04466_amd.track_expert_decoder import ExpertTrackDecoder
+    with pytest.raises(ValueError, match=name):
+        ExpertTrackDecoder(0, **{**dict(streams=1, heads=2, device="cpu"), **bad})
+
+
+@pytest.mark.parametrize("head_dim", [16, 64])
+def test_the_expert_decoders_widest_and_narrowest_heads(head_dim):
+    from paper_2402_04466_amd.track_expert_decoder import ExpertTrackDecoder
+    assert ExpertTrackDecoder(0, streams=1, heads=2, head_dim=head_dim, experts=8, top=8, hidden=8, device="cpu").channels == 2 * head_dim
