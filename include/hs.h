@@ -573,7 +573,8 @@ hs_status hs_retention(hs_ctx* ctx, const hs_retention_desc* desc, void* hip_str
  * A key j of batch b is visible if j < lengths[b] (all without lengths; values outside 0..k_tokens
  * are taken as the nearer end) and, with a mask, mask[b][j] != 0.  Hidden keys and values are not used
  * whatever they hold (infinities and NaN included).  A token that sees no key gets zeros and a log-sum-exp
- * of minus infinity. */
+ * of minus infinity; one whose visible scores are all minus infinity NaN, with the same log-sum-exp.  Scores are fp32: products
+ * beyond that are infinite. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k, v, out                                        */
   int batch, q_tokens, k_tokens;
@@ -640,7 +641,7 @@ hs_status hs_delta_rule(hs_ctx* ctx, const hs_delta_rule_desc* desc, void* hip_s
  * q has 2 * q_heads heads, q_0 and q_1 of head h being heads 2h and 2h + 1, k has 2 * kv_heads likewise, v has kv_heads
  * and out q_heads heads; head h has the keys and values of head h / (q_heads / kv_heads).  Visible keys as in
  * hs_cross_attention (lengths, mask; hidden keys and values are not used whatever they hold); a token that sees no key gets zeros,
- * one whose visible scores are all minus infinity, in either map, NaN.  Scores are fp32: products beyond that are infinite.
+ * one whose visible scores are all minus infinity, in either map, NaN.
  * The difference is formed and normalised in fp32. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k, v, out                                        */

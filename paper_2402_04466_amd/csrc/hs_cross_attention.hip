@@ -175,7 +175,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
           if (!(bits >> (8 * (e / 4) + e % 4) & 1)) s[kb][e] = -INFINITY;
       }
     }
-    float top = s[0][0];
+    float top = kLowest;                               // (some key is seen)
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
       for (int d = 0; d < DT; ++d) o[d] *= keep;
       m = raised;
     }
-    const float mc = m == -INFINITY ? 0.0f : fmaf(m, c, -kRaise<T>);
+    const float mc = exponent_of<T>(m, c);
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
         ll = fmaf(part_ml[2 * (g * QW * 32 + r) + 1], f[g], ll);
       }
       const bool whole = grid.splits == 1;
-      const float inv = whole ? ll > 0.0f ? 1.0f / ll : ll == 0.0f ? 0.0f : ll : 1.0f;
+      const float inv = whole ? inverse_sum(mm, ll) : 1.0f;
       const uint32_t tok = at_row / group;
       const int hh = hk * p.group + (int)(at_row - tok * group);
       const int64_t part_row = (int64_t)(split * (int64_t)(p.batch * kv_heads) + bh) * rows + at_row;
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * QW * KW, 2) void k_cross(CrossParams p, CrossG
       }
     return;
   }
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  const float inv = inverse_sum(m, l);
   T* const dst = at_out<T>(p.out, b, token, head);
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p, int splits) {
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], 32);
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  const float inv = inverse_sum(top, l);
   if (half == 0 && d0 < p.dim) *(x4*)(at_out<T>(p.out, b, token, head) + d0) = round4<T>(sum * inv);
   if (p.lse && lane == 0) p.lse[(b * p.q_heads + head) * p.q_tokens + token] = l == 0.0f ? -INFINITY : fmaf(top, scale, logf(l) - kRaise<T> * kLn2);
 }

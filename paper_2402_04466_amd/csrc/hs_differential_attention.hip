@@ -36,8 +36,6 @@ __device__ __forceinline__ float sum16(float x) {
   return x + moved<0x140>(x);              // 15 - lane
 }
 
-// A map's sum is zero where no key is seen, which m = -INFINITY says, or where all scores are, which leaves 0 / 0.
-__device__ __forceinline__ float inverse_sum(float m, float l) { return m == -INFINITY ? 0.0f : 1.0f / l; }
 // What a row's values are multiplied by: its norm's inverse.
 __device__ __forceinline__ float row_factor(const DifferentialParams& p, float squares) {
   return p.norm ? rsqrtf(squares / (float)p.value_dim + p.eps) : 1.0f;

@@ -140,6 +140,9 @@ constexpr float kLn2 = 0.69314718055994530942f;
 template <class T>
 __device__ __forceinline__ float exponent_of(float m, float c) { return m == -INFINITY ? 0.0f : fmaxf(fmaf(m, c, -kRaise<T>), kLowest); }
 
+// A softmax's sum is zero where no key is seen, which m = -INFINITY says, or where all scores are minus infinity, which leaves 0 / 0.
+__device__ __forceinline__ float inverse_sum(float m, float l) { return m == -INFINITY ? 0.0f : 1.0f / l; }
+
 __device__ __forceinline__ float positive_scale(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale); }
 
 // The order of the products before it and of the LDS reads that they take one each: two groups of reads, then each group's products

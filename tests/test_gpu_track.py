@@ -745,3 +745,52 @@ def test_retention_of_every_width(hs, ctx, gen, dtype, dk, dv, b, n, h):
     work = retention_call(hs, ctx, q, k, v, out, state, end, decay, dk ** -0.5, lengths)
     assert (work.numel() > 0) == (n > 1000)
     retention_check(out, end, ref, t, n, "widths")
+
+
+# Few rows, few rows whose keys are cut, row tiles, row tiles whose keys are cut.
+ATTENTION_FORMS = [(2, 3, 500, 4), (1, 8, 6480, 4), (33, 250, 130, 8), (1, 256, 20000, 5)]
+
+
+@pytest.mark.parametrize("b, nq, nk, h", ATTENTION_FORMS)
+def test_rows_whose_scores_are_all_minus_infinity_are_nan(hs, ctx, gen, b, nq, nk, h):
+    """A visible key is seen whatever its score: 0 / 0, of an infinite query and of scores beyond fp32; the sum's logarithm is minus
+    infinity."""
+    t = torch.bfloat16
+    q, k, v = (normal(gen, b, n, h, 64, dtype=t) for n in (nq, nk, nk))
+    k[..., 0] = k[..., 0].abs() + 4
+    clean, out = torch.empty_like(q), torch.empty_like(q)
+    lse, lse_clean = torch.empty(b, h, nq, device=DEV), torch.empty(b, h, nq, device=DEV)
+    cross_call(hs, ctx, q, k, v, clean, 0.125, lse=lse_clean)
+    q[-1, 0, 0] = torch.tensor([-math.inf] + [0.0] * 63, dtype=t, device=DEV)
+    q[0, 2, h - 1, 0] = -3e38
+    cross_call(hs, ctx, q, k, v, out, 0.125, lse=lse)
+    bad = torch.zeros(b, nq, h, dtype=torch.bool, device=DEV)
+    bad[-1, 0, 0], bad[0, 2, h - 1] = True, True
+    assert torch.isnan(out[bad]).all() and (lse.transpose(1, 2)[bad] == -math.inf).all()
+    assert torch.equal(out[~bad], clean[~bad]) and torch.equal(lse.transpose(1, 2)[~bad], lse_clean.transpose(1, 2)[~bad])
+
+
+@pytest.mark.parametrize("last", [True, False])
+@pytest.mark.parametrize("b, nq, nk, h", ATTENTION_FORMS)
+def test_keys_of_minus_infinity_among_others_weigh_nothing(hs, ctx, gen, b, nq, nk, h, last):
+    """The first or last nine tenths of the keys, whole tiles and parts of them, have scores below fp32's range: as if they were hidden."""
+    t = torch.bfloat16
+    q, k, v = (normal(gen, b, n, h, 64, dtype=t) for n in (nq, nk, nk))
+    none = torch.arange(nk, device=DEV) >= nk // 10 if last else torch.arange(nk, device=DEV) < nk - nk // 10
+    q[..., 0], k[..., 0] = -3e38, 0.0
+    k[:, none, :, 0] = 4.0
+    out, lse = torch.empty_like(q), torch.empty(b, h, nq, device=DEV)
+    cross_call(hs, ctx, q, k, v, out, 0.125, lse=lse)
+    q[..., 0] = 0.0
+    cross_check(out, lse, q, k, v, 0.125, (~none).expand(b, nk), "as hidden")
+
+
+@pytest.mark.parametrize("b, nq, nk, h", ATTENTION_FORMS)
+def test_rows_that_see_no_key_are_zero(hs, ctx, gen, b, nq, nk, h):
+    q, k, v = (normal(gen, b, n, h, 64, dtype=torch.bfloat16) for n in (nq, nk, nk))
+    q[:, 1] = -math.inf
+    for seen in (dict(mask=torch.zeros(1, nk, dtype=torch.uint8, device=DEV).expand(b, nk)),
+                 dict(lengths=torch.zeros(b, dtype=torch.int32, device=DEV))):
+        out, lse = torch.full_like(q, 7.0), torch.full((b, h, nq), 7.0, device=DEV)
+        cross_call(hs, ctx, q, k, v, out, 0.125, lse=lse, **seen)
+        assert not out.any() and (lse == -math.inf).all()
