@@ -605,7 +605,7 @@ hs_status hs_cross_attention(hs_ctx* ctx, const hs_cross_attention_desc* desc, v
  * key of head h / (heads / qk_heads).  Keys are used as they are: of length 1 (hs_norm_rotate with a weight of
  * 1 / sqrt(key_dim)) and beta in [0, 1] the state stays bounded; with longer ones it grows as the formula has it.
  * The state and what enters it are fp32 or, where they go through the matrix pipe in calls of several tokens, carry 24 bits of each
- * value; outputs take 16 bits of each before their own rounding.  A clip cut into calls carries the same state up to the order of these sums.
+ * value; outputs take 16 bits of each, rounded, before their own rounding.  A clip cut into calls carries the same state up to the order of these sums.
  * Columns of the state (value dimensions) are apart.  Where a token or the state holds an infinity or NaN, those outputs and values of
  * the state are infinite or NaN that are so by the formula (which of the two is open): of a value its own column, of a key or a gate all
  * of the head's, each from that token on, of the state that column, of a query that token's outputs.  What the formula leaves finite

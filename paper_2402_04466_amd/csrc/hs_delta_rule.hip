@@ -115,25 +115,23 @@ __global__ __launch_bounds__(256, ROWS > 4 ? 4 : 6) void k_delta_steps(DeltaPara
 // 4g .. 4g + 3, 16 + 4g .. 16 + 4g + 3.
 //
 // Precision.  What enters the state is exact to 24 bits: the state and U go through the matrix pipe as three bf16 parts
-// (8 bits each, split by truncation, which is exact and cannot overflow), fp16 keys and queries as two, M in fp32.
-// Outputs, which are rounded to 16 bits, take two parts of each: 16 bits.
+// (8 bits each, rounded, what is left is exact; a value that bf16 rounds to infinity sends its chunk the way of infinities), fp16 keys and
+// queries as two, M in fp32.  Outputs, which are rounded to 16 bits, take two parts of each and not the two second parts' product: at most 3 * 2^-17
+// of a query times a value of the state, 2^-15 of a weight times a U.  Parts that are cut off, not rounded, lose four times that
+// (8 x 7200 tokens 520 us, 531 rounded).
 //
 // Bound by a chunk's chain of products and splits in the state's waves, one of which a SIMD has beside one of the others: 8 x 7200 tokens of
-// 16 heads of 128 x 128, 225 chunks one after the other in 256 workgroups, take 525 us, 2.3 us a chunk (vector pipe 49 %, matrix pipe 29 %, LDS
+// 16 heads of 128 x 128, 225 chunks one after the other in 256 workgroups, take 531 us, 2.4 us a chunk (vector pipe 49 %, matrix pipe 29 %, LDS
 // 38 % busy; the state's waves alone 500, without their products with the state 365, without its splits 430).
 constexpr int kChunk = 32, kStateWaves = 4, kOtherWaves = 4;
 constexpr int kMPitch = 36;                          // floats per row of M: 16 rows' same 16 bytes lie in different banks
 constexpr int kPPitch = 80;                          // bytes per row of P: as well
 
 typedef Vec<bf16>::x8 b8;
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ uint32_t bits_of(float x) { return __builtin_bit_cast(uint32_t, x); }
-__device__ __forceinline__ float upper_half(float x) { return __builtin_bit_cast(float, bits_of(x) & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack_upper(float even, float odd) { return __builtin_amdgcn_perm(bits_of(odd), bits_of(even), 0x07060302u); }
-
-// Eight values as PARTS bf16 vectors that add up to them (exactly, for three).
+// Eight values as PARTS bf16 vectors that add up to them (exactly, for three), each part rounded: two parts leave at most 2^-17 of a value.
 template <int PARTS>
 __device__ __forceinline__ void split8(const float* x, b8* part) {
   float rest[8];
@@ -141,14 +139,19 @@ __device__ __forceinline__ void split8(const float* x, b8* part) {
   for (int i = 0; i < 8; ++i) rest[i] = x[i];
 #pragma unroll
   for (int n = 0; n < PARTS; ++n) {
-    u32x4 words;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) words[i] = pack_upper(rest[2 * i], rest[2 * i + 1]);
-    part[n] = __builtin_bit_cast(b8, words);
+    part[n] = round8<bf16>(rest);
     if (n + 1 < PARTS)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rest[i] -= upper_half(rest[i]);
+      for (int i = 0; i < 8; ++i) rest[i] -= (float)part[n][i];
   }
+}
+
+// The larger of `most` and of the magnitudes, as whole numbers, of eight bf16 values: 0x7f80 and more of infinities and NaN.
+__device__ __forceinline__ u16x2 most_of(u16x2 most, b8 x) {
+  const u32x4 words = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, words[i] & 0x7fff7fffu));
+  return most;
 }
 
 struct ChunkGates {                                  // of one chunk
@@ -278,6 +281,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] = u[0][i], y[4 + i] = u[1][i];
       split8<2>(y, part);
+      u16x2 most = most_of(u16x2{0, 0}, part[0]);
       f32x4 o[2] = {}, fresh[ST] = {};
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
@@ -297,6 +301,7 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
         for (int i = 0; i < 4; ++i) y[4 * tt + i] *= left[i];
       }
       split8<3>(y, part);
+      most = most_of(most, part[0]);
       const float whole = gate.since[kChunk - 1];
 #pragma unroll
       for (int t0 = 0; t0 < ST; t0 += 2) {
@@ -320,13 +325,8 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
           for (int t = 0; t < 2; ++t) fresh[t0 + t] = mfma16(kk[t][0], part[e], fresh[t0 + t]);
       }
 
-      // Something is not finite: the recurrence says where it goes, token by token.
-      float most = 0.0f;
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) most += u[tt][i] * 0.0f;
-      if (__any(most != 0.0f)) {
+      // Something is not finite, or not as bf16: the recurrence says where it goes, token by token.
+      if (__any(std::max(most[0], most[1]) >= 0x7f80)) {
         const int here_n = min(kChunk, n - c * kChunk);
         for (int j = 0; j < here_n; ++j) {
           const float decay = gate.decay[j], beta = gate.beta[j];
@@ -597,11 +597,11 @@ __global__ __launch_bounds__(64 * (kStateWaves + kOtherWaves)) void k_delta_chun
           for (int i = 0; i < 4; ++i) d[i] = it == jt && 4 * g + i > row ? 0.0f : w[i] * d[i];
         }
         char* const to = next + kP + (16 * it + row) * kPPitch + 16 * g + 8 * jt;
-        float rest[4];
+        const Vec<bf16>::x4 hi = round4<bf16>(d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rest[i] = d[i] - upper_half(d[i]);
-        *(u32x2*)to = u32x2{pack_upper(d[0], d[1]), pack_upper(d[2], d[3])};
-        *(u32x2*)(to + kChunk * kPPitch) = u32x2{pack_upper(rest[0], rest[1]), pack_upper(rest[2], rest[3])};
+        for (int i = 0; i < 4; ++i) d[i] -= (float)hi[i];
+        *(Vec<bf16>::x4*)to = hi;
+        *(Vec<bf16>::x4*)(to + kChunk * kPPitch) = round4<bf16>(d);
       }
       if (c + 2 < chunks) {
         fetch_rows(key, p.k.token, c + 2, kk);

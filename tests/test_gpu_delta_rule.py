@@ -305,3 +305,85 @@ def test_both_forms_next_to_the_number_of_tokens_that_parts_them(hs, ctx, gen, d
     out, end = torch.full((b, n, h, dv), 7.0, dtype=t, device=DEV), torch.full_like(state, 7.0)
     delta_call(hs, ctx, q, k, v, out, log_decay, beta, state, end, 0.25, lens)
     check(out, end, reference(q, k, v, log_decay, beta, state, 0.25, lens), t, "next to it")
+
+
+def of_two_parts(dtype):
+    """What outputs lose of a product with a state's or token's 24 bits that go through the matrix pipe as two bf16 parts, each rounded: 2^-17 of what
+    the parts leave, and 2^-16 for the two second parts' product where the other factor has more than 8 bits too."""
+    return 2.0 ** -17 + (2.0 ** -16 if dtype == torch.float16 else 0.0)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("dk", [8, 64, 128])
+@pytest.mark.parametrize("n", [3, 40])
+def test_what_a_state_loses_on_its_way_to_outputs(hs, ctx, gen, dtype, dk, n):
+    """A state that stays as it is (beta 0, no decay), of values whose last bits all count the same way in products that nearly cancel."""
+    t = TYPES[dtype]
+    half = dk // 2
+    a = 1 + 2.0 ** -7 - 2.0 ** -10 if dtype == "fp16" else 1.0            # cut off after 8 bits it would lose nearly 2^-7 (nothing)
+    for s in (1 + 2.0 ** -7 - 2.0 ** -23, 1 + 2.0 ** -8 + 2.0 ** -15 - 2.0 ** -23, None):
+        q = torch.full((1, n, 1, dk), -1.0, device=DEV)
+        state = torch.empty(1, 1, dk, 8, device=DEV)
+        if s is None:
+            q[..., :half], state[:, :, :half] = normal(gen, n, 1, half), normal(gen, half, 8)
+        else:
+            q[..., :half], state[:, :, :half] = a, s
+        q = q.to(t)
+        state[:, :, half:] = (q[0, 0, 0, :half, None].float() * state[:, :, :half]).to(torch.bfloat16).float()
+        k, v = normal(gen, 1, n, 1, dk, dtype=t), normal(gen, 1, n, 1, 8, dtype=t)
+        out, end = torch.empty(1, n, 1, 8, dtype=t, device=DEV), torch.empty_like(state)
+        delta_call(hs, ctx, q, k, v, out, None, torch.zeros(1, n, 1, device=DEV), state, end, 1.0)
+        assert torch.equal(end, state)
+        want = (q[0, :, 0].double() @ state[0, 0].double())[None, :, None]
+        size = (q[0, :, 0].double().abs() @ state[0, 0].double().abs())[None, :, None]
+        bound = half_step(t) * want.abs() * (1 + 2.0 ** -8) + (of_two_parts(t) + (dk + 32) * F32) * size + smallest(t)
+        close(out, want, bound, f"state of {s}")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n", [4, 32, 50])
+def test_what_tokens_lose_on_their_way_to_outputs(hs, ctx, gen, dtype, n):
+    """Keys that have nothing in common, so that each token adds beta times its value, 24 bits of it, which later tokens' queries
+    weigh; as above.  The weights are in two parts as well: 2^-16 for the two second parts' product, 2^-17 for what each leaves."""
+    t, dk = TYPES[dtype], 64
+    k = torch.eye(dk, device=DEV)[:n].view(1, n, 1, dk).to(t)
+    a = 1 + 2.0 ** -7 - 2.0 ** -10 if dtype == "fp16" else 1.0
+    for crafted in (True, False):
+        q = torch.full((1, n, 1, dk), -1.0, device=DEV)
+        q[..., 0::2] = a if crafted else normal(gen, n, 1, dk // 2)
+        q = q.to(t)
+        v = torch.ones(1, n, 1, 8, dtype=t, device=DEV)
+        beta = torch.empty(1, n, 1, device=DEV)
+        beta[:, 0::2] = 1 + 2.0 ** -7 - 2.0 ** -23 if crafted else torch.rand(1, n, 1, generator=gen, device=DEV)[:, 0::2]
+        beta[:, 1::2] = (a * beta[:, 0:n // 2 * 2:2]).to(torch.bfloat16).float()
+        out, end = torch.empty(1, n, 1, 8, dtype=t, device=DEV), torch.empty(1, 1, dk, 8, device=DEV)
+        delta_call(hs, ctx, q, k, v, out, None, beta, None, end, 1.0)
+        weights = torch.tril(q[0, :, 0, :n].double())                     # of token j for token i
+        u = beta[0].double().expand(n, 8)
+        want, size = (weights @ u)[None, :, None], (weights.abs() @ u.abs())[None, :, None]
+        bound = half_step(t) * want.abs() * (1 + 2.0 ** -8) + (2.0 ** -15 + (n + 32) * F32) * size + smallest(t)
+        close(out, want, bound, f"crafted {crafted}")
+
+
+@pytest.mark.parametrize("n", [3, 40])
+def test_finite_values_beyond_the_largest_of_bf16(hs, ctx, gen, n):
+    """fp32 goes a little further than bf16: such values of the state, and of a token's value times beta, stay what they are."""
+    t, dk, dv = torch.bfloat16, 16, 24
+    far = 3.4e38
+    assert torch.isinf(torch.tensor(far).to(t)) and far < torch.finfo(torch.float32).max
+    k = torch.zeros(1, n, 1, dk, dtype=t, device=DEV)
+    k[0, 1, 0, 3] = 1.0
+    q = torch.full_like(k, 2.0 ** -20)
+    v = torch.zeros(1, n, 1, dv, dtype=t, device=DEV)
+    v[0, 1, 0, 5] = torch.finfo(t).max
+    beta = torch.full((1, n, 1), far / torch.finfo(t).max, device=DEV)
+    state = torch.zeros(1, 1, dk, dv, device=DEV)
+    state[0, 0, 7, 2], state[0, 0, 8, 20] = far, 1.5
+    out, end = torch.empty(1, n, 1, dv, dtype=t, device=DEV), torch.empty_like(state)
+    delta_call(hs, ctx, q, k, v, out, None, beta, state, end, 1.0)
+    want = state.clone()
+    want[0, 0, 3, 5] = (v[0, 1, 0, 5].float() * beta[0, 1, 0])
+    assert torch.equal(end, want) and torch.isfinite(want).all()
+    for i in range(n):
+        y = (want if i >= 1 else state)[0, 0].double().sum(0) * 2.0 ** -20
+        close(out[0, i, 0], y, (half_step(t) + 16 * F32) * y.abs() + smallest(t), f"token {i}")
