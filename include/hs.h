@@ -605,7 +605,8 @@ hs_status hs_cross_attention(hs_ctx* ctx, const hs_cross_attention_desc* desc, v
  * key of head h / (heads / qk_heads).  Keys are used as they are: of length 1 (hs_norm_rotate with a weight of
  * 1 / sqrt(key_dim)) and beta in [0, 1] the state stays bounded; with longer ones it grows as the formula has it.
  * The state and what enters it are fp32 or, where they go through the matrix pipe in calls of several tokens, carry 24 bits of each
- * value; outputs take 16 bits of each, rounded, before their own rounding.  A clip cut into calls carries the same state up to the order of these sums.
+ * value; outputs take 16 bits of each, rounded, before their own rounding.  A clip cut into calls carries the same state up to the order of
+ * these sums.  In a call of several tokens a decay over up to 32 of them that is below 2^-126 leaves nothing.
  * Columns of the state (value dimensions) are apart.  Where a token or the state holds an infinity or NaN, those outputs and values of
  * the state are infinite or NaN that are so by the formula (which of the two is open): of a value its own column, of a key or a gate all
  * of the head's, each from that token on, of the state that column, of a query that token's outputs.  What the formula leaves finite
@@ -642,7 +643,7 @@ hs_status hs_delta_rule(hs_ctx* ctx, const hs_delta_rule_desc* desc, void* hip_s
  * and out q_heads heads; head h has the keys and values of head h / (q_heads / kv_heads).  Visible keys as in
  * hs_cross_attention (lengths, mask; hidden keys and values are not used whatever they hold); a token that sees no key gets zeros,
  * one whose visible scores are all minus infinity, in either map, NaN.
- * The difference is formed and normalised in fp32. */
+ * The difference is formed and normalised in fp32, where a mean of squares beyond its range is infinite and leaves zeros. */
 typedef struct {
   int dtype;                    /* hs_dtype of q, k, v, out                                        */
   int batch, q_tokens, k_tokens;

@@ -616,7 +616,8 @@ namespace {
 DeltaGrid grid_of(const DeltaParams& p) {
   const int columns = (p.value_dim + 15) / 16;
   DeltaGrid grid;
-  // as many of the state's waves in a workgroup as leave a workgroup for every CU
+  // As many of the state's waves in a workgroup as leave a workgroup for every CU, since all of them wait for the waves that prepare its chunks:
+  // 2048 tokens of 128 heads of 128 x 128 (8 sequences of 16) in four waves 170 us, in two 295, in one 552; of 64 of 64 x 64 in four 109, in one 99.
   grid.waves = std::min(kStateWaves, columns);
   while (grid.waves > 1 && (int64_t)p.batch * p.heads * ((columns + grid.waves - 1) / grid.waves) < 256) --grid.waves;
   grid.blocks = (columns + grid.waves - 1) / grid.waves;

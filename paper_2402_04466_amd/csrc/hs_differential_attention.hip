@@ -12,16 +12,19 @@ namespace hs {
 // share keys), S^T = K Q^T leaves each row's scores in one lane pair, and O^T += V^T P^T takes them, rounded to 16 bits
 // once, from the lanes that have them.
 // That rounding spares a second product for what it leaves; where weights are spread over thousands of keys, and the difference
-// is as small as what they average, half a step in each weight (bf16: up to 2^-8 of it) counts like the output's own rounding: an rms error of 2.5e-3 on 8160 keys, where
-// the rounded output alone has 1.7e-3 (fp16: 3.0e-4 and 2.1e-4 on 405).  bf16 values as fp16 with weights of 11 bits, where that is
-// exact, reach 1.7e-3, for a launch more and 924 -> 1076 us.
+// is as small as what they average, half a step in each weight (bf16: up to 2^-8 of it) counts like the output's own rounding: an rms error
+// of 2.55e-3 on 8160 keys, where the rounded output alone has 1.66e-3 (fp16: 3.2e-4 and 2.1e-4).  Weights in two parts, which need two thirds
+// as many products again and registers that are not there, reach that for 840 -> 1230 us (2040 rows of 8 heads, 8 times); both maps' second
+// parts in one product, by the ratio of the sums so far, for 1280; the first map's alone, 1003, would leave something of equal maps; bf16
+// values as fp16 with weights of 11 bits, where that is exact, take a launch more and 924 -> 1076 us.
 //
-// Many rows (k_differential): eight waves have other rows and share the tiles; a wave forms both maps of its rows, so that each value
-// that it reads from LDS is used twice: with a map per wave LDS would be busy as long as the matrix pipe.
+// Many rows (k_differential): eight waves, or four where heads and values are both of more than 64, have other rows and share the tiles; a wave
+// forms both maps of its rows, so that each value that it reads from LDS is used twice: with a map per wave LDS would be busy as
+// long as the matrix pipe.
 // Few rows (k_differential_few): the waves of a workgroup have the same rows and take the keys in turn.
 // Where either leaves the device idle the keys are cut further, over `splits` workgroups, which k_differential_join puts together.
 //
-// Many rows are bound by exponentials and products in turns (2040 rows of 8 heads of 64 on 8160 keys, values of 128, 8 times: 820 to 930 us,
+// Many rows are bound by exponentials and products in turns (2040 rows of 8 heads of 64 on 8160 keys, values of 128, 8 times: 800 to 930 us,
 // 0.88 to 1.0 PFLOP/s; vector pipe 56 %, matrix pipe 42 % busy), few by their keys' and values' way from memory and the
 // chain of loads, products and join (8 on up to 6480 keys, 48 heads: 26 us, 3.1 TB/s, and 6 for the join; 8 on 405, 4 heads: 10 us).
 struct DifferentialGrid {
@@ -538,7 +541,7 @@ __global__ __launch_bounds__(256) void k_differential_join(DifferentialParams p,
 
 namespace {
 struct DifferentialPlan {
-  bool wide;                    // eight waves with 32 rows each and the same keys, else eight with the same 16 rows
+  bool wide;                    // k_differential: eight or four waves with 32 rows each and the same keys; else eight with the same 16 rows
   DifferentialGrid grid;
   int64_t workgroups;
 };
@@ -550,13 +553,22 @@ DifferentialPlan plan_of(const DifferentialParams& p) {
   auto at_most = [](int64_t room, int64_t base, int64_t parts) {
     return (int)std::max<int64_t>(1, std::min<int64_t>({room / std::max<int64_t>(base, 1), parts, kMostParts}));
   };
+  // Where row tiles are too few for the device their keys are cut into parts of eight tiles and more, if at least half of the rows are there
+  // and that fills most of it: 256 tokens of 5 heads on 20000 keys 61 us, 72 by the other form; with parts of four tiles 66, of sixteen 72; 1000
+  // on 2000 (4 times, 4 heads) 61, 63 and 72.  Where it fills less the other form is taken: 500 on 3000 (twice, 4 heads) 36 us and 48, 129 on 2100
+  // (twice, 2 heads) 18 and 38; from about half of the device on it is the slower one: 1000 on 1100 (4 times, 4 heads on 2) 64 and 52.
   const int cut = at_most(256, wide, keys64 / 8);
   const int64_t tiles = ((int64_t)p.k_tokens + 31) / 32, few = bh * ((rows + 15) / 16);
+  // Row tiles enough for the device are taken whatever their rows: 128 tokens on 405 keys (64 times, 4 heads) 37 us, 82 by the other form, 100
+  // tokens 36 and 72, 40 tokens 32 and 32, 130 on 40 keys 13 and 58.  With fewer rows it is the slower one: 8 on 405 keys (64 times) 31 and 15,
+  // (600 times) 296 and 146.  Rows that fill less than the device are taken by the other form on a few keys too, of whose waves most have none
+  // then: 1755 tokens on 5 keys of 4 heads 14 us, 20 by row tiles, of 12 heads 38 and 20; 2040 on 405 of 12 heads 65 and 37.
   plan.wide = wide >= 256 || (2 * rows >= wide_tiles * tile && wide * cut >= 192);
   plan.grid.row_tiles = (int)std::min<int64_t>(plan.wide ? wide_tiles : (rows + 15) / 16, INT32_MAX);
   plan.grid.splits = wide >= 256 ? 1 : cut;
   if (!plan.wide) {
-    // the second launch, which joins the parts, costs as much as some rounds of tiles
+    // Parts of sixteen tiles and more (8 tokens of 4 heads on 6480 keys 19 us, with eight 21, with 24 21).  The second launch, which joins them,
+    // costs as much as five rounds of tiles: on 1001 keys 15.6 us in one launch and 15.0 in two, on 2040 24.3 and 15.4; 5 x 77 on 1001 15.2 and 15.3.
     const int splits = at_most(256, few, tiles / 16);
     const bool apart = (tiles + 8 * splits - 1) / (8 * splits) + 5 < (few + 255) / 256 * ((tiles + 7) / 8);
     plan.grid.splits = apart ? splits : 1;

@@ -10,15 +10,19 @@ namespace {
 
 // The choice (k_expert_route), the hidden layer, what comes out of each expert, and the sum over a token's experts (k_expert_sum):
 // up to 64 tokens by strips of 16 weight rows (k_expert_in, k_expert_out), a frame's 16 with the choice and the hidden layer in one
-// launch (k_expert_frame); more by tiles of 128 rows (k_expert_tiles).
+// launch (k_expert_frame); more by tiles of 64 (k_expert_tiles).
 // Bound by the weights' way from memory: 128 tokens, 4 of 32 experts of 1024 x 2048, take 95 us, of them 50 and 33 for the products' 268 and 134
 // MB (5.4 and 4.0 TB/s); a frame's 8 tokens 22 us for 33 MB, a chain of three launches; 1024 tokens 193 us, in which staging tokens, products and
 // weights hide each other only in part (each left out saves 20 to 40).
 // A product has a weight's rows as its first and tokens as its second operand, so that few tokens waste little of the matrix pipe, and
 // every weight that is needed is read once, straight from memory into the registers that multiply it.
+// Hidden values enter the second product rounded to 16 bits: a second part would double their way through memory and that product's work.
+// It counts like the output's own rounding: an rms error of 2.3e-3 in bf16, where the rounded output alone has 1.65e-3, 3.0e-4 in fp16 and 2.1e-4.
 //
 // fp16: hidden values are kept divided by a power of two, one for each token and 16 of them, which lets them neither overflow nor lose
 // bits; the second product takes all of a token's divided by their largest.
+// Strips up to here: 3 of 6 experts of 520 x 1336 take 22.7 us for 24 tokens and 23.9 for 48, in tiles 25.3 and 26.2.  With more experts strips are
+// the slower ones: 64 tokens, 4 of 32 of 1024 x 2048, 123 us and 95, 2 of 16 of 512 x 1024 28.6 and 26.9.
 constexpr int kFewTokens = 64;
 constexpr int kSlice = 16;
 constexpr int kNoPower = -1000;                      // of a slice of zeros
@@ -719,15 +723,23 @@ template <class T>
 hipError_t launch_of(const ExpertParams& p, hipStream_t stream) {
   ExpertParams params = p;
   ExpertParts parts = parts_of(p);
+  // Weights are asked for before it is known that they are needed where each expert has a token on average: 8 tokens, 2 of 16 of 512 x 1024,
+  // 20.9 us, 21.3 without.  Of experts without a token they are read in vain: 2 tokens, 2 of 64 of 1024 x 1024, 59 and 41, 8 tokens 70 and 54;
+  // of large ones with one token each too many are, by chance: 16 tokens, 2 of 32 of 1024 x 2048, 81.6 and 76.5.
   int ahead = (int64_t)p.tokens * p.top >= p.experts;
   void* args[] = {&params, &parts, &ahead};
-  // In one launch where every workgroup, which works the choice out by itself, has a CU of its own: 8 tokens on 16 experts of 512 x 1024 21.3 us,
-  // 25.7 with the choice in a launch of its own; on 64 experts, four workgroups per CU, 73 and 38.
+  // In one launch where every workgroup, which works the choice out by itself, has a CU of its own: 8 tokens on 16 experts of 512 x 1024 20.9 us,
+  // 25.4 with the choice in a launch of its own; on 64 experts, four workgroups per CU, 73 and 38.  And where the router is small enough, of
+  // which every workgroup reads all: 16 experts of 1024 x 1024 29.1 and 32.0, of 2048 channels 53.8 and 51.6, of 3584 82.5 and 76.3;
+  // 32 of 512 x 512 22.8 and 22.5, of 1024 channels 33.6 and 28.7; 64 of 256 x 256 21.9 and 24.5, of 512 channels 29.9 and 29.2, of 1024 44.3 and 37.8.
   const bool frame = p.tokens <= 16 && p.experts <= kFusedExperts && p.experts * ((slices_of(p) + 3) / 4) <= 256 && (p.experts + 15) / 16 * p.channels <= 2048;
   hipError_t e = hipSuccess;
   if (!frame) e = launch_kernel((const void*)k_expert_route<T>, p.tokens, 256, args, stream);
   if (e != hipSuccess) return e;
-  const int64_t each = (int64_t)p.tokens * p.top / p.experts;          // tokens of an expert, on average
+  // Tiles of 32, 64 or 160 tokens by an expert's tokens on average, which are less than a tile holds, as some experts have more.
+  // 4 of 32 experts of 1024 x 2048: 20 tokens each 100, 102 and 137 us, 24 118, 104 and 138, 48 178, 139 and 151, 56 190, 151 and 155,
+  // 64 209, 171 and 162, 128 353, 255 and 226.
+  const int64_t each = (int64_t)p.tokens * p.top / p.experts;
   if (p.tokens <= kFewTokens) e = p.tokens <= 16 ? launch_few<T, 1>(p, frame, args, stream) : launch_few<T, 2>(p, false, args, stream);
   else e = each <= 20 ? launch_tiles<T, 2, 3, 4>(p, args, stream) : each <= 48 ? launch_tiles<T, 4, 3, 3>(p, args, stream) : launch_tiles<T, 10, 2, 2>(p, args, stream);
   return e != hipSuccess ? e : launch_kernel((const void*)k_expert_sum<T>, ((int64_t)p.tokens * (p.channels / 8) + 255) / 256, 256, args, stream);

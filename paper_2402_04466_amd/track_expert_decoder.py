@@ -12,7 +12,7 @@ import torch
 
 from . import api
 from .harness import gates_of, heads_of
-from .track_decoder import DTYPES, LiveTracks, TrackDecoder, run_example
+from .track_decoder import DTYPES, TrackDecoder, run_example
 
 
 class ExpertTrackDecoder(TrackDecoder):
@@ -87,9 +87,6 @@ class ExpertTrackDecoder(TrackDecoder):
             keep.append(self._workspace(desc, api.hs_query_expert_layer_workspace(desc)))
             api.hs_expert_layer(self.ctx, desc, stream)
         return x + out.view(x.shape)
-
-    def live(self, cells: int) -> LiveTracks:
-        return LiveTracks(self, cells)
 
 
 if __name__ == "__main__":
